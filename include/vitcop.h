@@ -497,6 +497,75 @@ int vitcop_decode_attn(const uint16_t* q, const uint16_t* k, const uint16_t* v, 
                        float* lse_out, int B, int N, int Hq, int Hkv, int d, float scale,
                        void* ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------------
+ * 4 bits for what a decoding step streams: the KV cache a (pruned) prefill left behind, and the weights.
+ * The format: groups of VITCOP_MX4_GROUP neighbouring values of a row share an exponent byte s and stand for
+ * code * 2^(s - 127); a code is four bits, sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (in this order; the
+ * sign is bit 3), two codes to a byte, the lower index in the lower half.  4.25 bits a value; every value is
+ * a bf16, and the products below are those of vitcop_decode_attn and vitcop_project on these values.
+ * To 4 bits: s - 127 is the least exponent in [-125,125] for which no magnitude of the group is above
+ * 7 * 2^(s-127); the code is the nearest value, ties going to the even code, what is above 6 to 6, and a zero
+ * keeps its sign.  A group that holds an infinity or a NaN gets s = 255 and reads back as NaN (here inputs
+ * need not be finite).  s = 253 and 254, which these calls never write, may stand for infinities.
+ */
+#define VITCOP_MX4_GROUP 32
+
+/* Rows of bf16 to 4 bits, and back: x, y [M,K] bf16, rows x_row_stride / y_row_stride elements apart
+ * (multiples of 8, >= K); codes [M,K/2], scales [M,K/32] uint8 dense.  K % 32 == 0; M*K < 2^33. */
+int vitcop_mx4_quantize(const uint16_t* x, int64_t x_row_stride, int M, int K, uint8_t* codes, uint8_t* scales,
+                        void* stream);
+int vitcop_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int M, int K, uint16_t* y,
+                          int64_t y_row_stride, void* stream);
+
+/* One layer's KV cache in 4 bits: `capacity` rows per sample and KV head, HEAD-major (an attention reads one
+ * head's rows one after the other): codes [B,Hkv,capacity,d/2], scales [B,Hkv,capacity,d/32], uint8, dense.
+ * d in {64,128}; capacity*d < 2^31; B, Hkv <= 65535.  The descriptor itself is host memory read during the call. */
+typedef struct {
+    int B, capacity, Hkv, d;
+    uint8_t* k_codes;
+    uint8_t* k_scales;
+    uint8_t* v_codes;
+    uint8_t* v_scales;
+} vitcop_cache_mx4_t;
+
+/* T rows per sample into the cache: row t of sample b goes to row start + t, or start_samples[b] + t.
+ *   k, v [B,T,Hkv,d] bf16, a token's heads side by side, tokens row_stride and samples batch_stride elements
+ *        apart (multiples of 8, >= 0: K and V may sit inside fused QKV rows); one of them may be NULL, and its
+ *        side of the cache too
+ *   start_samples, n_samples: int32 [B] DEVICE, may be NULL.  With n_samples only the first n_samples[b]
+ *        (clamped to [0,T]) rows of sample b are written: a right-padded batch.
+ * All other rows of the cache stay as they were.  start + T <= capacity is checked; of start_samples, rows
+ * outside [0,capacity) are skipped on the device.  A decoding step appends with T = 1.
+ * B*Hkv*(T/32+1) < 2^26, here and when reading. */
+int vitcop_cache_mx4_write(const vitcop_cache_mx4_t* C, const uint16_t* k, const uint16_t* v, int64_t row_stride,
+                           int64_t batch_stride, int T, int start, const int32_t* start_samples,
+                           const int32_t* n_samples, void* stream);
+
+/* T rows per sample back: k, v [B,T,Hkv,d] bf16 dense (one may be NULL, and its side of the cache too), from
+ * row start or start_samples[b] on.  Rows outside the cache (start_samples) are zeros. */
+int vitcop_cache_mx4_read(const vitcop_cache_mx4_t* C, uint16_t* k, uint16_t* v, int T, int start,
+                          const int32_t* start_samples, void* stream);
+
+/* vitcop_decode_attn over such a cache: the new token of sample b attends over the cache's first N rows, or
+ * over its first n_samples[b] (int32 [B] DEVICE, may be NULL; clamped to [0,N]).  A sample without rows gets
+ * zeros and an lse of -inf; rows from n_samples[b] on are not looked at, whatever they hold.
+ *   q [B,Hq,d] bf16;  out [B,Hq,d] bf16;  lse_out [B,Hq] fp32, may be NULL;  scale 0 selects 1/sqrt(d)
+ * Hq % Hkv == 0; 0 <= N <= capacity; B*Hq < 2^24; B, Hkv, d are the descriptor's. */
+size_t vitcop_decode_attn_mx4_workspace_bytes(int B, int N, int Hq, int Hkv, int d);
+int vitcop_decode_attn_mx4(const uint16_t* q, const vitcop_cache_mx4_t* C, uint16_t* out, float* lse_out, int N,
+                           const int32_t* n_samples, int Hq, float scale, void* ws, size_t ws_bytes, void* stream);
+
+/* vitcop_project with a matrix in 4 bits: y[m,n] = bf16( sum_k x[m,k] * w[n,k] (+ residual[m,n]) ), fp32
+ * accumulate, for the few rows of a decoding step.
+ *   x [M,K] bf16, w_codes [N,K/2], w_scales [N,K/32] (vitcop_mx4_quantize of w [N,K]), y [M,N] bf16;
+ *   residual: NULL, or [M,N] bf16; row strides in elements, multiples of 8
+ *   ws: NULL, or device scratch of ws_bytes >= vitcop_project_mx4_workspace_bytes(M,N,K) (16-byte aligned)
+ * K % 32 == 0, N % 16 == 0, M <= 2^20, M*x_row_stride < 2^30, N*K < 2^31. */
+size_t vitcop_project_mx4_workspace_bytes(int M, int N, int K);
+int vitcop_project_mx4(const uint16_t* x, int64_t x_row_stride, const uint8_t* w_codes, const uint8_t* w_scales,
+                       uint16_t* y, int64_t y_row_stride, const uint16_t* residual, int64_t res_row_stride,
+                       int M, int N, int K, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

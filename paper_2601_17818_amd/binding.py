@@ -43,6 +43,9 @@ EXPORTS = (
     "vitcop_full_schedule_workspace_bytes", "vitcop_full_schedule_prefill",
     "vitcop_decoder_decode_workspace_bytes", "vitcop_decoder_decode_step",
     "vitcop_filter_visual_static",
+    "vitcop_mx4_quantize", "vitcop_mx4_dequantize", "vitcop_cache_mx4_write", "vitcop_cache_mx4_read",
+    "vitcop_decode_attn_mx4_workspace_bytes", "vitcop_decode_attn_mx4",
+    "vitcop_project_mx4_workspace_bytes", "vitcop_project_mx4",
 )
 
 
@@ -109,6 +112,11 @@ class FullScheduleT(C.Structure):
                 ("T_final", C.POINTER(C.c_int)), ("n_stage2", C.POINTER(C.c_int)),
                 ("labels", C.c_void_p), ("norms", C.c_void_p), ("out_index", C.c_void_p),
                 ("T_final_samples", C.POINTER(C.c_int)), ("cache_len_samples", C.POINTER(C.c_int))]
+
+
+class CacheMx4T(C.Structure):
+    _fields_ = ([(n, C.c_int) for n in ("B", "capacity", "Hkv", "d")] +
+                [(n, C.c_void_p) for n in ("k_codes", "k_scales", "v_codes", "v_scales")])
 
 
 class ScheduleT(C.Structure):
@@ -200,6 +208,22 @@ def _load() -> C.CDLL:
     lib.vitcop_decoder_decode_workspace_bytes.argtypes = [C.POINTER(DecoderDecodeT)]
     lib.vitcop_decoder_decode_step.restype = i32
     lib.vitcop_decoder_decode_step.argtypes = [C.POINTER(DecoderDecodeT), vp, sz, vp]
+    lib.vitcop_mx4_quantize.restype = i32
+    lib.vitcop_mx4_quantize.argtypes = [vp, i64, i32, i32, vp, vp, vp]
+    lib.vitcop_mx4_dequantize.restype = i32
+    lib.vitcop_mx4_dequantize.argtypes = [vp, vp, i32, i32, vp, i64, vp]
+    lib.vitcop_cache_mx4_write.restype = i32
+    lib.vitcop_cache_mx4_write.argtypes = [C.POINTER(CacheMx4T), vp, vp, i64, i64, i32, i32, vp, vp, vp]
+    lib.vitcop_cache_mx4_read.restype = i32
+    lib.vitcop_cache_mx4_read.argtypes = [C.POINTER(CacheMx4T), vp, vp, i32, i32, vp, vp]
+    lib.vitcop_decode_attn_mx4_workspace_bytes.restype = sz
+    lib.vitcop_decode_attn_mx4_workspace_bytes.argtypes = [i32] * 5
+    lib.vitcop_decode_attn_mx4.restype = i32
+    lib.vitcop_decode_attn_mx4.argtypes = [vp, C.POINTER(CacheMx4T), vp, vp, i32, vp, i32, f32, vp, sz, vp]
+    lib.vitcop_project_mx4_workspace_bytes.restype = sz
+    lib.vitcop_project_mx4_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.vitcop_project_mx4.restype = i32
+    lib.vitcop_project_mx4.argtypes = [vp, i64, vp, vp, vp, i64, vp, i64, i32, i32, i32, vp, sz, vp]
     return lib
 
 
@@ -754,3 +778,195 @@ def vitcop_schedule_prefill(x, weights, Hq, Hkv, d, vis_start, n_vis, schedule):
     plan = SchedulePlan(x, weights, Hq, Hkv, d, vis_start, n_vis, schedule)
     plan.run()
     return plan.y, plan.positions
+
+
+# ----------------------------------------------------------------- a KV cache and weights in 4 bits
+
+MX4_GROUP = 32
+
+
+def _expect(t, name: str, shape, dtype, device) -> None:
+    """A contiguous tensor of this shape and type on this device (dtype None: any 16-bit type)."""
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {tuple(shape)}, not {tuple(t.shape)}")
+    if t.dtype != dtype if dtype is not None else t.element_size() != 2:
+        raise ValueError(f"{name} must be {dtype if dtype is not None else 'a 16-bit (bf16) tensor'}, not {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _here(t, name: str) -> torch.device:
+    """The tensor's device, which has to be the current one: that is whose stream the call goes to."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is {torch.cuda.current_device()}")
+    return t.device
+
+
+def _rows_of(t, name: str):
+    """(M, K, row stride) of a 16-bit matrix whose rows are contiguous."""
+    if t.dim() != 2 or t.element_size() != 2:
+        raise ValueError(f"{name} must be a 16-bit (bf16) matrix")
+    M, K = t.shape
+    if K > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return M, K, t.stride(0) if M > 1 else K
+
+
+def vitcop_mx4_quantize(x, out=None):
+    """x [M,K] bf16 (rows may be strided) -> (codes [M,K/2], scales [M,K/32]) uint8, groups of 32 along K."""
+    dev = _here(x, "x")
+    M, K, stride = _rows_of(x, "x")
+    if out is None:
+        out = (torch.empty((M, K // 2), dtype=torch.uint8, device=dev),
+               torch.empty((M, K // MX4_GROUP), dtype=torch.uint8, device=dev))
+    codes, scales = out
+    _expect(codes, "codes", (M, K // 2), torch.uint8, dev)
+    _expect(scales, "scales", (M, K // MX4_GROUP), torch.uint8, dev)
+    _check(lib.vitcop_mx4_quantize(_ptr(x), stride, M, K, _ptr(codes), _ptr(scales), _stream()))
+    return codes, scales
+
+
+def vitcop_mx4_dequantize(codes, scales, out=None):
+    """(codes [M,K/2], scales [M,K/32]) uint8 -> [M,K] bf16 (exact)."""
+    dev = _here(codes, "codes")
+    M, K = codes.shape[0], codes.shape[1] * 2
+    _expect(codes, "codes", (M, K // 2), torch.uint8, dev)
+    _expect(scales, "scales", (M, K // MX4_GROUP), torch.uint8, dev)
+    if out is None:
+        out = torch.empty((M, K), dtype=torch.bfloat16, device=dev)
+    if out.device != dev or tuple(out.shape) != (M, K):
+        raise ValueError(f"out must be {(M, K)} on {dev}")
+    _check(lib.vitcop_mx4_dequantize(_ptr(codes), _ptr(scales), M, K, _ptr(out), _rows_of(out, "out")[2], _stream()))
+    return out
+
+
+class CacheMx4:
+    """One layer's KV cache in 4 bits: k_codes, v_codes [B,Hkv,capacity,d/2] and k_scales, v_scales [B,Hkv,capacity,d/32],
+    uint8, contiguous.  ``CacheMx4.empty`` allocates one (rows that nothing has been written to hold anything)."""
+
+    def __init__(self, k_codes, k_scales, v_codes, v_scales):
+        self.device = _here(k_codes, "k_codes")
+        if k_codes.dim() != 4:
+            raise ValueError("k_codes must be [B,Hkv,capacity,d/2]")
+        B, Hkv, capacity, half = k_codes.shape
+        for t, name, width in ((k_codes, "k_codes", half), (k_scales, "k_scales", half * 2 // MX4_GROUP),
+                               (v_codes, "v_codes", half), (v_scales, "v_scales", half * 2 // MX4_GROUP)):
+            _expect(t, name, (B, Hkv, capacity, width), torch.uint8, self.device)
+        self.B, self.Hkv, self.capacity, self.d = B, Hkv, capacity, half * 2
+        self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
+        self.desc = CacheMx4T(B, capacity, Hkv, half * 2, _ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales))
+
+    @classmethod
+    def empty(cls, B: int, capacity: int, Hkv: int, d: int, device="cuda"):
+        widths = (d // 2, d // MX4_GROUP, d // 2, d // MX4_GROUP)
+        return cls(*[torch.empty((B, Hkv, capacity, w), dtype=torch.uint8, device=device) for w in widths])
+
+    def per_sample(self, t, name: str):
+        if t is not None:
+            _expect(t, name, (self.B,), torch.int32, self.device)
+        return _ptr(t)
+
+
+def vitcop_cache_mx4_write(cache: CacheMx4, k, v, start: int = 0, start_samples=None, n_samples=None) -> None:
+    """Rows of k, v [B,T,Hkv,d] (either may be None) to rows start + t of the cache, or start_samples[b] + t (int32 [B]);
+    with n_samples (int32 [B]) the first n_samples[b] rows of sample b only.  A token's heads lie side by side; tokens and
+    samples may be strided (views of fused QKV rows)."""
+    sides, T = [], 0
+    for t, name in ((k, "k"), (v, "v")):
+        if t is None:
+            sides.append(None)
+            continue
+        if t.device != cache.device or t.element_size() != 2 or t.dim() != 4:
+            raise ValueError(f"{name} must be a 16-bit [B,T,Hkv,d] tensor on {cache.device}")
+        T = t.shape[1]
+        if tuple(t.shape) != (cache.B, T, cache.Hkv, cache.d):
+            raise ValueError(f"{name} must be {(cache.B, T, cache.Hkv, cache.d)}, not {tuple(t.shape)}")
+        if t.stride(3) != 1 or (cache.Hkv > 1 and t.stride(2) != cache.d):
+            raise ValueError(f"{name}: a token's heads must lie side by side")
+        row = t.stride(1) if T > 1 else cache.Hkv * cache.d
+        sides.append((row, t.stride(0) if cache.B > 1 else T * row))
+    if k is not None and v is not None and k.shape[1] != v.shape[1]:
+        raise ValueError("k and v differ in their number of rows")
+    _here(cache.k_codes, "the cache")
+    start_p, n_p = cache.per_sample(start_samples, "start_samples"), cache.per_sample(n_samples, "n_samples")
+    if sides[0] is not None and sides[1] is not None and sides[0] != sides[1]:       # strides of their own: two calls
+        vitcop_cache_mx4_write(cache, k, None, start, start_samples, n_samples)
+        vitcop_cache_mx4_write(cache, None, v, start, start_samples, n_samples)
+        return
+    row, batch = sides[0] or sides[1] or (0, 0)
+    _check(lib.vitcop_cache_mx4_write(C.byref(cache.desc), _ptr(k), _ptr(v), row, batch, T, start, start_p, n_p, _stream()))
+
+
+def vitcop_cache_mx4_read(cache: CacheMx4, T: int, start: int = 0, start_samples=None, out=None):
+    """Rows [start, start + T) of every sample, or T rows from start_samples[b] (int32 [B]) on, as (k, v) [B,T,Hkv,d]
+    bf16; ``out`` = (k, v) reuses buffers, of which one may be None."""
+    _here(cache.k_codes, "the cache")
+    shape = (cache.B, T, cache.Hkv, cache.d)
+    if out is None:
+        if T < 0:
+            raise ValueError("T must not be negative")
+        out = tuple(torch.empty(shape, dtype=torch.bfloat16, device=cache.device) for _ in range(2))
+    k, v = out
+    for t, name in ((k, "k"), (v, "v")):
+        if t is not None:
+            _expect(t, name, shape, None, cache.device)
+    _check(lib.vitcop_cache_mx4_read(C.byref(cache.desc), _ptr(k), _ptr(v), T, start,
+                                     cache.per_sample(start_samples, "start_samples"), _stream()))
+    return k, v
+
+
+def vitcop_decode_attn_mx4(q, cache: CacheMx4, N: int, n_samples=None, scale: float = 0.0, want_lse: bool = True, out=None,
+                           ws=None):
+    """q [B,Hq,d] over the first N rows of the cache, or n_samples[b] (int32 [B], at most N) of sample b's -> (out [B,Hq,d],
+    lse [B,Hq] or None).  ``out`` = (out, lse) reuses buffers, ``ws`` a uint8 workspace."""
+    dev = _here(q, "q")
+    if q.dim() != 3:
+        raise ValueError("q must be [B,Hq,d]")
+    Hq = q.shape[1]
+    _expect(q, "q", (cache.B, Hq, cache.d), None, cache.device)
+    if out is None:
+        o = torch.empty_like(q)
+        lse = torch.empty((cache.B, Hq), dtype=torch.float32, device=dev) if want_lse else None
+    else:
+        o, lse = out
+        _expect(o, "out", q.shape, None, dev)
+        if lse is not None:
+            _expect(lse, "lse", (cache.B, Hq), torch.float32, dev)
+    if ws is None:
+        ws = _ws(lib.vitcop_decode_attn_mx4_workspace_bytes(cache.B, N, Hq, cache.Hkv, cache.d), q)
+    elif ws.device != dev or ws.dtype != torch.uint8:
+        raise ValueError(f"ws must be a uint8 tensor on {dev}")
+    _check(lib.vitcop_decode_attn_mx4(_ptr(q), C.byref(cache.desc), _ptr(o), _ptr(lse), N,
+                                      cache.per_sample(n_samples, "n_samples"), Hq, scale, _ptr(ws), ws.numel(), _stream()))
+    return o, lse
+
+
+def vitcop_project_mx4(x, codes, scales, residual=None, out=None, ws=None):
+    """x [M,K] bf16 (rows may be strided), a matrix [N,K] as codes [N,K/2] and scales [N,K/32] (vitcop_mx4_quantize) ->
+    x W^T (+ residual) [M,N].  ``out`` reuses a buffer (rows may be strided), ``ws`` a uint8 workspace."""
+    dev = _here(x, "x")
+    M, K, x_stride = _rows_of(x, "x")
+    N = codes.shape[0]
+    _expect(codes, "codes", (N, K // 2), torch.uint8, dev)
+    _expect(scales, "scales", (N, K // MX4_GROUP), torch.uint8, dev)
+    if out is None:
+        out = torch.empty((M, N), dtype=x.dtype, device=dev)
+    res_stride = N
+    for t, name in ((out, "out"), (residual, "residual")):
+        if t is not None and (t.device != dev or tuple(t.shape) != (M, N)):
+            raise ValueError(f"{name} must be {(M, N)} on {dev}")
+    if residual is not None:
+        res_stride = _rows_of(residual, "residual")[2]
+    nb = lib.vitcop_project_mx4_workspace_bytes(M, N, K)
+    if ws is None:
+        ws = _ws(nb, x) if nb else None
+    elif ws.device != dev or ws.dtype != torch.uint8:
+        raise ValueError(f"ws must be a uint8 tensor on {dev}")
+    _check(lib.vitcop_project_mx4(_ptr(x), x_stride, _ptr(codes), _ptr(scales), _ptr(out), _rows_of(out, "out")[2],
+                                  _ptr(residual), res_stride, M, N, K, _ptr(ws), ws.numel() if ws is not None else 0,
+                                  _stream()))
+    return out

@@ -1313,5 +1313,148 @@ int vitcop_decoder_decode_step(const vitcop_decoder_decode_t* S, void* ws, size_
     return VITCOP_OK;
 }
 
+/* ------------------------------------------- a cache and weights in 4 bits */
+
+static int check_mx4_rows(const char* what, const void* bf16, int64_t stride, int M, int K, const uint8_t* codes,
+                          const uint8_t* scales) {
+    REQUIRE(M >= 0 && K >= 1, VITCOP_EINVAL, "%s: M=%d K=%d", what, M, K);
+    REQUIRE(K % VITCOP_MX4_GROUP == 0, VITCOP_EUNSUPPORTED, "%s: K=%d not a multiple of %d", what, K, VITCOP_MX4_GROUP);
+    REQUIRE(stride >= K && stride % 8 == 0, VITCOP_EINVAL, "%s: row stride %lld", what, (long long)stride);
+    REQUIRE((int64_t)M * K < ((int64_t)1 << 33), VITCOP_EUNSUPPORTED, "%s: M*K of 2^33 and more", what);
+    if (M == 0) return VITCOP_OK;
+    REQUIRE(bf16 && codes && scales, VITCOP_EINVAL, "%s: null pointer", what);
+    REQUIRE(aligned16(bf16) && aligned16(codes) && aligned16(scales), VITCOP_EINVAL, "%s: pointers must be 16-byte aligned", what);
+    return VITCOP_OK;
+}
+
+int vitcop_mx4_quantize(const uint16_t* x, int64_t x_row_stride, int M, int K, uint8_t* codes, uint8_t* scales,
+                        void* stream) {
+    const int rc = check_mx4_rows("mx4_quantize", x, x_row_stride, M, K, codes, scales);
+    if (rc || M == 0) return rc;
+    return launch_mx4_quantize(x, x_row_stride, M, K, codes, scales, static_cast<hipStream_t>(stream));
+}
+
+int vitcop_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int M, int K, uint16_t* y, int64_t y_row_stride,
+                          void* stream) {
+    const int rc = check_mx4_rows("mx4_dequantize", y, y_row_stride, M, K, codes, scales);
+    if (rc || M == 0) return rc;
+    return launch_mx4_dequantize(codes, scales, M, K, y, y_row_stride, static_cast<hipStream_t>(stream));
+}
+
+static int check_cache_mx4(const char* what, const vitcop_cache_mx4_t* C, bool need_k, bool need_v) {
+    REQUIRE(C, VITCOP_EINVAL, "%s: descriptor is null", what);
+    REQUIRE(C->B >= 0 && C->capacity >= 0 && C->Hkv >= 1, VITCOP_EINVAL, "%s: B=%d capacity=%d Hkv=%d", what, C->B,
+            C->capacity, C->Hkv);
+    REQUIRE(C->d == 64 || C->d == 128, VITCOP_EUNSUPPORTED, "%s: d=%d (64 or 128)", what, C->d);
+    REQUIRE(C->B <= 65535 && C->Hkv <= 65535, VITCOP_EUNSUPPORTED, "%s: Hkv or B above 65535", what);
+    REQUIRE((int64_t)C->capacity * C->d < ((int64_t)1 << 31), VITCOP_EUNSUPPORTED,
+            "%s: one head's rows must stay below 2^31 values", what);
+    if (C->B == 0 || C->capacity == 0) return VITCOP_OK;
+    REQUIRE((!need_k || (C->k_codes && C->k_scales)) && (!need_v || (C->v_codes && C->v_scales)), VITCOP_EINVAL,
+            "%s: the cache has a null pointer", what);
+    REQUIRE(aligned16(C->k_codes) && aligned16(C->k_scales) && aligned16(C->v_codes) && aligned16(C->v_scales), VITCOP_EINVAL,
+            "%s: the cache's pointers must be 16-byte aligned", what);
+    return VITCOP_OK;
+}
+
+static int check_cache_mx4_rows(const char* what, const vitcop_cache_mx4_t* C, const void* k, const void* v, int T,
+                                int start, const int32_t* start_samples) {
+    const int rc = check_cache_mx4(what, C, k != nullptr, v != nullptr);
+    if (rc) return rc;
+    REQUIRE(T >= 0, VITCOP_EINVAL, "%s: T=%d", what, T);
+    REQUIRE(start_samples || (start >= 0 && (int64_t)start + T <= C->capacity), VITCOP_EINVAL,
+            "%s: rows [%d,%lld) outside [0,%d)", what, start, (long long)start + T, C->capacity);
+    REQUIRE((int64_t)C->B * C->Hkv * (T / 32 + 1) < ((int64_t)1 << 26), VITCOP_EUNSUPPORTED, "%s: B*Hkv*(T/32+1) of 2^26 and more",
+            what);
+    if (C->B == 0 || T == 0) return VITCOP_OK;
+    REQUIRE(k || v, VITCOP_EINVAL, "%s: k and v are both null", what);
+    REQUIRE(aligned16(k) && aligned16(v), VITCOP_EINVAL, "%s: k and v must be 16-byte aligned", what);
+    return VITCOP_OK;
+}
+
+int vitcop_cache_mx4_write(const vitcop_cache_mx4_t* C, const uint16_t* k, const uint16_t* v, int64_t row_stride,
+                           int64_t batch_stride, int T, int start, const int32_t* start_samples,
+                           const int32_t* n_samples, void* stream) {
+    const int rc = check_cache_mx4_rows("cache_mx4_write", C, k, v, T, start, start_samples);
+    if (rc) return rc;
+    REQUIRE(row_stride >= 0 && batch_stride >= 0 && row_stride % 8 == 0 && batch_stride % 8 == 0, VITCOP_EINVAL,
+            "cache_mx4_write: strides (%lld, %lld)", (long long)row_stride, (long long)batch_stride);
+    if (C->B == 0 || T == 0 || C->capacity == 0) return VITCOP_OK;
+    return launch_cache_mx4_write(*C, k, v, row_stride, batch_stride, T, start, start_samples, n_samples,
+                                  static_cast<hipStream_t>(stream));
+}
+
+int vitcop_cache_mx4_read(const vitcop_cache_mx4_t* C, uint16_t* k, uint16_t* v, int T, int start,
+                          const int32_t* start_samples, void* stream) {
+    const int rc = check_cache_mx4_rows("cache_mx4_read", C, k, v, T, start, start_samples);
+    if (rc || C->B == 0 || T == 0) return rc;
+    return launch_cache_mx4_read(*C, k, v, T, start, start_samples, static_cast<hipStream_t>(stream));
+}
+
+static int check_decode_mx4(int B, int N, int Hq, int Hkv, int d) {
+    REQUIRE(B >= 0 && N >= 0 && Hq >= 1 && Hkv >= 1, VITCOP_EINVAL, "decode_attn_mx4: B=%d N=%d Hq=%d Hkv=%d", B, N, Hq, Hkv);
+    REQUIRE(Hq % Hkv == 0, VITCOP_EINVAL, "decode_attn_mx4: Hq=%d not a multiple of Hkv=%d", Hq, Hkv);
+    REQUIRE(d == 64 || d == 128, VITCOP_EUNSUPPORTED, "decode_attn_mx4: d=%d (64 or 128)", d);
+    REQUIRE(Hkv <= 65535 && B <= 65535, VITCOP_EUNSUPPORTED, "decode_attn_mx4: Hkv or B above 65535");
+    REQUIRE((int64_t)B * Hq < ((int64_t)1 << 24), VITCOP_EUNSUPPORTED, "decode_attn_mx4: B*Hq of 2^24 and more");
+    REQUIRE((int64_t)N * d < ((int64_t)1 << 31), VITCOP_EUNSUPPORTED,
+            "decode_attn_mx4: one head's rows must stay below 2^31 values");
+    return VITCOP_OK;
+}
+
+size_t vitcop_decode_attn_mx4_workspace_bytes(int B, int N, int Hq, int Hkv, int d) {
+    if (check_decode_mx4(B, N, Hq, Hkv, d) != VITCOP_OK || B == 0) return 0;
+    return decode_mx4_workspace_bytes(B, N, Hq, Hkv, d);
+}
+
+int vitcop_decode_attn_mx4(const uint16_t* q, const vitcop_cache_mx4_t* C, uint16_t* out, float* lse_out, int N,
+                           const int32_t* n_samples, int Hq, float scale, void* ws, size_t ws_bytes, void* stream) {
+    int rc = check_cache_mx4("decode_attn_mx4", C, N > 0, N > 0);
+    if (rc) return rc;
+    rc = check_decode_mx4(C->B, N, Hq, C->Hkv, C->d);
+    if (rc) return rc;
+    REQUIRE(N <= C->capacity, VITCOP_EINVAL, "decode_attn_mx4: N=%d above the capacity %d", N, C->capacity);
+    REQUIRE(std::isfinite(scale) && scale >= 0.f, VITCOP_EINVAL, "decode_attn_mx4: scale");
+    if (C->B == 0) return VITCOP_OK;
+    REQUIRE(q && out, VITCOP_EINVAL, "decode_attn_mx4: null pointer");
+    REQUIRE(aligned16(q) && aligned16(out) && aligned16(ws), VITCOP_EINVAL, "decode_attn_mx4: pointers must be 16-byte aligned");
+    const size_t need = decode_mx4_workspace_bytes(C->B, N, Hq, C->Hkv, C->d);
+    REQUIRE(ws && ws_bytes >= need, VITCOP_EWORKSPACE, "decode_attn_mx4: workspace %zu < %zu", ws_bytes, need);
+    if (scale == 0.f) scale = 1.0f / std::sqrt((float)C->d);
+    return launch_decode_attn_mx4(q, *C, out, lse_out, N, n_samples, Hq, scale, ws, static_cast<hipStream_t>(stream));
+}
+
+static int check_project_mx4(int M, int N, int K) {
+    REQUIRE(M >= 0 && N >= 0 && K >= 1, VITCOP_EINVAL, "project_mx4: M=%d N=%d K=%d", M, N, K);
+    REQUIRE(K % VITCOP_MX4_GROUP == 0 && N % 16 == 0, VITCOP_EUNSUPPORTED, "project_mx4: K=%d %% %d, N=%d %% 16", K,
+            VITCOP_MX4_GROUP, N);
+    REQUIRE((int64_t)N * K < ((int64_t)1 << 31), VITCOP_EUNSUPPORTED, "project_mx4: matrix of 2^31 values and more");
+    REQUIRE(M <= (1 << 20), VITCOP_EUNSUPPORTED, "project_mx4: M=%d above 2^20", M);
+    return VITCOP_OK;
+}
+
+size_t vitcop_project_mx4_workspace_bytes(int M, int N, int K) {
+    if (check_project_mx4(M, N, K) != VITCOP_OK) return 0;
+    return project_mx4_workspace_bytes(M, N, K);
+}
+
+int vitcop_project_mx4(const uint16_t* x, int64_t x_row_stride, const uint8_t* w_codes, const uint8_t* w_scales,
+                       uint16_t* y, int64_t y_row_stride, const uint16_t* residual, int64_t res_row_stride, int M, int N,
+                       int K, void* ws, size_t ws_bytes, void* stream) {
+    const int rc = check_project_mx4(M, N, K);
+    if (rc) return rc;
+    REQUIRE(x_row_stride >= K && x_row_stride % 8 == 0 && y_row_stride >= N && y_row_stride % 8 == 0, VITCOP_EINVAL,
+            "project_mx4: strides (%lld, %lld)", (long long)x_row_stride, (long long)y_row_stride);
+    REQUIRE(!residual || (res_row_stride >= N && res_row_stride % 8 == 0), VITCOP_EINVAL, "project_mx4: residual stride %lld",
+            (long long)res_row_stride);
+    REQUIRE((int64_t)M * x_row_stride < ((int64_t)1 << 30), VITCOP_EUNSUPPORTED, "project_mx4: x of 2^30 elements and more");
+    if (M == 0 || N == 0) return VITCOP_OK;
+    REQUIRE(x && w_codes && w_scales && y, VITCOP_EINVAL, "project_mx4: null pointer");
+    REQUIRE(aligned16(x) && aligned16(w_codes) && aligned16(w_scales) && aligned16(y) && aligned16(residual) && aligned16(ws),
+            VITCOP_EINVAL, "project_mx4: pointers must be 16-byte aligned");
+    return launch_project_mx4(x, x_row_stride, w_codes, w_scales, y, y_row_stride, residual, res_row_stride, M, N, K, ws,
+                              ws ? ws_bytes : 0, static_cast<hipStream_t>(stream));
+}
+
 #pragma GCC visibility pop
 }  // extern "C"

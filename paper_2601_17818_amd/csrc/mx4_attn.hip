@@ -1,0 +1,257 @@
+// One decoding step over a KV cache held in 4 bits (format: mx4_device.h): o = softmax(scale K q) V for the new token of
+// every sample.  Bound by the cache's bytes, 17/32 of one a value, each read once for every 16 query heads of a KV head.
+//
+// A workgroup takes one KV head of a sample and one slice of the keys, a wavefront 32 keys at a time: scores S^T = K Q^T
+// (16x16x32: a lane holds 4 keys of one head), the softmax with the lane's head as its only query, O^T += V^T P^T.  The
+// products are on the matrix cores also where a KV head has a single query head and 15 of 16 columns are idle: on the vector
+// pipe a key's 2 d values would cost an FMA each and, before it, half a conversion; here the conversions alone remain.
+//  - K goes from the conversion straight into the product: a lane's 16 (8) bytes of a row are 32 (16) neighbouring
+//    channels, and the order of the channels in a sum is free as long as q is read in the same one.
+//  - V has to be turned (a product's operand holds one channel of several keys): its bf16 rows go through LDS and come back
+//    transposed (ds_read_b64_tr_b16).  The key of element 4 t + r of a lane's 8 is 16 t + 4 (lane / 16) + r, which is where
+//    the scores are.
+//  - A probability is the sum of two bf16 (16 bits, off by at most 2^-16 of itself), one product for each: one alone would add an
+//    error as large as the rounding of the output.
+//  - The running reference of the softmax moves only when a score exceeds it by 2^8, which is rare after the first tiles; until
+//    then no lane needs to know another's scores.  Sums, references and outputs are fp32.
+// mx4_merge_kernel combines the slices; a single slice is finished on the spot.
+#include "vitcop_internal.h"
+#include "mx4_device.h"
+
+#include <algorithm>
+
+namespace vitcop {
+
+constexpr int MA_MAX_G = 16, MA_KEYS = 32;
+constexpr float MA_SLACK = 8.f;              // log2
+
+// what a head without any key gives: zeros, and minus infinity as the logarithm of its sum
+__device__ __forceinline__ float mx4_quotient(float o, float l) { return l == 0.f ? 0.f : o / l; }
+__device__ __forceinline__ float mx4_lse(float m, float l) {
+    return l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
+template <int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, D == 128 ? 3 : 4) void mx4_attn_kernel(
+    const uint16_t* __restrict__ q, const uint8_t* __restrict__ k_codes, const uint8_t* __restrict__ k_scales,
+    const uint8_t* __restrict__ v_codes, const uint8_t* __restrict__ v_scales, float* __restrict__ part_o,
+    float* __restrict__ part_ml, int capacity, int N, int Hq, int Hkv, int g0, int G, float scale_log2e, int keys_per_split,
+    int n_splits, const int32_t* __restrict__ n_samples, uint16_t* __restrict__ out, float* __restrict__ lse) {
+    constexpr int STEPS = D / 32, BLOCKS = D / 16;
+    constexpr int ROW = D / 2, GROUPS = D / MX4_GROUP;               // bytes of a row of codes, of exponents
+    constexpr int VROW = 2 * D + 32;                                 // bytes of a V row in LDS: the pad keeps eight rows apart
+    constexpr int LPR = ROW / 16, RPL = 64 / LPR, VL = MA_KEYS / RPL;         // V: lanes a row, rows a load, loads a tile
+    static_assert(MA_KEYS * VROW >= MA_MAX_G * D * 4, "the outputs take V's place at the end");
+    __shared__ __attribute__((aligned(16))) char vt[WAVES][MA_KEYS * VROW];
+    __shared__ float sm[WAVES][MA_MAX_G][2];
+    float (&so)[WAVES][MA_MAX_G][D] = *reinterpret_cast<float (*)[WAVES][MA_MAX_G][D]>(&vt[0][0]);
+    const int split = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, l16 = lane & 15, g4 = lane >> 4;
+    const int h0 = hk * (Hq / Hkv) + g0;                     // first query head of this pass
+    const int n_keys = n_samples ? min(max(n_samples[b], 0), N) : N;
+    const int key_begin = split * keys_per_split, key_end = min(n_keys, key_begin + keys_per_split);
+
+    f32x4 o[BLOCKS];
+#pragma unroll
+    for (int i = 0; i < BLOCKS; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;                            // of head l16 (m for all its keys, l over this lane's)
+
+    // Rows past the slice's end read as zeros: the descriptors end there.
+    const int64_t head_row = ((int64_t)b * Hkv + hk) * capacity;
+    const unsigned rows = (unsigned)max(key_end, 0);
+    const auto kc_desc = __builtin_amdgcn_make_buffer_rsrc((void*)(k_codes + head_row * ROW), 0, rows * ROW, 0x00020000);
+    const auto ks_desc = __builtin_amdgcn_make_buffer_rsrc((void*)(k_scales + head_row * GROUPS), 0, rows * GROUPS, 0x00020000);
+    const auto vc_desc = __builtin_amdgcn_make_buffer_rsrc((void*)(v_codes + head_row * ROW), 0, rows * ROW, 0x00020000);
+    const auto vs_desc = __builtin_amdgcn_make_buffer_rsrc((void*)(v_scales + head_row * GROUPS), 0, rows * GROUPS, 0x00020000);
+    constexpr int NT = 2;                                    // non-temporal
+    typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
+    u32x4 kr[2], vr[VL];                                     // (d = 64: two dwords of K)
+    uint32_t ke[2], ve[VL];
+    auto load = [&](int key0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const unsigned row = (unsigned)(key0 + 16 * t + l16);
+            if constexpr (D == 128) {
+                kr[t] = __builtin_amdgcn_raw_buffer_load_b128(kc_desc, row * ROW + 16 * g4, 0, NT);
+            } else {
+                const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(kc_desc, row * ROW + 8 * g4, 0, NT);
+                kr[t] = u32x4{w.x, w.y, 0u, 0u};
+            }
+            ke[t] = __builtin_amdgcn_raw_buffer_load_b8(ks_desc, row * GROUPS + g4 * GROUPS / 4, 0, NT);
+        }
+#pragma unroll
+        for (int i = 0; i < VL; ++i) {
+            const unsigned row = (unsigned)(key0 + RPL * i + lane / LPR);
+            vr[i] = __builtin_amdgcn_raw_buffer_load_b128(vc_desc, row * ROW + 16 * (lane % LPR), 0, NT);
+            ve[i] = __builtin_amdgcn_raw_buffer_load_b8(vs_desc, row * GROUPS + lane % LPR, 0, NT);
+        }
+    };
+    const int first = key_begin + wv * MA_KEYS;
+    if (first < key_end) load(first);
+    bf16x8 qf[STEPS];                                        // Q^T of head l16 (heads past G: head G - 1), channels as K's
+#pragma unroll
+    for (int c = 0; c < STEPS; ++c)
+        qf[c] = *reinterpret_cast<const bf16x8*>(q + ((int64_t)b * Hq + h0 + min(l16, G - 1)) * D + D / 4 * g4 + 8 * c);
+    typedef __attribute__((ext_vector_type(4))) short s16x4;
+    typedef __attribute__((ext_vector_type(8))) short s16x8;
+    char* const mine = vt[wv];
+    const unsigned tr = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)mine +
+                        (4 * g4 + ((lane >> 2) & 3)) * VROW + (lane & 3) * 8;
+    for (int key0 = first; key0 < key_end; key0 += WAVES * MA_KEYS) {
+        f32x4 s[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            const float e = mx4_scale(ke[t]);
+#pragma unroll
+            for (int c = 0; c < STEPS; ++c)
+                s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, mx4_values(kr[t][c], e)), qf[c], s[t],
+                                                               0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < VL; ++i) {
+            const float e = mx4_scale(ve[i]);
+            u32x4* const row = reinterpret_cast<u32x4*>(mine + (RPL * i + lane / LPR) * VROW + lane % LPR * 64);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) row[c] = mx4_values(vr[i][c], e);
+        }
+        if (key0 + WAVES * MA_KEYS < key_end) load(key0 + WAVES * MA_KEYS);      // (uniform) in flight from here on
+        float p[8], top = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int key = key0 + 16 * (e >> 2) + 4 * g4 + (e & 3);
+            p[e] = key < key_end ? s[e >> 2][e & 3] * scale_log2e : -INFINITY;
+            top = fmaxf(top, p[e]);
+        }
+        if (__builtin_amdgcn_ballot_w64(top > m + MA_SLACK) != 0) {
+            top = fmaxf(top, __shfl_xor(top, 16, 64));
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            const float m_new = fmaxf(m, top);
+            const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+            m = m_new;
+            l *= alpha;
+#pragma unroll
+            for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[i][r] *= alpha;
+        }
+        const float base = m == -INFINITY ? 0.f : m;         // (nothing but -inf so far: 0, not NaN)
+        u32x4 part[2];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float a = __builtin_amdgcn_exp2f(p[2 * e] - base), c = __builtin_amdgcn_exp2f(p[2 * e + 1] - base);
+            l += a;
+            l += c;
+            const uint32_t w = pack_bf16(a, c);
+            part[0][e] = w;
+            part[1][e] = pack_bf16(a - bf16_lo(w), c - bf16_hi(w));
+        }
+        __builtin_amdgcn_wave_barrier();                     // (one wavefront's LDS accesses stay in order)
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) {
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) s16x4*)(uintptr_t)(tr + i * 32));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) s16x4*)(uintptr_t)(tr + i * 32 + 16 * VROW));
+            const bf16x8 vf = __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+                o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, part[n]), o[i], 0, 0, 0);
+        }
+        __builtin_amdgcn_wave_barrier();                     // the next tile's rows replace these
+    }
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    __syncthreads();                                         // all are done with V
+    if (g4 == 0) {
+        sm[wv][l16][0] = m;
+        sm[wv][l16][1] = l;
+    }
+#pragma unroll
+    for (int i = 0; i < BLOCKS; ++i) *reinterpret_cast<f32x4*>(&so[wv][l16][16 * i + 4 * g4]) = o[i];
+    __syncthreads();
+    // the wavefronts' states combined by threads (head, channel): this slice's partial, or with `out` the output
+    for (int idx = threadIdx.x; idx < G * D; idx += 64 * WAVES) {
+        const int g = idx / D, ch = idx - g * D;
+        float mn = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) mn = fmaxf(mn, sm[w][g][0]);
+        float lt = 0.f, ot = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float a = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(sm[w][g][0] - mn);
+            lt += sm[w][g][1] * a;
+            ot += so[w][g][ch] * a;
+        }
+        if (out != nullptr) {
+            const int64_t bh = (int64_t)b * Hq + h0 + g;
+            const float r = mx4_quotient(ot, lt), r1 = __shfl_down(r, 1, 64);        // (a wavefront's lanes share g: D >= 64)
+            if ((ch & 1) == 0) *reinterpret_cast<uint32_t*>(out + bh * D + ch) = pack_bf16(r, r1);
+            if (lse && ch == 0) lse[bh] = mx4_lse(mn, lt);
+            continue;
+        }
+        const int64_t slot = ((int64_t)b * Hq + h0 + g) * n_splits + split;
+        part_o[slot * D + ch] = ot;
+        if (ch == 0) {
+            part_ml[slot * 2] = mn;
+            part_ml[slot * 2 + 1] = lt;
+        }
+    }
+}
+
+template <int D>
+__global__ __launch_bounds__(D) void mx4_merge_kernel(const float* __restrict__ part_o, const float* __restrict__ part_ml,
+                                                      int n_splits, uint16_t* __restrict__ out, float* __restrict__ lse) {
+    const int64_t bh = blockIdx.x;
+    const int ch = threadIdx.x;
+    float mn = -INFINITY;
+    for (int s = 0; s < n_splits; ++s) mn = fmaxf(mn, part_ml[(bh * n_splits + s) * 2]);
+    float lt = 0.f, ot = 0.f;
+    for (int s = 0; s < n_splits; ++s) {
+        const float a = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(part_ml[(bh * n_splits + s) * 2] - mn);
+        lt += part_ml[(bh * n_splits + s) * 2 + 1] * a;
+        ot += part_o[(bh * n_splits + s) * D + ch] * a;
+    }
+    const float r = mx4_quotient(ot, lt), r1 = __shfl_down(r, 1, 64);        // neighbouring channels: one 32-bit store
+    if ((ch & 1) == 0) *reinterpret_cast<uint32_t*>(out + bh * D + ch) = pack_bf16(r, r1);
+    if (lse && ch == 0) lse[bh] = mx4_lse(mn, lt);
+}
+
+// Slices of the keys: workgroups for every CU, of at least 128 keys each.
+static int attn_splits(int B, int N, int Hkv) {
+    const long pairs = (long)B * Hkv;
+    return (int)std::max(1L, std::min((512 + pairs - 1) / pairs, (N + 127L) / 128));
+}
+
+size_t decode_mx4_workspace_bytes(int B, int N, int Hq, int Hkv, int d) {
+    const size_t s = attn_splits(B, N, Hkv);
+    return up256((size_t)B * Hq * s * d * 4) + up256((size_t)B * Hq * s * 2 * 4);
+}
+
+template <int D>
+static int launch_attn_d(const uint16_t* q, const vitcop_cache_mx4_t& C, uint16_t* out, float* lse, int N,
+                         const int32_t* n_samples, int Hq, float scale, void* ws, hipStream_t s) {
+    constexpr int WAVES = 4;
+    const int B = C.B, group = Hq / C.Hkv, ns = attn_splits(B, N, C.Hkv);
+    const int kps = ((N + ns - 1) / ns + 127) / 128 * 128;
+    float* po = static_cast<float*>(ws);
+    float* pml = reinterpret_cast<float*>(static_cast<char*>(ws) + up256((size_t)B * Hq * ns * D * 4));
+    for (int g0 = 0; g0 < group; g0 += MA_MAX_G) {
+        hipLaunchKernelGGL((mx4_attn_kernel<D, WAVES>), dim3(ns, C.Hkv, B), dim3(64 * WAVES), 0, s, q, C.k_codes, C.k_scales,
+                           C.v_codes, C.v_scales, po, pml, C.capacity, N, Hq, C.Hkv, g0, std::min(MA_MAX_G, group - g0),
+                           scale * 1.4426950408889634f, kps, ns, n_samples, ns == 1 ? out : nullptr, lse);
+        const int rc = launch_status("mx4_attn");
+        if (rc) return rc;
+    }
+    if (ns == 1) return VITCOP_OK;
+    hipLaunchKernelGGL((mx4_merge_kernel<D>), dim3((unsigned)(B * Hq)), dim3(D), 0, s, po, pml, ns, out, lse);
+    return launch_status("mx4_merge");
+}
+
+int launch_decode_attn_mx4(const uint16_t* q, const vitcop_cache_mx4_t& C, uint16_t* out, float* lse, int N,
+                           const int32_t* n_samples, int Hq, float scale, void* ws, hipStream_t s) {
+    return C.d == 64 ? launch_attn_d<64>(q, C, out, lse, N, n_samples, Hq, scale, ws, s)
+                     : launch_attn_d<128>(q, C, out, lse, N, n_samples, Hq, scale, ws, s);
+}
+
+}  // namespace vitcop

@@ -234,4 +234,21 @@ int launch_decode_attn(const uint16_t* q, const uint16_t* k, const uint16_t* v, 
                        DecodeParts* hand_over = nullptr, const int32_t* n_cached_samples = nullptr,
                        const DecodeNew* fresh = nullptr);
 
+// ---- rows, a KV cache and weights in 4 bits (mx4.hip, mx4_attn.hip, mx4_project.hip) ------------------------
+int launch_mx4_quantize(const uint16_t* x, int64_t x_stride, int M, int K, uint8_t* codes, uint8_t* scales, hipStream_t s);
+int launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int M, int K, uint16_t* y, int64_t y_stride,
+                          hipStream_t s);
+int launch_cache_mx4_write(const vitcop_cache_mx4_t& C, const uint16_t* k, const uint16_t* v, int64_t row_stride,
+                           int64_t batch_stride, int T, int start, const int32_t* start_samples,
+                           const int32_t* n_samples, hipStream_t s);
+int launch_cache_mx4_read(const vitcop_cache_mx4_t& C, uint16_t* k, uint16_t* v, int T, int start,
+                          const int32_t* start_samples, hipStream_t s);
+size_t decode_mx4_workspace_bytes(int B, int N, int Hq, int Hkv, int d);
+int launch_decode_attn_mx4(const uint16_t* q, const vitcop_cache_mx4_t& C, uint16_t* out, float* lse, int N,
+                           const int32_t* n_samples, int Hq, float scale, void* ws, hipStream_t s);
+size_t project_mx4_workspace_bytes(int M, int N, int K);
+int launch_project_mx4(const uint16_t* x, int64_t x_stride, const uint8_t* codes, const uint8_t* scales, uint16_t* y,
+                       int64_t y_stride, const uint16_t* res, int64_t res_stride, int M, int N, int K, void* ws,
+                       size_t ws_bytes, hipStream_t s);
+
 }  // namespace vitcop
