@@ -1429,7 +1429,7 @@ static int check_project_mx4(int M, int N, int K) {
     REQUIRE(K % VITCOP_MX4_GROUP == 0 && N % 16 == 0, VITCOP_EUNSUPPORTED, "project_mx4: K=%d %% %d, N=%d %% 16", K,
             VITCOP_MX4_GROUP, N);
     REQUIRE((int64_t)N * K < ((int64_t)1 << 31), VITCOP_EUNSUPPORTED, "project_mx4: matrix of 2^31 values and more");
-    REQUIRE(M <= (1 << 20), VITCOP_EUNSUPPORTED, "project_mx4: M=%d above 2^20", M);
+    REQUIRE(M <= (1 << 19) && K <= (1 << 16), VITCOP_EUNSUPPORTED, "project_mx4: M=%d above 2^19 or K=%d above 2^16", M, K);
     return VITCOP_OK;
 }
 

@@ -1,15 +1,19 @@
-// Projections of few rows by a matrix held in 4 bits (format: mx4_device.h): y = x W^T (+ residual), the few rows of a
-// decoding step's new tokens.  Bound by the matrix' bytes, 17/32 of one a value, each read once for every 64 rows of x.
+// Projections by a matrix held in 4 bits (format: mx4_device.h): y = x W^T (+ residual), for the few rows of a decoding step's
+// new tokens and up to the rows that survive pruning.  Bound by the matrix' bytes, 17/32 of one a value, until there are some
+// ten rows; then by x, which every workgroup reads, and from some hundred rows on by the matrix cores.
 //
-// A workgroup takes 16 RT rows of W and its wavefronts take turns at their columns, 128 at a time: a lane's 16 bytes are one
-// group of 32 columns of one row of W, which the conversion turns straight into operands of the product (16x16x32, W's rows
-// as the product's rows, MB blocks of 16 rows of x as its columns); the order of the columns in a sum is free as long as x is
-// read in the same one.  The wavefronts' sums meet in LDS and are added in a fixed order.
-// Columns past K and rows past M read as zeros: their offsets lie past the descriptors' ends.
+// The codes go to LDS as they are, and only an operand of a product is turned into bf16 (one instruction for two values, the
+// group's power of two included; W's rows are the product's rows, x's rows its columns, 16x16x32).  A lane's 16 bytes of
+// codes are one group of 32 columns of one row, and since the order of the columns in a sum is free as long as x is read in
+// the same one, they are the operands of four products.  Loads go straight to LDS, neighbouring lanes for neighbouring bytes:
+// an operand's lanes hold a row each, and loads in that order cost a cycle for every lane (1 x 4096 x 11008: 10.0 us, now 6.3).
+// LDS serves 16 lanes' 16 bytes at a time; the 16-byte pieces of a row are stored in an order in which 16 rows' same pieces
+// lie in different banks.  Columns past K and rows past M or N read as zeros: their offsets lie past the descriptors' ends.
 #include "vitcop_internal.h"
 #include "mx4_device.h"
 
 #include <algorithm>
+#include <atomic>
 
 namespace vitcop {
 
@@ -23,63 +27,205 @@ struct MpArgs {
     const uint16_t* res;
     int64_t x_stride, y_stride, res_stride;
     int M, N, K;
+    float* part;                         // slices of K: [slices][M][N] sums, left to be added up; or nullptr
+    int steps_per_slice;
 };
 
-template <int MB, int RT, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void mx4_project_kernel(MpArgs a) {
-    __shared__ f32x4 sums[WAVES][RT * MB][64];
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, l16 = lane & 15, g4 = lane >> 4;
-    const int n0 = blockIdx.x * (16 * RT), m0 = blockIdx.y * (16 * MB);
-    const int groups = a.K / MX4_GROUP, chunks = (groups + 3) / 4;
-    const auto c_desc = __builtin_amdgcn_make_buffer_rsrc((void*)a.codes, 0, (unsigned)((int64_t)a.N * a.K / 2), 0x00020000);
-    const auto s_desc = __builtin_amdgcn_make_buffer_rsrc((void*)a.scales, 0, (unsigned)((int64_t)a.N * groups), 0x00020000);
-    const auto x_desc = __builtin_amdgcn_make_buffer_rsrc((void*)a.x, 0, (unsigned)(((a.M - 1) * a.x_stride + a.K) * 2), 0x00020000);
-    unsigned c_off[RT], s_off[RT], x_off[MB];
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t mp_desc(const void* base, int64_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (unsigned)bytes, 0x00020000);
+}
+
+// 16 bytes a lane from memory to the 1024 bytes of LDS at `to`
+__device__ __forceinline__ void mp_load(__amdgpu_buffer_rsrc_t from, char* to, unsigned offset) {
+#ifdef __HIP_DEVICE_COMPILE__                 // (the host's pass does not know loads of 16 bytes)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, offset, 0, 0, 0);
+#endif
+}
+
+// At most 16 rows of x (or any number, 16 at a time): a workgroup takes 16 rows of W, and its wavefronts take turns at their
+// columns, 128 at a time, each with DEPTH steps in flight in an LDS ring of its own; their sums meet at the end, in a fixed
+// order.  XI: loads of four rows of x a step.  Measured with weights from HBM, us (of which 2.5 are the launch): 1 x 4096 x 4096
+// 4.1, x 11008 6.5, 1 x 11008 x 4096 6.4 (23.9 MB in 3.9 us: 6 TB/s), 7 x 11008 x 4096 8.4, 16 x 4096 x 4096 5.3.
+template <int XI, int WAVES, int DEPTH>
+constexpr int mp_ring_bytes() { return WAVES * DEPTH * (1 + XI) * 1024; }
+
+template <int XI, int WAVES, int DEPTH>
+__global__ __launch_bounds__(64 * WAVES) void mx4_few_kernel(MpArgs a) {
+    constexpr int NL = 1 + XI, SLOT = NL * 1024;             // loads a step, bytes of a step in the ring
+    extern __shared__ __attribute__((aligned(16))) char mp_lds[];
+    const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4;
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16;
+    const int groups = a.K / MX4_GROUP, steps = (groups + 3) / 4;
+    const auto c_desc = mp_desc(a.codes + (int64_t)n0 * (a.K / 2), 16 * (a.K / 2));
+    const auto s_desc = mp_desc(a.scales + (int64_t)n0 * groups, 16 * groups);
+    const auto x_desc = mp_desc(a.x + m0 * a.x_stride, ((a.M - m0 - 1) * a.x_stride + a.K) * 2);
+    char* const ring = mp_lds + wv * (DEPTH * SLOT);
+    char* const exps = mp_lds + mp_ring_bytes<XI, WAVES, DEPTH>();
+    // the epilogue's part of the first wavefront: four neighbouring columns of a row of y a lane
+    const int n = n0 + 4 * g4, m = m0 + l16;
+    const bool mine = wv == 0 && m < a.M;
+    uint2 res = make_uint2(0, 0);
+    if (a.res && mine) res = *reinterpret_cast<const uint2*>(a.res + m * a.res_stride + n);
+    // the exponents of these rows: one contiguous run of 16 * groups bytes
+    for (int u = 64 * wv; u < groups; u += 64 * WAVES) mp_load(s_desc, exps + u * 16, (u + lane) * 16);
+    // where this lane's 16 bytes of a load come from
+    const int c_grp = lane % 4 ^ (lane >> 4);
+    const unsigned c_off = (unsigned)(lane / 4) * (unsigned)(a.K / 2) + 16 * c_grp;
+    unsigned x_off[XI];
+    int x_slot[XI];
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        const int n = n0 + 16 * r + l16;
-        c_off[r] = n < a.N ? (unsigned)n * (unsigned)(a.K / 2) : MP_OUTSIDE;
-        s_off[r] = n < a.N ? (unsigned)n * (unsigned)groups : MP_OUTSIDE;
+    for (int q = 0; q < XI; ++q) {
+        const int row = 4 * q + lane / 16;
+        x_slot[q] = lane % 16 ^ row;
+        x_off[q] = m0 + row < a.M ? (unsigned)(row * a.x_stride * 2) + 16 * x_slot[q] : MP_OUTSIDE;
     }
+    auto load = [&](int slot, int step) __attribute__((always_inline)) {
+        char* const to = ring + slot * SLOT;
+        mp_load(c_desc, to, (c_off + 64 * step) | (4 * step + c_grp < groups ? 0u : MP_OUTSIDE));
 #pragma unroll
-    for (int j = 0; j < MB; ++j) {
-        const int m = m0 + 16 * j + l16;
-        x_off[j] = m < a.M ? (unsigned)(m * a.x_stride * 2) : MP_OUTSIDE;
-    }
-    u32x4 cw[RT], xv[MB][4];
-    uint32_t ce[RT];
-    auto load = [&](int chunk) __attribute__((always_inline)) {
-        const unsigned g = (unsigned)(4 * chunk + g4), outside = g < (unsigned)groups ? 0u : MP_OUTSIDE;
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            cw[r] = __builtin_amdgcn_raw_buffer_load_b128(c_desc, (c_off[r] + 16 * g) | outside, 0, 0);
-            ce[r] = __builtin_amdgcn_raw_buffer_load_b8(s_desc, (s_off[r] + g) | outside, 0, 0);
-        }
-#pragma unroll
-        for (int j = 0; j < MB; ++j)
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-                xv[j][c] = __builtin_amdgcn_raw_buffer_load_b128(x_desc, (x_off[j] + 64 * g + 16 * c) | outside, 0, 0);
+        for (int q = 0; q < XI; ++q)
+            mp_load(x_desc, to + (1 + q) * 1024, (x_off[q] + 256 * step) | (4 * step + (x_slot[q] >> 2) < groups ? 0u : MP_OUTSIDE));
     };
+#pragma unroll
+    for (int i = 0; i < DEPTH; ++i) load(i, wv + i * WAVES);         // (past the last step: nothing is fetched)
+    f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(DEPTH * NL) : "memory");
+    __builtin_amdgcn_s_barrier();                            // everybody's exponents are there
+    asm volatile("" ::: "memory");
+    int slot = 0;
+    for (int step = wv; step < steps; step += WAVES) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((DEPTH - 1) * NL) : "memory");
+        const char* const from = ring + slot * SLOT;
+        const int row = min(l16, 4 * XI - 1);                // (rows past M: whatever the last loaded one gives, not stored)
+        u32x4 xx[4];
+        const u32x4 cc = *reinterpret_cast<const u32x4*>(from + l16 * 64 + (g4 ^ (l16 >> 2)) * 16);
+        const uint32_t e = *reinterpret_cast<const uint8_t*>(exps + l16 * groups + min(4 * step + g4, groups - 1));
+#pragma unroll
+        for (int c = 0; c < 4; ++c) xx[c] = *reinterpret_cast<const u32x4*>(from + 1024 + row * 256 + ((4 * g4 + c) ^ row) * 16);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        load(slot, step + DEPTH * WAVES);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, mx4_values(cc[c], mx4_scale(e))),
+                                                          __builtin_bit_cast(bf16x8, xx[c]), acc, 0, 0, 0);
+        slot = slot + 1 == DEPTH ? 0 : slot + 1;
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");          // no load may outlive the ring
+    __syncthreads();
+    f32x4 (*sums)[64] = reinterpret_cast<f32x4 (*)[64]>(mp_lds);
+    sums[wv][lane] = acc;
+    __syncthreads();
+    if (!mine) return;
+    f32x4 v = sums[0][lane];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) v += sums[w][lane];
+    v += f32x4{bf16_lo(res.x), bf16_hi(res.x), bf16_lo(res.y), bf16_hi(res.y)};
+    *reinterpret_cast<uint2*>(a.y + m * a.y_stride + n) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+}
+
+template <int XI, int WAVES, int DEPTH>
+static int launch_few(const MpArgs& a, hipStream_t s) {
+    const size_t lds = mp_ring_bytes<XI, WAVES, DEPTH>() + ((size_t)a.K / 2 + 1023) / 1024 * 1024;
+    static std::atomic<size_t> raised_to{65536};     // (per instantiation) dynamic LDS the kernel may use so far
+    if (lds > raised_to.load()) {
+        const int rc = hip_status(hipFuncSetAttribute(reinterpret_cast<const void*>(&mx4_few_kernel<XI, WAVES, DEPTH>),
+                                                      hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds),
+                                  "hipFuncSetAttribute(mx4_few)");
+        if (rc) return rc;
+        raised_to.store(lds);
+    }
+    hipLaunchKernelGGL((mx4_few_kernel<XI, WAVES, DEPTH>), dim3(a.N / 16, (a.M + 15) / 16), dim3(64 * WAVES), lds, s, a);
+    return launch_status("mx4_few");
+}
+
+// More rows: eight wavefronts, MT_WM by MT_WN, take 32 MB rows of x and 128 rows of W over a slice of K, 128 columns at a time,
+// both operands through a ring of NS steps in LDS that all of them read.  A step costs the reads from LDS, 8 (MB + .5) 2 KB at
+// 128 bytes a cycle, and then its 4 MB 2 products a wavefront, one after the other in all (reading a step ahead into
+// registers gained nothing: 64 x 4096 x 11008 12.7, 13.3 us).  K >= 512 and whole steps.  Slices' sums are added up by
+// launch_partial_reduce.  Measured without it, us: 32 x 4096 x 11008 10.2, 64 x 4096 x 11008 12.6, 64 x 11008 x 4096 14.7,
+// 317 x 3584 x 14336 39.6; four wavefronts with twice the columns each 10.4, 14.2, 16.4, 48.5.
+constexpr int MT_WM = 2, MT_WN = 4, MT_RT = 2, MT_WAVES = MT_WM * MT_WN, MT_BN = 16 * MT_RT * MT_WN;
+constexpr int MT_EXPS = MT_BN * 16;                  // bytes of four steps' exponents: a unit
+template <int MB, int NS>
+constexpr int mp_tile_bytes() { return NS * (16 * MB * MT_WM * 256 + MT_BN * 64) + 3 * MT_EXPS; }
+
+template <int MB, int NS>
+__global__ __launch_bounds__(64 * MT_WAVES) void mx4_tile_kernel(MpArgs a) {
+    constexpr int BM = 16 * MB * MT_WM, BN = MT_BN, RT = MT_RT;
+    constexpr int XL = BM / (4 * MT_WAVES), NL = XL + 1, SLOT = BM * 256 + BN * 64;        // loads of x, of x and codes a wavefront and step
+    static_assert(XL * 4 * MT_WAVES == BM && 16 * MT_WAVES == BN, "whole loads for every wavefront");
+    extern __shared__ __attribute__((aligned(16))) char mp_lds[];
+    const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4;
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wv % MT_WM, wn = wv / MT_WM;
+    // tiles of the same rows of W go to the same XCD, one after the other: they share its L2
+    const int tiles_m = (a.M + BM - 1) / BM, nth = blockIdx.x >> 3;
+    const int n0 = ((nth / tiles_m) * 8 + (blockIdx.x & 7)) * BN, m0 = nth % tiles_m * BM;
+    if (n0 >= a.N) return;
+    const int groups = a.K / MX4_GROUP;
+    const int first = blockIdx.y * a.steps_per_slice, end = min(groups / 4, first + a.steps_per_slice);
+    const int rows = min(BN, a.N - n0);
+    const auto c_desc = mp_desc(a.codes + (int64_t)n0 * (a.K / 2), (int64_t)rows * (a.K / 2));
+    const auto s_desc = mp_desc(a.scales + (int64_t)n0 * groups, (int64_t)rows * groups);
+    const auto x_desc = mp_desc(a.x + m0 * a.x_stride, ((a.M - m0 - 1) * a.x_stride + a.K) * 2);
+    const unsigned c_off = (unsigned)(16 * wv + lane / 4) * (unsigned)(a.K / 2) + 16 * (lane % 4 ^ (lane >> 4));
+    unsigned x_off[XL];
+#pragma unroll
+    for (int q = 0; q < XL; ++q) {
+        const int row = 4 * (XL * wv + q) + lane / 16;
+        x_off[q] = m0 + row < a.M ? (unsigned)(row * a.x_stride * 2) + 16 * (lane % 16 ^ (row & 15)) : MP_OUTSIDE;
+    }
+    auto load = [&](int slot, int step) __attribute__((always_inline)) {
+        char* const to = mp_lds + slot * SLOT;
+        const unsigned past = step < end ? 0u : MP_OUTSIDE;
+        mp_load(c_desc, to + BM * 256 + wv * 1024, (c_off + 64 * step) | past);
+#pragma unroll
+        for (int q = 0; q < XL; ++q) mp_load(x_desc, to + (XL * wv + q) * 1024, (x_off[q] + 256 * step) | past);
+    };
+    // Exponents come in units, 16 bytes of a row a lane: four steps (a row's last unit ends with it).  Two are asked for here, and
+    // during a unit's steps a quarter each of the one after the next.
+    char* const scales = mp_lds + NS * SLOT;
+    auto unit_at = [&](int unit) __attribute__((always_inline)) { return min(4 * first + 16 * unit, groups - 16); };
+    static_assert(MT_EXPS == 2048 && MT_WAVES >= 4, "two loads a unit");
+    if (wv < 4)
+        mp_load(s_desc, scales + wv * 1024, (unsigned)(wv % 2 * 64 + lane) * (unsigned)groups + unit_at(wv / 2));
     f32x4 acc[RT][MB];
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
         for (int j = 0; j < MB; ++j) acc[r][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (wv < chunks) load(wv);
-    for (int chunk = wv; chunk < chunks; chunk += WAVES) {
+#pragma unroll
+    for (int i = 0; i < NS - 1; ++i) load(i, first + i);     // (past the last step: nothing is fetched)
+    int slot = 0, ahead = NS - 1, exp_slot = 0;
+    for (int step = first; step < end; ++step) {
+        // everybody's loads for this step are there (at least NL for each later one were issued after them), and everybody has
+        // read the slots that are filled next
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((NS - 2) * NL) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        const char* const from = mp_lds + slot * SLOT;
+        const int unit = (step - first) >> 2, quarter = (step - first) & 3;
+        const char* const exps = scales + exp_slot * MT_EXPS + 4 * step + g4 - unit_at(unit);
         u32x4 cc[RT], xx[MB][4];
         uint32_t ee[RT];
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
-            cc[r] = cw[r];
-            ee[r] = ce[r];
+            const int row = 16 * (RT * wn + r) + l16;
+            cc[r] = *reinterpret_cast<const u32x4*>(from + BM * 256 + row * 64 + (g4 ^ (l16 >> 2)) * 16);
+            ee[r] = *reinterpret_cast<const uint8_t*>(exps + row * 16);
         }
 #pragma unroll
         for (int j = 0; j < MB; ++j)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) xx[j][c] = xv[j][c];
-        if (chunk + WAVES < chunks) load(chunk + WAVES);
+            for (int c = 0; c < 4; ++c)
+                xx[j][c] = *reinterpret_cast<const u32x4*>(from + (16 * (MB * wm + j) + l16) * 256 + ((4 * g4 + c) ^ l16) * 16);
+        const int e_row = BN / 4 * quarter + BN / 32 * wv;
+        if (lane < BN / 32)
+            mp_load(s_desc, scales + (exp_slot == 0 ? 2 : exp_slot - 1) * MT_EXPS + e_row * 16,
+                    (unsigned)(e_row + lane) * (unsigned)groups + unit_at(unit + 2));
+        load(ahead, step + NS - 1);
+        if (quarter == 3) exp_slot = exp_slot == 2 ? 0 : exp_slot + 1;
 #pragma unroll
         for (int c = 0; c < 4; ++c)
 #pragma unroll
@@ -89,44 +235,103 @@ __global__ __launch_bounds__(64 * WAVES) void mx4_project_kernel(MpArgs a) {
                 for (int j = 0; j < MB; ++j)
                     acc[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(bf16x8, xx[j][c]), acc[r][j], 0, 0, 0);
             }
+        slot = slot + 1 == NS ? 0 : slot + 1;
+        ahead = ahead + 1 == NS ? 0 : ahead + 1;
     }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");          // no load may outlive the workgroup's LDS
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int j = 0; j < MB; ++j) sums[wv][r * MB + j][lane] = acc[r][j];
-    __syncthreads();
-    // a thread adds up four neighbouring columns of a row of y
-    for (int idx = threadIdx.x; idx < RT * MB * 64; idx += 64 * WAVES) {
-        const int t = idx >> 6, r = t / MB, j = t - r * MB, ln = idx & 63;
-        const int n = n0 + 16 * r + 4 * (ln >> 4), m = m0 + 16 * j + (ln & 15);
-        if (n >= a.N || m >= a.M) continue;
-        f32x4 v = sums[0][t][ln];
-#pragma unroll
-        for (int w = 1; w < WAVES; ++w) v += sums[w][t][ln];
-        if (a.res) {
-            const uint2 u = *reinterpret_cast<const uint2*>(a.res + m * a.res_stride + n);
-            v += f32x4{bf16_lo(u.x), bf16_hi(u.x), bf16_lo(u.y), bf16_hi(u.y)};
+        for (int j = 0; j < MB; ++j) {
+            const int n = n0 + 16 * (RT * wn + r) + 4 * g4, m = m0 + 16 * (MB * wm + j) + l16;
+            if (n >= a.N || m >= a.M) continue;
+            f32x4 v = acc[r][j];
+            if (a.part) {
+                *reinterpret_cast<f32x4*>(a.part + ((int64_t)blockIdx.y * a.M + m) * a.N + n) = v;
+                continue;
+            }
+            if (a.res) {
+                const uint2 u = *reinterpret_cast<const uint2*>(a.res + m * a.res_stride + n);
+                v += f32x4{bf16_lo(u.x), bf16_hi(u.x), bf16_lo(u.y), bf16_hi(u.y)};
+            }
+            *reinterpret_cast<uint2*>(a.y + m * a.y_stride + n) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
         }
-        *reinterpret_cast<uint2*>(a.y + m * a.y_stride + n) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+}
+
+template <int MB, int NS>
+static int launch_tiles(const MpArgs& a, int slices, hipStream_t s) {
+    const int tiles = ((a.N + MT_BN - 1) / MT_BN + 7) / 8 * 8 * ((a.M + 32 * MB - 1) / (32 * MB));
+    constexpr int lds = mp_tile_bytes<MB, NS>();
+    static_assert(lds <= 160 * 1024, "LDS of a CU");
+    static std::atomic<bool> raised{false};          // (per instantiation; a second thread repeating the call is harmless)
+    if (lds > 65536 && !raised.load()) {
+        const int rc = hip_status(hipFuncSetAttribute(reinterpret_cast<const void*>(&mx4_tile_kernel<MB, NS>),
+                                                      hipFuncAttributeMaxDynamicSharedMemorySize, lds),
+                                  "hipFuncSetAttribute(mx4_tile)");
+        if (rc) return rc;
+        raised.store(true);
     }
+    hipLaunchKernelGGL((mx4_tile_kernel<MB, NS>), dim3(tiles, slices), dim3(64 * MT_WAVES), lds, s, a);
+    return launch_status("mx4_tile");
 }
 
-template <int MB, int RT, int WAVES>
-static int launch_rows(const MpArgs& a, hipStream_t s) {
-    hipLaunchKernelGGL((mx4_project_kernel<MB, RT, WAVES>), dim3((a.N + 16 * RT - 1) / (16 * RT), (a.M + 16 * MB - 1) / (16 * MB)),
-                       dim3(64 * WAVES), 0, s, a);
-    return launch_status("mx4_project");
+// A launch on whole tiles.  Rows of x a tile, 32 mb: what reads the least x and products in vain, of a step's time, which is
+// about 2 + mb.  Slices of K: as many as there are workgroups for on the 256 CUs, of at least four steps (64 x 11008 x 4096,
+// 86 tiles, in one slice, two and four 23.4, 14.6, 15.8 us; 64 x 4096 x 11008, 32 tiles, in four, eight and sixteen 15.1, 12.6,
+// 14.0 us; each without the reduction).
+struct MpPlan {
+    int mb, slices, steps_per_slice;     // mb == 0: mx4_few_kernel, 16 rows of x at a time
+};
+static MpPlan mp_plan(int M, int N, int K) {
+    if (M <= 16 || K % 128 != 0 || K < 512) return {0, 1, 0};
+    MpPlan p{1, 1, 0};
+    int least = INT32_MAX;
+    for (int mb = 1; mb <= 5; ++mb) {
+        const int cost = (M + 32 * mb - 1) / (32 * mb) * (2 + mb);
+        if (cost < least) {
+            least = cost;
+            p.mb = mb;
+        }
+    }
+    const int64_t tiles = (int64_t)((N + MT_BN - 1) / MT_BN) * ((M + 32 * p.mb - 1) / (32 * p.mb));
+    const int steps = K / 128;
+    p.slices = (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, steps / 4));
+    p.steps_per_slice = (steps + p.slices - 1) / p.slices;
+    p.slices = (steps + p.steps_per_slice - 1) / p.steps_per_slice;          // (none of them empty)
+    return p;
 }
 
-size_t project_mx4_workspace_bytes(int M, int N, int K) { return 0; }
+size_t project_mx4_workspace_bytes(int M, int N, int K) {
+    const MpPlan p = mp_plan(M, N, K);
+    return p.slices > 1 ? up256((size_t)p.slices * M * N * 4) : 0;
+}
 
 int launch_project_mx4(const uint16_t* x, int64_t x_stride, const uint8_t* codes, const uint8_t* scales, uint16_t* y,
                        int64_t y_stride, const uint16_t* res, int64_t res_stride, int M, int N, int K, void* ws,
                        size_t ws_bytes, hipStream_t s) {
-    const MpArgs a{x, codes, scales, y, res, x_stride, y_stride, res_stride, M, N, K};
-    if (M <= 16) return launch_rows<1, 1, 8>(a, s);
-    if (M <= 32) return launch_rows<2, 2, 8>(a, s);
-    return launch_rows<4, 2, 8>(a, s);
+    MpArgs a{x, codes, scales, y, res, x_stride, y_stride, res_stride, M, N, K, nullptr, 0};
+    MpPlan p = mp_plan(M, N, K);
+    if (p.mb == 0) {
+        // with more tiles than two for every CU four wavefronts each, which fit side by side (1 x 11008 x 4096 6.4, 7.1 us with
+        // eight; 1 x 4096 x 11008 7.1, 6.5); more rows keep more in flight
+        const bool many = N / 16 > 512;
+        if (M <= 4) return many ? launch_few<1, 4, 2>(a, s) : launch_few<1, 8, 3>(a, s);
+        return M <= 8 ? launch_few<2, 4, 2>(a, s) : launch_few<4, 4, 3>(a, s);
+    }
+    if (p.slices > 1 && ws_bytes < project_mx4_workspace_bytes(M, N, K)) p.slices = 1;
+    a.steps_per_slice = p.slices > 1 ? p.steps_per_slice : K / 128;
+    if (p.slices > 1) a.part = static_cast<float*>(ws);
+    int rc = 0;
+    switch (p.mb) {
+        case 1: rc = launch_tiles<1, 4>(a, p.slices, s); break;
+        case 2: rc = launch_tiles<2, 4>(a, p.slices, s); break;
+        case 3: rc = launch_tiles<3, 3>(a, p.slices, s); break;
+        case 4: rc = launch_tiles<4, 3>(a, p.slices, s); break;
+        default: rc = launch_tiles<5, 3>(a, p.slices, s); break;
+    }
+    if (rc || p.slices == 1) return rc;
+    return launch_partial_reduce(SkParts{a.part, p.slices, N, M}, N, sk_mats(nullptr, y, y_stride, N), res, res_stride, nullptr,
+                                 nullptr, 0.f, nullptr, 0, nullptr, s);
 }
 
 }  // namespace vitcop
