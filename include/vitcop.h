@@ -550,6 +550,8 @@ int vitcop_cache_mx4_read(const vitcop_cache_mx4_t* C, uint16_t* k, uint16_t* v,
  * over its first n_samples[b] (int32 [B] DEVICE, may be NULL; clamped to [0,N]).  A sample without rows gets
  * zeros and an lse of -inf; rows from n_samples[b] on are not looked at, whatever they hold.
  *   q [B,Hq,d] bf16;  out [B,Hq,d] bf16;  lse_out [B,Hq] fp32, may be NULL;  scale 0 selects 1/sqrt(d)
+ *   ws: device scratch of ws_bytes >= vitcop_decode_attn_mx4_workspace_bytes, NULL where that is 0 (it is 0 too
+ *   where the sizes are refused)
  * Hq % Hkv == 0; 0 <= N <= capacity; B*Hq < 2^24; B, Hkv, d are the descriptor's. */
 size_t vitcop_decode_attn_mx4_workspace_bytes(int B, int N, int Hq, int Hkv, int d);
 int vitcop_decode_attn_mx4(const uint16_t* q, const vitcop_cache_mx4_t* C, uint16_t* out, float* lse_out, int N,

@@ -787,6 +787,8 @@ MX4_GROUP = 32
 
 def _expect(t, name: str, shape, dtype, device) -> None:
     """A contiguous tensor of this shape and type on this device (dtype None: any 16-bit type)."""
+    if t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous():
+        return
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, not on {device}")
     if tuple(t.shape) != tuple(shape):
@@ -801,19 +803,21 @@ def _here(t, name: str) -> torch.device:
     """The tensor's device, which has to be the current one: that is whose stream the call goes to."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, the current device is {torch.cuda.current_device()}")
+    current = _current_device() if _current_device is not None else torch.cuda.current_device()
+    if t.get_device() != current:
+        raise ValueError(f"{name} is on {t.device}, the current device is {current}")
     return t.device
 
 
 def _rows_of(t, name: str):
     """(M, K, row stride) of a 16-bit matrix whose rows are contiguous."""
-    if t.dim() != 2 or t.element_size() != 2:
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 2 or t.element_size() != 2:
         raise ValueError(f"{name} must be a 16-bit (bf16) matrix")
-    M, K = t.shape
-    if K > 1 and t.stride(1) != 1:
+    M, K = shape
+    if K > 1 and strides[1] != 1:
         raise ValueError(f"{name} must have contiguous rows")
-    return M, K, t.stride(0) if M > 1 else K
+    return M, K, strides[0] if M > 1 else K
 
 
 def vitcop_mx4_quantize(x, out=None):
@@ -821,26 +825,30 @@ def vitcop_mx4_quantize(x, out=None):
     dev = _here(x, "x")
     M, K, stride = _rows_of(x, "x")
     if out is None:
-        out = (torch.empty((M, K // 2), dtype=torch.uint8, device=dev),
-               torch.empty((M, K // MX4_GROUP), dtype=torch.uint8, device=dev))
-    codes, scales = out
-    _expect(codes, "codes", (M, K // 2), torch.uint8, dev)
-    _expect(scales, "scales", (M, K // MX4_GROUP), torch.uint8, dev)
-    _check(lib.vitcop_mx4_quantize(_ptr(x), stride, M, K, _ptr(codes), _ptr(scales), _stream()))
+        codes = torch.empty((M, K // 2), dtype=torch.uint8, device=dev)
+        scales = torch.empty((M, K // MX4_GROUP), dtype=torch.uint8, device=dev)
+    else:
+        codes, scales = out
+        _expect(codes, "codes", (M, K // 2), torch.uint8, dev)
+        _expect(scales, "scales", (M, K // MX4_GROUP), torch.uint8, dev)
+    _check(lib.vitcop_mx4_quantize(x.data_ptr(), stride, M, K, codes.data_ptr(), scales.data_ptr(), _stream()))
     return codes, scales
 
 
 def vitcop_mx4_dequantize(codes, scales, out=None):
-    """(codes [M,K/2], scales [M,K/32]) uint8 -> [M,K] bf16 (exact)."""
+    """(codes [M,K/2], scales [M,K/32]) uint8 -> [M,K] bf16 (exact); ``out`` reuses a buffer (rows may be strided)."""
     dev = _here(codes, "codes")
     M, K = codes.shape[0], codes.shape[1] * 2
     _expect(codes, "codes", (M, K // 2), torch.uint8, dev)
     _expect(scales, "scales", (M, K // MX4_GROUP), torch.uint8, dev)
+    stride = K
     if out is None:
         out = torch.empty((M, K), dtype=torch.bfloat16, device=dev)
-    if out.device != dev or tuple(out.shape) != (M, K):
+    elif out.device != dev or out.shape != (M, K):
         raise ValueError(f"out must be {(M, K)} on {dev}")
-    _check(lib.vitcop_mx4_dequantize(_ptr(codes), _ptr(scales), M, K, _ptr(out), _rows_of(out, "out")[2], _stream()))
+    else:
+        stride = _rows_of(out, "out")[2]
+    _check(lib.vitcop_mx4_dequantize(codes.data_ptr(), scales.data_ptr(), M, K, out.data_ptr(), stride, _stream()))
     return out
 
 
@@ -858,7 +866,8 @@ class CacheMx4:
             _expect(t, name, (B, Hkv, capacity, width), torch.uint8, self.device)
         self.B, self.Hkv, self.capacity, self.d = B, Hkv, capacity, half * 2
         self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
-        self.desc = CacheMx4T(B, capacity, Hkv, half * 2, _ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales))
+        self.desc = CacheMx4T(B, capacity, Hkv, half * 2, k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(),
+                              v_scales.data_ptr())
 
     @classmethod
     def empty(cls, B: int, capacity: int, Hkv: int, d: int, device="cuda"):
@@ -866,39 +875,44 @@ class CacheMx4:
         return cls(*[torch.empty((B, Hkv, capacity, w), dtype=torch.uint8, device=device) for w in widths])
 
     def per_sample(self, t, name: str):
-        if t is not None:
-            _expect(t, name, (self.B,), torch.int32, self.device)
-        return _ptr(t)
+        if t is None:
+            return None
+        _expect(t, name, (self.B,), torch.int32, self.device)
+        return t.data_ptr()
+
+
+def _cache_rows(cache: CacheMx4, t, name: str):
+    """(T, row stride, batch stride) of K or V rows [B,T,Hkv,d] whose heads lie side by side."""
+    shape = t.shape
+    if t.device != cache.device or t.element_size() != 2 or len(shape) != 4:
+        raise ValueError(f"{name} must be a 16-bit [B,T,Hkv,d] tensor on {cache.device}")
+    T = shape[1]
+    if shape != (cache.B, T, cache.Hkv, cache.d):
+        raise ValueError(f"{name} must be {(cache.B, T, cache.Hkv, cache.d)}, not {tuple(shape)}")
+    sb, st, sh, sd = t.stride()
+    if sd != 1 or (cache.Hkv > 1 and sh != cache.d):
+        raise ValueError(f"{name}: a token's heads must lie side by side")
+    row = st if T > 1 else cache.Hkv * cache.d
+    return T, row, sb if cache.B > 1 else T * row
 
 
 def vitcop_cache_mx4_write(cache: CacheMx4, k, v, start: int = 0, start_samples=None, n_samples=None) -> None:
     """Rows of k, v [B,T,Hkv,d] (either may be None) to rows start + t of the cache, or start_samples[b] + t (int32 [B]);
     with n_samples (int32 [B]) the first n_samples[b] rows of sample b only.  A token's heads lie side by side; tokens and
     samples may be strided (views of fused QKV rows)."""
-    sides, T = [], 0
-    for t, name in ((k, "k"), (v, "v")):
-        if t is None:
-            sides.append(None)
-            continue
-        if t.device != cache.device or t.element_size() != 2 or t.dim() != 4:
-            raise ValueError(f"{name} must be a 16-bit [B,T,Hkv,d] tensor on {cache.device}")
-        T = t.shape[1]
-        if tuple(t.shape) != (cache.B, T, cache.Hkv, cache.d):
-            raise ValueError(f"{name} must be {(cache.B, T, cache.Hkv, cache.d)}, not {tuple(t.shape)}")
-        if t.stride(3) != 1 or (cache.Hkv > 1 and t.stride(2) != cache.d):
-            raise ValueError(f"{name}: a token's heads must lie side by side")
-        row = t.stride(1) if T > 1 else cache.Hkv * cache.d
-        sides.append((row, t.stride(0) if cache.B > 1 else T * row))
-    if k is not None and v is not None and k.shape[1] != v.shape[1]:
-        raise ValueError("k and v differ in their number of rows")
     _here(cache.k_codes, "the cache")
-    start_p, n_p = cache.per_sample(start_samples, "start_samples"), cache.per_sample(n_samples, "n_samples")
-    if sides[0] is not None and sides[1] is not None and sides[0] != sides[1]:       # strides of their own: two calls
-        vitcop_cache_mx4_write(cache, k, None, start, start_samples, n_samples)
+    k_rows = _cache_rows(cache, k, "k") if k is not None else None
+    v_rows = _cache_rows(cache, v, "v") if v is not None else k_rows
+    if k_rows is not None and k_rows != v_rows:
+        if k_rows[0] != v_rows[0]:
+            raise ValueError("k and v differ in their number of rows")
+        vitcop_cache_mx4_write(cache, k, None, start, start_samples, n_samples)      # strides of their own: two calls
         vitcop_cache_mx4_write(cache, None, v, start, start_samples, n_samples)
         return
-    row, batch = sides[0] or sides[1] or (0, 0)
-    _check(lib.vitcop_cache_mx4_write(C.byref(cache.desc), _ptr(k), _ptr(v), row, batch, T, start, start_p, n_p, _stream()))
+    T, row, batch = v_rows if v_rows is not None else (0, 0, 0)
+    _check(lib.vitcop_cache_mx4_write(cache.desc, _ptr(k), _ptr(v), row, batch, T, start,
+                                      cache.per_sample(start_samples, "start_samples"),
+                                      cache.per_sample(n_samples, "n_samples"), _stream()))
 
 
 def vitcop_cache_mx4_read(cache: CacheMx4, T: int, start: int = 0, start_samples=None, out=None):
@@ -914,7 +928,7 @@ def vitcop_cache_mx4_read(cache: CacheMx4, T: int, start: int = 0, start_samples
     for t, name in ((k, "k"), (v, "v")):
         if t is not None:
             _expect(t, name, shape, None, cache.device)
-    _check(lib.vitcop_cache_mx4_read(C.byref(cache.desc), _ptr(k), _ptr(v), T, start,
+    _check(lib.vitcop_cache_mx4_read(cache.desc, _ptr(k), _ptr(v), T, start,
                                      cache.per_sample(start_samples, "start_samples"), _stream()))
     return k, v
 
@@ -937,36 +951,42 @@ def vitcop_decode_attn_mx4(q, cache: CacheMx4, N: int, n_samples=None, scale: fl
         if lse is not None:
             _expect(lse, "lse", (cache.B, Hq), torch.float32, dev)
     if ws is None:
-        ws = _ws(lib.vitcop_decode_attn_mx4_workspace_bytes(cache.B, N, Hq, cache.Hkv, cache.d), q)
+        nb = lib.vitcop_decode_attn_mx4_workspace_bytes(cache.B, N, Hq, cache.Hkv, cache.d)
+        ws = _ws(nb, q) if nb else None
     elif ws.device != dev or ws.dtype != torch.uint8:
         raise ValueError(f"ws must be a uint8 tensor on {dev}")
-    _check(lib.vitcop_decode_attn_mx4(_ptr(q), C.byref(cache.desc), _ptr(o), _ptr(lse), N,
-                                      cache.per_sample(n_samples, "n_samples"), Hq, scale, _ptr(ws), ws.numel(), _stream()))
+    _check(lib.vitcop_decode_attn_mx4(q.data_ptr(), cache.desc, o.data_ptr(), _ptr(lse), N,
+                                      cache.per_sample(n_samples, "n_samples"), Hq, scale, _ptr(ws),
+                                      ws.numel() if ws is not None else 0, _stream()))
     return o, lse
 
 
 def vitcop_project_mx4(x, codes, scales, residual=None, out=None, ws=None):
     """x [M,K] bf16 (rows may be strided), a matrix [N,K] as codes [N,K/2] and scales [N,K/32] (vitcop_mx4_quantize) ->
-    x W^T (+ residual) [M,N].  ``out`` reuses a buffer (rows may be strided), ``ws`` a uint8 workspace."""
+    x W^T (+ residual) [M,N].  ``out`` reuses a buffer (rows may be strided; the residual itself, too), ``ws`` a uint8
+    workspace (one that is too small for slices of K is not used)."""
     dev = _here(x, "x")
     M, K, x_stride = _rows_of(x, "x")
     N = codes.shape[0]
     _expect(codes, "codes", (N, K // 2), torch.uint8, dev)
     _expect(scales, "scales", (N, K // MX4_GROUP), torch.uint8, dev)
+    y_stride = res_stride = N
     if out is None:
         out = torch.empty((M, N), dtype=x.dtype, device=dev)
-    res_stride = N
-    for t, name in ((out, "out"), (residual, "residual")):
-        if t is not None and (t.device != dev or tuple(t.shape) != (M, N)):
-            raise ValueError(f"{name} must be {(M, N)} on {dev}")
+    elif out.device != dev or out.shape != (M, N):
+        raise ValueError(f"out must be {(M, N)} on {dev}")
+    else:
+        y_stride = _rows_of(out, "out")[2]
     if residual is not None:
+        if residual.device != dev or residual.shape != (M, N):
+            raise ValueError(f"residual must be {(M, N)} on {dev}")
         res_stride = _rows_of(residual, "residual")[2]
-    nb = lib.vitcop_project_mx4_workspace_bytes(M, N, K)
     if ws is None:
+        nb = lib.vitcop_project_mx4_workspace_bytes(M, N, K) if M > 16 else 0
         ws = _ws(nb, x) if nb else None
     elif ws.device != dev or ws.dtype != torch.uint8:
         raise ValueError(f"ws must be a uint8 tensor on {dev}")
-    _check(lib.vitcop_project_mx4(_ptr(x), x_stride, _ptr(codes), _ptr(scales), _ptr(out), _rows_of(out, "out")[2],
+    _check(lib.vitcop_project_mx4(x.data_ptr(), x_stride, codes.data_ptr(), scales.data_ptr(), out.data_ptr(), y_stride,
                                   _ptr(residual), res_stride, M, N, K, _ptr(ws), ws.numel() if ws is not None else 0,
                                   _stream()))
     return out

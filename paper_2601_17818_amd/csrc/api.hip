@@ -1419,7 +1419,7 @@ int vitcop_decode_attn_mx4(const uint16_t* q, const vitcop_cache_mx4_t* C, uint1
     REQUIRE(q && out, VITCOP_EINVAL, "decode_attn_mx4: null pointer");
     REQUIRE(aligned16(q) && aligned16(out) && aligned16(ws), VITCOP_EINVAL, "decode_attn_mx4: pointers must be 16-byte aligned");
     const size_t need = decode_mx4_workspace_bytes(C->B, N, Hq, C->Hkv, C->d);
-    REQUIRE(ws && ws_bytes >= need, VITCOP_EWORKSPACE, "decode_attn_mx4: workspace %zu < %zu", ws_bytes, need);
+    REQUIRE(need == 0 || (ws && ws_bytes >= need), VITCOP_EWORKSPACE, "decode_attn_mx4: workspace %zu < %zu", ws_bytes, need);
     if (scale == 0.f) scale = 1.0f / std::sqrt((float)C->d);
     return launch_decode_attn_mx4(q, *C, out, lse_out, N, n_samples, Hq, scale, ws, static_cast<hipStream_t>(stream));
 }

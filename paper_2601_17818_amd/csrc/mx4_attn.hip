@@ -31,8 +31,10 @@ __device__ __forceinline__ float mx4_lse(float m, float l) {
     return l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
+// WAVES wavefronts, 32 keys at a time each, share the slice (attn_plan: how many).  Registers for three workgroups of four on a
+// CU, two of eight.
 template <int D, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, D == 128 ? 3 : 4) void mx4_attn_kernel(
+__global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 3) void mx4_attn_kernel(
     const uint16_t* __restrict__ q, const uint8_t* __restrict__ k_codes, const uint8_t* __restrict__ k_scales,
     const uint8_t* __restrict__ v_codes, const uint8_t* __restrict__ v_scales, float* __restrict__ part_o,
     float* __restrict__ part_ml, int capacity, int N, int Hq, int Hkv, int g0, int G, float scale_log2e, int keys_per_split,
@@ -43,26 +45,18 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 ? 3 : 4) void mx4_attn_kernel(
     constexpr int LPR = ROW / 16, RPL = 64 / LPR, VL = MA_KEYS / RPL;         // V: lanes a row, rows a load, loads a tile
     static_assert(MA_KEYS * VROW >= MA_MAX_G * D * 4, "the outputs take V's place at the end");
     __shared__ __attribute__((aligned(16))) char vt[WAVES][MA_KEYS * VROW];
-    __shared__ float sm[WAVES][MA_MAX_G][2];
-    float (&so)[WAVES][MA_MAX_G][D] = *reinterpret_cast<float (*)[WAVES][MA_MAX_G][D]>(&vt[0][0]);
-    const int split = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, l16 = lane & 15, g4 = lane >> 4;
+    const int split = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
     const int h0 = hk * (Hq / Hkv) + g0;                     // first query head of this pass
-    const int n_keys = n_samples ? min(max(n_samples[b], 0), N) : N;
-    const int key_begin = split * keys_per_split, key_end = min(n_keys, key_begin + keys_per_split);
-
-    f32x4 o[BLOCKS];
-#pragma unroll
-    for (int i = 0; i < BLOCKS; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.f;                            // of head l16 (m for all its keys, l over this lane's)
+    const int key_begin = split * keys_per_split, slice_end = min(N, key_begin + keys_per_split);
+    const int first = key_begin + wv * MA_KEYS;
 
     // Rows past the slice's end read as zeros: the descriptors end there.
     const int64_t head_row = ((int64_t)b * Hkv + hk) * capacity;
-    const unsigned rows = (unsigned)max(key_end, 0);
-    const auto kc_desc = __builtin_amdgcn_make_buffer_rsrc((void*)(k_codes + head_row * ROW), 0, rows * ROW, 0x00020000);
-    const auto ks_desc = __builtin_amdgcn_make_buffer_rsrc((void*)(k_scales + head_row * GROUPS), 0, rows * GROUPS, 0x00020000);
-    const auto vc_desc = __builtin_amdgcn_make_buffer_rsrc((void*)(v_codes + head_row * ROW), 0, rows * ROW, 0x00020000);
-    const auto vs_desc = __builtin_amdgcn_make_buffer_rsrc((void*)(v_scales + head_row * GROUPS), 0, rows * GROUPS, 0x00020000);
+    const auto kc_desc = __builtin_amdgcn_make_buffer_rsrc((void*)(k_codes + head_row * ROW), 0, slice_end * ROW, 0x00020000);
+    const auto ks_desc = __builtin_amdgcn_make_buffer_rsrc((void*)(k_scales + head_row * GROUPS), 0, slice_end * GROUPS, 0x00020000);
+    const auto vc_desc = __builtin_amdgcn_make_buffer_rsrc((void*)(v_codes + head_row * ROW), 0, slice_end * ROW, 0x00020000);
+    const auto vs_desc = __builtin_amdgcn_make_buffer_rsrc((void*)(v_scales + head_row * GROUPS), 0, slice_end * GROUPS, 0x00020000);
     constexpr int NT = 2;                                    // non-temporal
     typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
     u32x4 kr[2], vr[VL];                                     // (d = 64: two dwords of K)
@@ -86,12 +80,16 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 ? 3 : 4) void mx4_attn_kernel(
             ve[i] = __builtin_amdgcn_raw_buffer_load_b8(vs_desc, row * GROUPS + lane % LPR, 0, NT);
         }
     };
-    const int first = key_begin + wv * MA_KEYS;
-    if (first < key_end) load(first);
+    if (first < slice_end) load(first);                      // (before it is known how many rows the sample has)
     bf16x8 qf[STEPS];                                        // Q^T of head l16 (heads past G: head G - 1), channels as K's
 #pragma unroll
     for (int c = 0; c < STEPS; ++c)
         qf[c] = *reinterpret_cast<const bf16x8*>(q + ((int64_t)b * Hq + h0 + min(l16, G - 1)) * D + D / 4 * g4 + 8 * c);
+    const int key_end = n_samples ? min(slice_end, max(n_samples[b], 0)) : slice_end;
+    f32x4 o[BLOCKS];
+#pragma unroll
+    for (int i = 0; i < BLOCKS; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;                            // of head l16 (m for all its keys, l over this lane's)
     typedef __attribute__((ext_vector_type(4))) short s16x4;
     typedef __attribute__((ext_vector_type(8))) short s16x8;
     char* const mine = vt[wv];
@@ -108,6 +106,13 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 ? 3 : 4) void mx4_attn_kernel(
                 s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, mx4_values(kr[t][c], e)), qf[c], s[t],
                                                                0, 0, 0);
         }
+        if (key0 + MA_KEYS > key_end)                        // rows past the sample's: zeros, whatever they hold
+#pragma unroll
+            for (int i = 0; i < VL; ++i)
+                if (key0 + RPL * i + lane / LPR >= key_end) {
+                    vr[i] = u32x4{0u, 0u, 0u, 0u};
+                    ve[i] = 0u;
+                }
 #pragma unroll
         for (int i = 0; i < VL; ++i) {
             const float e = mx4_scale(ve[i]);
@@ -115,7 +120,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 ? 3 : 4) void mx4_attn_kernel(
 #pragma unroll
             for (int c = 0; c < 4; ++c) row[c] = mx4_values(vr[i][c], e);
         }
-        if (key0 + WAVES * MA_KEYS < key_end) load(key0 + WAVES * MA_KEYS);      // (uniform) in flight from here on
+        if (key0 + WAVES * MA_KEYS < key_end) load(key0 + WAVES * MA_KEYS);        // (uniform) in flight from here on
         float p[8], top = -INFINITY;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -162,13 +167,17 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 ? 3 : 4) void mx4_attn_kernel(
     }
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
+    __shared__ float sm[WAVES][MA_MAX_G][2];
+    float (&so)[WAVES][MA_MAX_G][D] = *reinterpret_cast<float (*)[WAVES][MA_MAX_G][D]>(&vt[0][0]);
     __syncthreads();                                         // all are done with V
-    if (g4 == 0) {
-        sm[wv][l16][0] = m;
-        sm[wv][l16][1] = l;
-    }
+    if (l16 < G) {
+        if (g4 == 0) {
+            sm[wv][l16][0] = m;
+            sm[wv][l16][1] = l;
+        }
 #pragma unroll
-    for (int i = 0; i < BLOCKS; ++i) *reinterpret_cast<f32x4*>(&so[wv][l16][16 * i + 4 * g4]) = o[i];
+        for (int i = 0; i < BLOCKS; ++i) *reinterpret_cast<f32x4*>(&so[wv][l16][16 * i + 4 * g4]) = o[i];
+    }
     __syncthreads();
     // the wavefronts' states combined by threads (head, channel): this slice's partial, or with `out` the output
     for (int idx = threadIdx.x; idx < G * D; idx += 64 * WAVES) {
@@ -199,52 +208,113 @@ __global__ __launch_bounds__(64 * WAVES, D == 128 ? 3 : 4) void mx4_attn_kernel(
     }
 }
 
+// The slices of a head combined: a thread takes four channels of every MM_GROUPSth slice, whose loads go out before the weights
+// are known; the groups' sums meet in LDS in a fixed order.
+constexpr int MM_THREADS = 256;
 template <int D>
-__global__ __launch_bounds__(D) void mx4_merge_kernel(const float* __restrict__ part_o, const float* __restrict__ part_ml,
-                                                      int n_splits, uint16_t* __restrict__ out, float* __restrict__ lse) {
+__global__ __launch_bounds__(MM_THREADS) void mx4_merge_kernel(const float* __restrict__ part_o, const float* __restrict__ part_ml,
+                                                               int n_splits, uint16_t* __restrict__ out, float* __restrict__ lse) {
+    constexpr int QUADS = D / 4, MM_GROUPS = MM_THREADS / QUADS, AHEAD = 4;
+    __shared__ f32x4 sums[MM_GROUPS][QUADS];
+    __shared__ float total[MM_GROUPS];
     const int64_t bh = blockIdx.x;
-    const int ch = threadIdx.x;
+    const int c = threadIdx.x % QUADS, grp = threadIdx.x / QUADS;
+    const float* po = part_o + bh * n_splits * D + 4 * c;
+    const float2* ml = reinterpret_cast<const float2*>(part_ml) + bh * n_splits;
+    f32x4 x[AHEAD];
+    float2 w[AHEAD];
+    auto request = [&](int s0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int t = 0; t < AHEAD; ++t) {
+            const int s = s0 + t * MM_GROUPS;
+            if (s < n_splits) {
+                x[t] = *reinterpret_cast<const f32x4*>(po + (int64_t)s * D);
+                w[t] = ml[s];
+            }
+        }
+    };
+    request(grp);
     float mn = -INFINITY;
-    for (int s = 0; s < n_splits; ++s) mn = fmaxf(mn, part_ml[(bh * n_splits + s) * 2]);
-    float lt = 0.f, ot = 0.f;
-    for (int s = 0; s < n_splits; ++s) {
-        const float a = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(part_ml[(bh * n_splits + s) * 2] - mn);
-        lt += part_ml[(bh * n_splits + s) * 2 + 1] * a;
-        ot += part_o[(bh * n_splits + s) * D + ch] * a;
+    for (int s = threadIdx.x & 63; s < n_splits; s += 64) mn = fmaxf(mn, ml[s].x);
+    mn = wave_max(mn);
+    f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
+    float l = 0.f;
+    for (int s0 = grp; s0 < n_splits; s0 += AHEAD * MM_GROUPS) {
+        if (s0 != grp) request(s0);
+#pragma unroll
+        for (int t = 0; t < AHEAD; ++t)
+            if (s0 + t * MM_GROUPS < n_splits) {
+                const float a = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(w[t].x - mn);
+                v += x[t] * a;
+                l += w[t].y * a;
+            }
     }
-    const float r = mx4_quotient(ot, lt), r1 = __shfl_down(r, 1, 64);        // neighbouring channels: one 32-bit store
-    if ((ch & 1) == 0) *reinterpret_cast<uint32_t*>(out + bh * D + ch) = pack_bf16(r, r1);
-    if (lse && ch == 0) lse[bh] = mx4_lse(mn, lt);
+    sums[grp][c] = v;
+    if (c == 0) total[grp] = l;
+    __syncthreads();
+    if (grp != 0) return;
+#pragma unroll
+    for (int i = 1; i < MM_GROUPS; ++i) {
+        v += sums[i][c];
+        l += total[i];
+    }
+    *reinterpret_cast<uint2*>(out + bh * D + 4 * c) = make_uint2(pack_bf16(mx4_quotient(v.x, l), mx4_quotient(v.y, l)),
+                                                                 pack_bf16(mx4_quotient(v.z, l), mx4_quotient(v.w, l)));
+    if (lse && c == 0) lse[bh] = mx4_lse(mn, l);
 }
 
-// Slices of the keys: workgroups for every CU, of at least 128 keys each.
-static int attn_splits(int B, int N, int Hkv) {
-    const long pairs = (long)B * Hkv;
-    return (int)std::max(1L, std::min((512 + pairs - 1) / pairs, (N + 127L) / 128));
+// How many slices of the keys and wavefronts to a slice.  A workgroup costs some two microseconds before its first and after
+// its last key, the merge of slices three, and 256 workgroups of eight wavefronts draw what the memory gives.  Measured, us
+// (samples x keys x KV heads of 128):
+//  - from 129 pairs of a sample and a KV head on, and up to 800 keys, one slice: 4 x 1000 x 32 8.7, in two and four 9.5, 9.3;
+//    1 x 640 x 32 6.4, in three 7.3; but 4 x 2000 x 32 13.2, in four 12.4; 1 x 2000 x 32 in two, four and eight 9.6, 8.8, 7.9.
+//  - slices of up to 512 keys take four wavefronts (1 x 1500 x 32 in six, with four and eight wavefronts 7.7, 7.9), longer ones
+//    eight and half as many (4 x 65536 x 4 in 32 and in 16 30.0, 29.5; 1 x 131072 x 4 in 128 and in 64 21.7, 20.0).
+//  - of one slice the more pairs there are, the fewer wavefronts: two, four and eight 8 x 640 x 32 14.0, 8.3, 7.6; 12 x 640 x 32
+//    13.7, 10.0, 11.3; 20 x 640 x 32 14.9, 14.4, 15.9; 28 x 640 x 32 17.0, 20.0, 20.7; 64 x 352 x 32 20.6, 23.3, 24.5; long ones
+//    want four again, 64 x 1536 x 32 69.3, 68.6, 74.1 (428 MB: 6.2 TB/s); and none of them to be without a key.
+struct AttnPlan {
+    int waves, keys_per_split, splits;
+};
+static AttnPlan attn_plan(int B, int N, int Hkv) {
+    const int64_t pairs = (int64_t)B * Hkv;
+    AttnPlan p{8, 0, 1};
+    if (pairs <= 128 && N > 800) {
+        p.waves = 4;
+        p.splits = (int)std::min<int64_t>(512 / pairs, (N + 255) / 256);
+        if ((N + p.splits - 1) / p.splits > 512) p = AttnPlan{8, 0, (int)(256 / pairs)};
+    } else {
+        if (pairs > 320) p.waves = pairs <= 768 || N > 1024 ? 4 : 2;
+        while (p.waves > 2 && (p.waves / 2) * MA_KEYS >= N) p.waves /= 2;
+    }
+    const int64_t unit = p.waves * MA_KEYS, keys = (N + p.splits - 1) / p.splits;
+    p.keys_per_split = (int)std::min<int64_t>(std::max<int64_t>(1, (keys + unit - 1) / unit) * unit, INT32_MAX);
+    p.splits = (int)std::max<int64_t>(1, ((int64_t)N + p.keys_per_split - 1) / p.keys_per_split);
+    return p;
 }
 
 size_t decode_mx4_workspace_bytes(int B, int N, int Hq, int Hkv, int d) {
-    const size_t s = attn_splits(B, N, Hkv);
-    return up256((size_t)B * Hq * s * d * 4) + up256((size_t)B * Hq * s * 2 * 4);
+    const size_t s = attn_plan(B, N, Hkv).splits;
+    return s == 1 ? 0 : up256((size_t)B * Hq * s * d * 4) + up256((size_t)B * Hq * s * 2 * 4);
 }
 
 template <int D>
 static int launch_attn_d(const uint16_t* q, const vitcop_cache_mx4_t& C, uint16_t* out, float* lse, int N,
                          const int32_t* n_samples, int Hq, float scale, void* ws, hipStream_t s) {
-    constexpr int WAVES = 4;
-    const int B = C.B, group = Hq / C.Hkv, ns = attn_splits(B, N, C.Hkv);
-    const int kps = ((N + ns - 1) / ns + 127) / 128 * 128;
+    const int B = C.B, group = Hq / C.Hkv;
+    const AttnPlan p = attn_plan(B, N, C.Hkv);
     float* po = static_cast<float*>(ws);
-    float* pml = reinterpret_cast<float*>(static_cast<char*>(ws) + up256((size_t)B * Hq * ns * D * 4));
+    float* pml = reinterpret_cast<float*>(static_cast<char*>(ws) + up256((size_t)B * Hq * p.splits * D * 4));
+    auto* kernel = p.waves == 8 ? mx4_attn_kernel<D, 8> : (p.waves == 4 ? mx4_attn_kernel<D, 4> : mx4_attn_kernel<D, 2>);
     for (int g0 = 0; g0 < group; g0 += MA_MAX_G) {
-        hipLaunchKernelGGL((mx4_attn_kernel<D, WAVES>), dim3(ns, C.Hkv, B), dim3(64 * WAVES), 0, s, q, C.k_codes, C.k_scales,
-                           C.v_codes, C.v_scales, po, pml, C.capacity, N, Hq, C.Hkv, g0, std::min(MA_MAX_G, group - g0),
-                           scale * 1.4426950408889634f, kps, ns, n_samples, ns == 1 ? out : nullptr, lse);
+        hipLaunchKernelGGL(kernel, dim3(p.splits, C.Hkv, B), dim3(64 * p.waves), 0, s, q, C.k_codes, C.k_scales, C.v_codes,
+                           C.v_scales, po, pml, C.capacity, N, Hq, C.Hkv, g0, std::min(MA_MAX_G, group - g0),
+                           scale * 1.4426950408889634f, p.keys_per_split, p.splits, n_samples, p.splits == 1 ? out : nullptr, lse);
         const int rc = launch_status("mx4_attn");
         if (rc) return rc;
     }
-    if (ns == 1) return VITCOP_OK;
-    hipLaunchKernelGGL((mx4_merge_kernel<D>), dim3((unsigned)(B * Hq)), dim3(D), 0, s, po, pml, ns, out, lse);
+    if (p.splits == 1) return VITCOP_OK;
+    hipLaunchKernelGGL((mx4_merge_kernel<D>), dim3((unsigned)(B * Hq)), dim3(MM_THREADS), 0, s, po, pml, p.splits, out, lse);
     return launch_status("mx4_merge");
 }
 

@@ -144,7 +144,7 @@ static int launch_few(const MpArgs& a, hipStream_t s) {
 // both operands through a ring of NS steps in LDS that all of them read.  A step costs the reads from LDS, 8 (MB + .5) 2 KB at
 // 128 bytes a cycle, and then its 4 MB 2 products a wavefront, one after the other in all (reading a step ahead into
 // registers gained nothing: 64 x 4096 x 11008 12.7, 13.3 us).  K >= 512 and whole steps.  Slices' sums are added up by
-// launch_partial_reduce.  Measured without it, us: 32 x 4096 x 11008 10.2, 64 x 4096 x 11008 12.6, 64 x 11008 x 4096 14.7,
+// mx4_sum_kernel.  Measured without it, us: 32 x 4096 x 11008 10.2, 64 x 4096 x 11008 12.6, 64 x 11008 x 4096 14.7,
 // 317 x 3584 x 14336 39.6; four wavefronts with twice the columns each 10.4, 14.2, 16.4, 48.5.
 constexpr int MT_WM = 2, MT_WN = 4, MT_RT = 2, MT_WAVES = MT_WM * MT_WN, MT_BN = 16 * MT_RT * MT_WN;
 constexpr int MT_EXPS = MT_BN * 16;                  // bytes of four steps' exponents: a unit
@@ -275,7 +275,35 @@ static int launch_tiles(const MpArgs& a, int slices, hipStream_t s) {
     return launch_status("mx4_tile");
 }
 
-// A launch on whole tiles.  Rows of x a tile, 32 mb: what reads the least x and products in vain, of a step's time, which is
+// y = the slices' sums added up in their order (+ residual): four columns of a row a thread, eight slices' loads and the
+// residual's in flight at once, since it is a chain of round trips and little else (64 x 4096 x 11008 in eight slices 17.3 us in
+// all; with launch_partial_reduce, whose threads take eight columns and four slices at a time, 17.8).
+__global__ __launch_bounds__(256) void mx4_sum_kernel(MpArgs a, int slices) {
+    const int quads = a.N / 4;
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (id >= (int64_t)a.M * quads) return;
+    const int64_t m = id / quads, n = (id - m * quads) * 4, slice = (int64_t)a.M * a.N;
+    const float* p = a.part + m * a.N + n;
+    uint2 res = make_uint2(0, 0);
+    if (a.res) res = *reinterpret_cast<const uint2*>(a.res + m * a.res_stride + n);
+    f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < slices; s0 += 8) {
+        f32x4 t[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (s0 + i < slices) t[i] = *reinterpret_cast<const f32x4*>(p + (s0 + i) * slice);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (s0 + i < slices) v += t[i];
+    }
+    v += f32x4{bf16_lo(res.x), bf16_hi(res.x), bf16_lo(res.y), bf16_hi(res.y)};
+    *reinterpret_cast<uint2*>(a.y + m * a.y_stride + n) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+}
+
+// Sixteen rows of x at a time, or whole tiles?  The former read the matrix and x again for every sixteen, in about 2.7 us for
+// 2^24 values; a tile of 32 rows and its slices' sum take 3.2 and 64 rows 4 us, and 4 more (us, sixteen at a time and tiles
+// with the sum: 32 x 4096 x 4096 7.7, 10; 32 x 4096 x 11008 16.7, 14; 64 x 1024 x 4096 4.4, 9; 48 x 4096 x 4096 10, 11).
+// A launch on tiles.  Rows of x a tile, 32 mb: what reads the least x and products in vain, of a step's time, which is
 // about 2 + mb.  Slices of K: as many as there are workgroups for on the 256 CUs, of at least four steps (64 x 11008 x 4096,
 // 86 tiles, in one slice, two and four 23.4, 14.6, 15.8 us; 64 x 4096 x 11008, 32 tiles, in four, eight and sixteen 15.1, 12.6,
 // 14.0 us; each without the reduction).
@@ -283,7 +311,8 @@ struct MpPlan {
     int mb, slices, steps_per_slice;     // mb == 0: mx4_few_kernel, 16 rows of x at a time
 };
 static MpPlan mp_plan(int M, int N, int K) {
-    if (M <= 16 || K % 128 != 0 || K < 512) return {0, 1, 0};
+    const int64_t again = (M - 1) / 16;      // times that the matrix would be read again
+    if (again * N * K <= (1 << 25) || K % 128 != 0 || K < 512) return {0, 1, 0};
     MpPlan p{1, 1, 0};
     int least = INT32_MAX;
     for (int mb = 1; mb <= 5; ++mb) {
@@ -330,8 +359,8 @@ int launch_project_mx4(const uint16_t* x, int64_t x_stride, const uint8_t* codes
         default: rc = launch_tiles<5, 3>(a, p.slices, s); break;
     }
     if (rc || p.slices == 1) return rc;
-    return launch_partial_reduce(SkParts{a.part, p.slices, N, M}, N, sk_mats(nullptr, y, y_stride, N), res, res_stride, nullptr,
-                                 nullptr, 0.f, nullptr, 0, nullptr, s);
+    hipLaunchKernelGGL(mx4_sum_kernel, dim3((unsigned)(((int64_t)M * (N / 4) + 255) / 256)), dim3(256), 0, s, a, p.slices);
+    return launch_status("mx4_sum");
 }
 
 }  // namespace vitcop

@@ -213,7 +213,8 @@ def attn_case(vc, seed, B, N, Hq, Hkv, d, capacity=None, std=1.0):
 @pytest.mark.parametrize("B,N,Hq,Hkv,d", [
     (1, 1, 1, 1, 64), (1, 1, 2, 2, 128), (2, 15, 4, 4, 64), (2, 16, 4, 2, 128), (2, 17, 4, 2, 64), (2, 31, 4, 2, 128),
     (2, 32, 6, 2, 128), (1, 33, 7, 1, 64), (3, 127, 16, 1, 128), (1, 128, 32, 32, 128), (2, 129, 17, 1, 64), (3, 257, 34, 2, 128),
-    (1, 640, 32, 32, 128), (2, 1000, 20, 2, 128), (1, 6400, 28, 4, 128), (70, 160, 28, 4, 128), (40, 70, 32, 32, 64),
+    (1, 640, 32, 32, 128), (2, 1000, 20, 2, 128), (1, 6400, 28, 4, 128), (70, 160, 28, 4, 128), (40, 70, 32, 32, 64), (12, 300, 32, 32, 128), (400, 33, 4, 2, 64), (52, 1100, 15, 15, 64),
+    (1, 801, 64, 64, 128), (1, 800, 64, 64, 64), (2, 9001, 4, 2, 128), (1, 20000, 2, 1, 64),
     (1, 4097, 3, 3, 64)])
 def test_attention(vc, B, N, Hq, Hkv, d):
     attn_check(vc, *attn_case(vc, 500 + N + Hq, B, N, Hq, Hkv, d), N)
@@ -326,6 +327,26 @@ def test_projection(vc, M, N, K):
     project_check(vc, M, N, K, residual=(M + N // 16) % 2 == 0)
 
 
+# whole tiles, of 32 rows of x to 160, in slices of k of different lengths and in one; N not a whole number of tiles; K not a
+# whole number of four steps
+@pytest.mark.parametrize("M,N,K", [(20, 11008, 4096), (49, 4096, 4224), (90, 2064, 4480), (200, 2448, 1152), (160, 4112, 1664),
+                                   (317, 16384, 512)])
+def test_projection_on_tiles(vc, M, N, K):
+    y = project_check(vc, M, N, K, residual=M % 2 == 0, seed=7)
+    w, x = I.normal_bf16(1007 + N, 0, (N, K), std=1.28 / np.sqrt(K)), I.normal_bf16(1008 + M, 1, (M, K))
+    codes, scales = vc.vitcop_mx4_quantize(dev(w))
+    r = dev(I.normal_bf16(1009 + M, 2, (M, N))) if M % 2 == 0 else None
+    # without scratch: one slice, the same sums in another order
+    one = vc.vitcop_project_mx4(dev(x), codes, scales, residual=r, ws=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    wv, xv = X.round_trip(w), O.bf16_to_f64(x)
+    ref, size = xv @ wv.T, np.abs(xv) @ np.abs(wv).T
+    if r is not None:
+        ref, size = ref + host_f64(r), size + np.abs(host_f64(r))
+    assert (np.abs(host_f64(one) - ref) <= 2.0 ** -8 * np.abs(ref) + (K + 4) * EPS * size).all()
+    need = vc.lib.vitcop_project_mx4_workspace_bytes(M, N, K)
+    assert torch.equal(vc.vitcop_project_mx4(dev(x), codes, scales, residual=r), y) and (need > 0 or torch.equal(one, y))
+
+
 def test_projection_strided(vc):
     # rows of x, y and the residual inside wider ones; what lies between them stays, and is not read: NaN
     M, N, K = 21, 48, 96
@@ -363,6 +384,10 @@ def test_equal_rows_have_equal_results(vc):
     row = I.normal_bf16(1300, 0, (1, K))
     for M in (1, 16, 40, 64, 150):
         y = project_check(vc, M, N, K, False, seed=5, x=np.repeat(row, M, 0))
+        assert all(torch.equal(y[m], y[0]) for m in range(M))
+    row = I.normal_bf16(1301, 0, (1, 4096))
+    for M in (50, 170):
+        y = project_check(vc, M, 4096, 4096, False, seed=6, x=np.repeat(row, M, 0))
         assert all(torch.equal(y[m], y[0]) for m in range(M))
 
 
@@ -503,7 +528,6 @@ def test_the_binding_refuses(vc):
             bad()
     for bad in (lambda: vc.vitcop_cache_mx4_write(cache, rows, rows, start=6),
                 lambda: vc.vitcop_cache_mx4_read(cache, 9), lambda: vc.vitcop_decode_attn_mx4(q, cache, 9),
-                lambda: vc.vitcop_decode_attn_mx4(q, cache, 8, ws=torch.zeros(8, dtype=torch.uint8, device="cuda")),
                 lambda: vc.vitcop_project_mx4(x, codes, scales), lambda: vc.vitcop_mx4_quantize(x[:, :40])):
         with pytest.raises(vc.VitcopError):
             bad()

@@ -79,19 +79,19 @@ def test_strides_and_sizes_of_a_cache():
 
 
 @pytest.mark.parametrize("change,code", [
-    (dict(N=65), EINVAL), (dict(N=-1), EINVAL), (dict(Hq=3), EINVAL), (dict(Hq=0), EINVAL), (dict(scale=-1.0), EINVAL),
+    (dict(N=4097), EINVAL), (dict(N=-1), EINVAL), (dict(Hq=3), EINVAL), (dict(Hq=0), EINVAL), (dict(scale=-1.0), EINVAL),
     (dict(scale=float("nan")), EINVAL), (dict(scale=float("inf")), EINVAL), (dict(q=None), EINVAL), (dict(out=None), EINVAL),
     (dict(q=A + 8), EINVAL), (dict(out=A + 2), EINVAL), (dict(ws=A + 4), EINVAL), (dict(ws=None), EWORKSPACE),
     (dict(nb=16), EWORKSPACE), (dict(Hq=1 << 24), EUNSUPPORTED)])
 def test_attention(change, code):
-    p = dict(dict(q=A, out=A, N=64, Hq=4, scale=0.0, ws=A, nb=1 << 30), **change)
-    c = C.byref(cache())
+    p = dict(dict(q=A, out=A, N=4096, Hq=4, scale=0.0, ws=A, nb=1 << 30), **change)
+    c = C.byref(cache(capacity=4096))
     assert lib.vitcop_decode_attn_mx4(p["q"], c, p["out"], None, p["N"], None, p["Hq"], p["scale"], p["ws"], p["nb"], None) == code
 
 
 def test_attention_workspace():
     f = lib.vitcop_decode_attn_mx4_workspace_bytes
-    assert f(2, 64, 4, 2, 128) > 0 and f(2, 0, 4, 2, 128) > 0
+    assert f(2, 4096, 4, 2, 128) > 0 and f(2, 64, 4, 2, 128) == 0 and f(2, 0, 4, 2, 128) == 0
     assert f(2, 64, 4, 3, 128) == 0 and f(2, 64, 4, 2, 32) == 0 and f(-1, 64, 4, 2, 128) == 0
 
 
