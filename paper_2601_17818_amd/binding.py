@@ -783,18 +783,19 @@ def vitcop_schedule_prefill(x, weights, Hq, Hkv, d, vis_start, n_vis, schedule):
 # ----------------------------------------------------------------- a KV cache and weights in 4 bits
 
 MX4_GROUP = 32
+_BF16 = (torch.bfloat16, torch.int16, torch.uint16)              # (bit patterns)
 
 
 def _expect(t, name: str, shape, dtype, device) -> None:
-    """A contiguous tensor of this shape and type on this device (dtype None: any 16-bit type)."""
+    """A contiguous tensor of this shape and type on this device (dtype None: bf16 or its bit patterns)."""
     if t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous():
         return
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, not on {device}")
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must be {tuple(shape)}, not {tuple(t.shape)}")
-    if t.dtype != dtype if dtype is not None else t.element_size() != 2:
-        raise ValueError(f"{name} must be {dtype if dtype is not None else 'a 16-bit (bf16) tensor'}, not {t.dtype}")
+    if t.dtype not in ((dtype,) if dtype is not None else _BF16):
+        raise ValueError(f"{name} must be {dtype if dtype is not None else 'bf16'}, not {t.dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
 
@@ -810,10 +811,10 @@ def _here(t, name: str) -> torch.device:
 
 
 def _rows_of(t, name: str):
-    """(M, K, row stride) of a 16-bit matrix whose rows are contiguous."""
+    """(M, K, row stride) of a bf16 matrix whose rows are contiguous."""
     shape, strides = t.shape, t.stride()
-    if len(shape) != 2 or t.element_size() != 2:
-        raise ValueError(f"{name} must be a 16-bit (bf16) matrix")
+    if len(shape) != 2 or t.dtype not in _BF16:
+        raise ValueError(f"{name} must be a bf16 matrix")
     M, K = shape
     if K > 1 and strides[1] != 1:
         raise ValueError(f"{name} must have contiguous rows")
@@ -838,6 +839,8 @@ def vitcop_mx4_quantize(x, out=None):
 def vitcop_mx4_dequantize(codes, scales, out=None):
     """(codes [M,K/2], scales [M,K/32]) uint8 -> [M,K] bf16 (exact); ``out`` reuses a buffer (rows may be strided)."""
     dev = _here(codes, "codes")
+    if codes.dim() != 2:
+        raise ValueError("codes must be [M,K/2]")
     M, K = codes.shape[0], codes.shape[1] * 2
     _expect(codes, "codes", (M, K // 2), torch.uint8, dev)
     _expect(scales, "scales", (M, K // MX4_GROUP), torch.uint8, dev)
@@ -884,8 +887,8 @@ class CacheMx4:
 def _cache_rows(cache: CacheMx4, t, name: str):
     """(T, row stride, batch stride) of K or V rows [B,T,Hkv,d] whose heads lie side by side."""
     shape = t.shape
-    if t.device != cache.device or t.element_size() != 2 or len(shape) != 4:
-        raise ValueError(f"{name} must be a 16-bit [B,T,Hkv,d] tensor on {cache.device}")
+    if t.device != cache.device or t.dtype not in _BF16 or len(shape) != 4:
+        raise ValueError(f"{name} must be a bf16 [B,T,Hkv,d] tensor on {cache.device}")
     T = shape[1]
     if shape != (cache.B, T, cache.Hkv, cache.d):
         raise ValueError(f"{name} must be {(cache.B, T, cache.Hkv, cache.d)}, not {tuple(shape)}")
@@ -967,7 +970,7 @@ def vitcop_project_mx4(x, codes, scales, residual=None, out=None, ws=None):
     workspace (one that is too small for slices of K is not used)."""
     dev = _here(x, "x")
     M, K, x_stride = _rows_of(x, "x")
-    N = codes.shape[0]
+    N = codes.shape[0] if codes.dim() == 2 else 0
     _expect(codes, "codes", (N, K // 2), torch.uint8, dev)
     _expect(scales, "scales", (N, K // MX4_GROUP), torch.uint8, dev)
     y_stride = res_stride = N

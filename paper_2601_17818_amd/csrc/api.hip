@@ -1364,7 +1364,7 @@ static int check_cache_mx4_rows(const char* what, const vitcop_cache_mx4_t* C, c
     REQUIRE(T >= 0, VITCOP_EINVAL, "%s: T=%d", what, T);
     REQUIRE(start_samples || (start >= 0 && (int64_t)start + T <= C->capacity), VITCOP_EINVAL,
             "%s: rows [%d,%lld) outside [0,%d)", what, start, (long long)start + T, C->capacity);
-    REQUIRE((int64_t)C->B * C->Hkv * (T / 32 + 1) < ((int64_t)1 << 26), VITCOP_EUNSUPPORTED, "%s: B*Hkv*(T/32+1) of 2^26 and more",
+    REQUIRE((int64_t)C->B * C->Hkv * (T / 8 + 1) < ((int64_t)1 << 26), VITCOP_EUNSUPPORTED, "%s: B*Hkv*(T/8+1) of 2^26 and more",
             what);
     if (C->B == 0 || T == 0) return VITCOP_OK;
     REQUIRE(k || v, VITCOP_EINVAL, "%s: k and v are both null", what);

@@ -1,6 +1,8 @@
 // Rows of bf16 to 4 bits and back (format: mx4_device.h), as matrices (weights) and as the rows of a KV cache.  Single
 // passes: 2 bytes a value on one side, 17/32 on the other, and a few instructions for eight values, so HBM-bound.
-// Eight values to a thread, 16 bytes of bf16 and one dword of codes: a group is a quad of lanes.
+// Eight values to a thread, 16 bytes of bf16 and one dword of codes: a group is a quad of lanes.  The bf16 side, read or written
+// once, goes past the caches: with rows from HBM a cache of 4 x 2944 x 32 x 128 (244 MB with its bf16 rows, K and V inside QKV rows)
+// to 4 bits 42.8 us, 5.7 TB/s, through the caches 46.6; back 34.7, through them 45; a matrix of 11776 x 4096 20.8 and 17.9 us.
 #include "vitcop_internal.h"
 #include "mx4_device.h"
 
@@ -8,7 +10,7 @@
 
 namespace vitcop {
 
-constexpr int MX_THREADS = 256, MX_UNROLL = 4;
+constexpr int MX_THREADS = 256, MX_UNROLL = 2;
 
 // Units of eight values, `per_row` to a row of the bf16 side (rows `stride` elements apart); the 4-bit side is dense.
 template <bool QUANTIZE>
@@ -45,7 +47,7 @@ __global__ __launch_bounds__(MX_THREADS) void mx4_rows_kernel(const uint16_t* __
 #pragma unroll
         for (int i = 0; i < MX_UNROLL; ++i) {
             const uint32_t u = first + i * MX_THREADS;
-            if (u < units) *reinterpret_cast<u32x4*>(y + at(u)) = mx4_values(c[i], mx4_scale(e[i]));
+            if (u < units) __builtin_nontemporal_store(mx4_values(c[i], mx4_scale(e[i])), reinterpret_cast<u32x4*>(y + at(u)));
         }
     }
 }
@@ -73,7 +75,7 @@ int launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int M, in
 // Rows of a cache.  The bf16 side is token-major, the cache head-major (an attention wavefront reads one head's rows one
 // after the other), so a wavefront takes one head's rows of consecutive tokens: MC_ROWS loads of 16 bytes a lane in flight,
 // pieces of a head's row (2 d bytes) on one side, one contiguous run on the other.
-constexpr int MC_THREADS = 256, MC_ROWS = 8;
+constexpr int MC_THREADS = 256, MC_ROWS = 2;
 
 struct Mx4Side {                         // K or V
     const uint16_t* x;                   // rows to write, or
@@ -135,8 +137,8 @@ __global__ __launch_bounds__(MC_THREADS) void mx4_cache_kernel(Mx4Rows a) {
         for (int i = 0; i < MC_ROWS; ++i) {
             const int t = t0 + i * RPL;
             if (t < a.T)
-                *reinterpret_cast<u32x4*>(side.y + (((int64_t)b * a.T + t) * a.Hkv + h) * D + 8 * c) =
-                    mx4_values(w[i], mx4_scale(e[i]));
+                __builtin_nontemporal_store(mx4_values(w[i], mx4_scale(e[i])),
+                                            reinterpret_cast<u32x4*>(side.y + (((int64_t)b * a.T + t) * a.Hkv + h) * D + 8 * c));
         }
     }
 }

@@ -141,11 +141,12 @@ static int launch_few(const MpArgs& a, hipStream_t s) {
 }
 
 // More rows: eight wavefronts, MT_WM by MT_WN, take 32 MB rows of x and 128 rows of W over a slice of K, 128 columns at a time,
-// both operands through a ring of NS steps in LDS that all of them read.  A step costs the reads from LDS, 8 (MB + .5) 2 KB at
-// 128 bytes a cycle, and then its 4 MB 2 products a wavefront, one after the other in all (reading a step ahead into
-// registers gained nothing: 64 x 4096 x 11008 12.7, 13.3 us).  K >= 512 and whole steps.  Slices' sums are added up by
-// mx4_sum_kernel.  Measured without it, us: 32 x 4096 x 11008 10.2, 64 x 4096 x 11008 12.6, 64 x 11008 x 4096 14.7,
-// 317 x 3584 x 14336 39.6; four wavefronts with twice the columns each 10.4, 14.2, 16.4, 48.5.
+// both operands through a ring of NS steps in LDS that all of them read.  A step moves 8 (MB 4 + 2) KB from LDS and MB 8 + 8 KB
+// into it at 128 bytes a cycle (MB = 5: 1750 cycles) and multiplies 8 MB times a wavefront (1280 cycles a SIMD); without loads
+// from memory it takes 2250, with them some 3000.  Reading a step ahead into registers, between the products, gains nothing
+// (64 x 4096 x 11008 13.4, 14.0 us; 317 x 3584 x 14336 43.1, 42.8), nor do four wavefronts with twice the columns each and fewer
+// reads (14.3, 48.1), nor different starts in k (13.6, 48).  K >= 512 and whole steps.  The slices' sums are added up by mx4_sum_kernel.
+// Measured without it, us: 32 x 4096 x 11008 10.4, 64 x 4096 x 11008 13.4, 64 x 11008 x 4096 15.8, 317 x 3584 x 14336 43.1 (0.76 PFLOP/s).
 constexpr int MT_WM = 2, MT_WN = 4, MT_RT = 2, MT_WAVES = MT_WM * MT_WN, MT_BN = 16 * MT_RT * MT_WN;
 constexpr int MT_EXPS = MT_BN * 16;                  // bytes of four steps' exponents: a unit
 template <int MB, int NS>
