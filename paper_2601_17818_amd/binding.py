@@ -786,12 +786,12 @@ MX4_GROUP = 32
 _BF16 = (torch.bfloat16, torch.int16, torch.uint16)              # (bit patterns)
 
 
-def _expect(t, name: str, shape, dtype, device) -> None:
+def _expect(t, name: str, shape, dtype, device: int) -> None:
     """A contiguous tensor of this shape and type on this device (dtype None: bf16 or its bit patterns)."""
-    if t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous():
+    if t.dtype is (dtype or torch.bfloat16) and t.shape == shape and t.get_device() == device and t.is_contiguous():
         return
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, not on cuda:{device}")
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must be {tuple(shape)}, not {tuple(t.shape)}")
     if t.dtype not in ((dtype,) if dtype is not None else _BF16):
@@ -800,14 +800,20 @@ def _expect(t, name: str, shape, dtype, device) -> None:
         raise ValueError(f"{name} must be contiguous")
 
 
-def _here(t, name: str) -> torch.device:
+def _here(t, name: str) -> int:
     """The tensor's device, which has to be the current one: that is whose stream the call goes to."""
-    if not t.is_cuda:
+    device = t.get_device()
+    if device < 0:
         raise ValueError(f"{name} must be a CUDA tensor")
     current = _current_device() if _current_device is not None else torch.cuda.current_device()
-    if t.get_device() != current:
+    if device != current:
         raise ValueError(f"{name} is on {t.device}, the current device is {current}")
-    return t.device
+    return device
+
+
+def _stream_of(device: int) -> int:
+    """The current stream of the current device, on which a tensor lies."""
+    return _current_raw_stream(device) if _current_raw_stream is not None else _stream()
 
 
 def _rows_of(t, name: str):
@@ -826,13 +832,13 @@ def vitcop_mx4_quantize(x, out=None):
     dev = _here(x, "x")
     M, K, stride = _rows_of(x, "x")
     if out is None:
-        codes = torch.empty((M, K // 2), dtype=torch.uint8, device=dev)
-        scales = torch.empty((M, K // MX4_GROUP), dtype=torch.uint8, device=dev)
+        codes = torch.empty((M, K // 2), dtype=torch.uint8, device=x.device)
+        scales = torch.empty((M, K // MX4_GROUP), dtype=torch.uint8, device=x.device)
     else:
         codes, scales = out
         _expect(codes, "codes", (M, K // 2), torch.uint8, dev)
         _expect(scales, "scales", (M, K // MX4_GROUP), torch.uint8, dev)
-    _check(lib.vitcop_mx4_quantize(x.data_ptr(), stride, M, K, codes.data_ptr(), scales.data_ptr(), _stream()))
+    _check(lib.vitcop_mx4_quantize(x.data_ptr(), stride, M, K, codes.data_ptr(), scales.data_ptr(), _stream_of(dev)))
     return codes, scales
 
 
@@ -846,12 +852,12 @@ def vitcop_mx4_dequantize(codes, scales, out=None):
     _expect(scales, "scales", (M, K // MX4_GROUP), torch.uint8, dev)
     stride = K
     if out is None:
-        out = torch.empty((M, K), dtype=torch.bfloat16, device=dev)
-    elif out.device != dev or out.shape != (M, K):
-        raise ValueError(f"out must be {(M, K)} on {dev}")
+        out = torch.empty((M, K), dtype=torch.bfloat16, device=codes.device)
+    elif out.get_device() != dev or out.shape != (M, K):
+        raise ValueError(f"out must be {(M, K)} on cuda:{dev}")
     else:
         stride = _rows_of(out, "out")[2]
-    _check(lib.vitcop_mx4_dequantize(codes.data_ptr(), scales.data_ptr(), M, K, out.data_ptr(), stride, _stream()))
+    _check(lib.vitcop_mx4_dequantize(codes.data_ptr(), scales.data_ptr(), M, K, out.data_ptr(), stride, _stream_of(dev)))
     return out
 
 
@@ -887,8 +893,8 @@ class CacheMx4:
 def _cache_rows(cache: CacheMx4, t, name: str):
     """(T, row stride, batch stride) of K or V rows [B,T,Hkv,d] whose heads lie side by side."""
     shape = t.shape
-    if t.device != cache.device or t.dtype not in _BF16 or len(shape) != 4:
-        raise ValueError(f"{name} must be a bf16 [B,T,Hkv,d] tensor on {cache.device}")
+    if t.get_device() != cache.device or t.dtype not in _BF16 or len(shape) != 4:
+        raise ValueError(f"{name} must be a bf16 [B,T,Hkv,d] tensor on cuda:{cache.device}")
     T = shape[1]
     if shape != (cache.B, T, cache.Hkv, cache.d):
         raise ValueError(f"{name} must be {(cache.B, T, cache.Hkv, cache.d)}, not {tuple(shape)}")
@@ -903,7 +909,7 @@ def vitcop_cache_mx4_write(cache: CacheMx4, k, v, start: int = 0, start_samples=
     """Rows of k, v [B,T,Hkv,d] (either may be None) to rows start + t of the cache, or start_samples[b] + t (int32 [B]);
     with n_samples (int32 [B]) the first n_samples[b] rows of sample b only.  A token's heads lie side by side; tokens and
     samples may be strided (views of fused QKV rows)."""
-    _here(cache.k_codes, "the cache")
+    dev = _here(cache.k_codes, "the cache")
     k_rows = _cache_rows(cache, k, "k") if k is not None else None
     v_rows = _cache_rows(cache, v, "v") if v is not None else k_rows
     if k_rows is not None and k_rows != v_rows:
@@ -915,24 +921,24 @@ def vitcop_cache_mx4_write(cache: CacheMx4, k, v, start: int = 0, start_samples=
     T, row, batch = v_rows if v_rows is not None else (0, 0, 0)
     _check(lib.vitcop_cache_mx4_write(cache.desc, _ptr(k), _ptr(v), row, batch, T, start,
                                       cache.per_sample(start_samples, "start_samples"),
-                                      cache.per_sample(n_samples, "n_samples"), _stream()))
+                                      cache.per_sample(n_samples, "n_samples"), _stream_of(dev)))
 
 
 def vitcop_cache_mx4_read(cache: CacheMx4, T: int, start: int = 0, start_samples=None, out=None):
     """Rows [start, start + T) of every sample, or T rows from start_samples[b] (int32 [B]) on, as (k, v) [B,T,Hkv,d]
     bf16; ``out`` = (k, v) reuses buffers, of which one may be None."""
-    _here(cache.k_codes, "the cache")
+    dev = _here(cache.k_codes, "the cache")
     shape = (cache.B, T, cache.Hkv, cache.d)
     if out is None:
         if T < 0:
             raise ValueError("T must not be negative")
-        out = tuple(torch.empty(shape, dtype=torch.bfloat16, device=cache.device) for _ in range(2))
+        out = tuple(torch.empty(shape, dtype=torch.bfloat16, device=cache.k_codes.device) for _ in range(2))
     k, v = out
     for t, name in ((k, "k"), (v, "v")):
         if t is not None:
             _expect(t, name, shape, None, cache.device)
     _check(lib.vitcop_cache_mx4_read(cache.desc, _ptr(k), _ptr(v), T, start,
-                                     cache.per_sample(start_samples, "start_samples"), _stream()))
+                                     cache.per_sample(start_samples, "start_samples"), _stream_of(dev)))
     return k, v
 
 
@@ -947,7 +953,7 @@ def vitcop_decode_attn_mx4(q, cache: CacheMx4, N: int, n_samples=None, scale: fl
     _expect(q, "q", (cache.B, Hq, cache.d), None, cache.device)
     if out is None:
         o = torch.empty_like(q)
-        lse = torch.empty((cache.B, Hq), dtype=torch.float32, device=dev) if want_lse else None
+        lse = torch.empty((cache.B, Hq), dtype=torch.float32, device=q.device) if want_lse else None
     else:
         o, lse = out
         _expect(o, "out", q.shape, None, dev)
@@ -956,11 +962,11 @@ def vitcop_decode_attn_mx4(q, cache: CacheMx4, N: int, n_samples=None, scale: fl
     if ws is None:
         nb = lib.vitcop_decode_attn_mx4_workspace_bytes(cache.B, N, Hq, cache.Hkv, cache.d)
         ws = _ws(nb, q) if nb else None
-    elif ws.device != dev or ws.dtype != torch.uint8:
-        raise ValueError(f"ws must be a uint8 tensor on {dev}")
+    elif ws.get_device() != dev or ws.dtype is not torch.uint8 or not ws.is_contiguous():
+        raise ValueError(f"ws must be a contiguous uint8 tensor on cuda:{dev}")
     _check(lib.vitcop_decode_attn_mx4(q.data_ptr(), cache.desc, o.data_ptr(), _ptr(lse), N,
                                       cache.per_sample(n_samples, "n_samples"), Hq, scale, _ptr(ws),
-                                      ws.numel() if ws is not None else 0, _stream()))
+                                      ws.numel() if ws is not None else 0, _stream_of(dev)))
     return o, lse
 
 
@@ -975,21 +981,21 @@ def vitcop_project_mx4(x, codes, scales, residual=None, out=None, ws=None):
     _expect(scales, "scales", (N, K // MX4_GROUP), torch.uint8, dev)
     y_stride = res_stride = N
     if out is None:
-        out = torch.empty((M, N), dtype=x.dtype, device=dev)
-    elif out.device != dev or out.shape != (M, N):
-        raise ValueError(f"out must be {(M, N)} on {dev}")
+        out = torch.empty((M, N), dtype=x.dtype, device=x.device)
+    elif out.get_device() != dev or out.shape != (M, N):
+        raise ValueError(f"out must be {(M, N)} on cuda:{dev}")
     else:
         y_stride = _rows_of(out, "out")[2]
     if residual is not None:
-        if residual.device != dev or residual.shape != (M, N):
-            raise ValueError(f"residual must be {(M, N)} on {dev}")
+        if residual.get_device() != dev or residual.shape != (M, N):
+            raise ValueError(f"residual must be {(M, N)} on cuda:{dev}")
         res_stride = _rows_of(residual, "residual")[2]
     if ws is None:
         nb = lib.vitcop_project_mx4_workspace_bytes(M, N, K) if M > 16 else 0
         ws = _ws(nb, x) if nb else None
-    elif ws.device != dev or ws.dtype != torch.uint8:
-        raise ValueError(f"ws must be a uint8 tensor on {dev}")
+    elif ws.get_device() != dev or ws.dtype is not torch.uint8 or not ws.is_contiguous():
+        raise ValueError(f"ws must be a contiguous uint8 tensor on cuda:{dev}")
     _check(lib.vitcop_project_mx4(x.data_ptr(), x_stride, codes.data_ptr(), scales.data_ptr(), out.data_ptr(), y_stride,
                                   _ptr(residual), res_stride, M, N, K, _ptr(ws), ws.numel() if ws is not None else 0,
-                                  _stream()))
+                                  _stream_of(dev)))
     return out
