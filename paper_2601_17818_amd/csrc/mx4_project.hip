@@ -145,14 +145,14 @@ static int launch_few(const MpArgs& a, hipStream_t s) {
 // into it at 128 bytes a cycle (MB = 5: 1750 cycles) and multiplies 8 MB times a wavefront (1280 cycles a SIMD); without loads
 // from memory it takes 2250, with them some 3000.  Reading a step ahead into registers, between the products, gains nothing
 // (64 x 4096 x 11008 13.4, 14.0 us; 317 x 3584 x 14336 43.1, 42.8), nor do four wavefronts with twice the columns each and fewer
-// reads (14.3, 48.1), nor different starts in k (13.6, 48).  K >= 512 and whole steps.  The slices' sums are added up by mx4_sum_kernel.
+// reads (14.3, 48.1), nor different starts in k (13.6, 48).  K >= 512; WHOLE: whole steps.  The slices' sums are added up by mx4_sum_kernel.
 // Measured without it, us: 32 x 4096 x 11008 10.4, 64 x 4096 x 11008 13.4, 64 x 11008 x 4096 15.8, 317 x 3584 x 14336 43.1 (0.76 PFLOP/s).
 constexpr int MT_WM = 2, MT_WN = 4, MT_RT = 2, MT_WAVES = MT_WM * MT_WN, MT_BN = 16 * MT_RT * MT_WN;
-constexpr int MT_EXPS = MT_BN * 16;                  // bytes of four steps' exponents: a unit
+constexpr int MT_EXPS = MT_BN * 16;                  // bytes of a unit of exponents
 template <int MB, int NS>
 constexpr int mp_tile_bytes() { return NS * (16 * MB * MT_WM * 256 + MT_BN * 64) + 3 * MT_EXPS; }
 
-template <int MB, int NS>
+template <int MB, int NS, bool WHOLE>
 __global__ __launch_bounds__(64 * MT_WAVES) void mx4_tile_kernel(MpArgs a) {
     constexpr int BM = 16 * MB * MT_WM, BN = MT_BN, RT = MT_RT;
     constexpr int XL = BM / (4 * MT_WAVES), NL = XL + 1, SLOT = BM * 256 + BN * 64;        // loads of x, of x and codes a wavefront and step
@@ -165,32 +165,42 @@ __global__ __launch_bounds__(64 * MT_WAVES) void mx4_tile_kernel(MpArgs a) {
     const int n0 = ((nth / tiles_m) * 8 + (blockIdx.x & 7)) * BN, m0 = nth % tiles_m * BM;
     if (n0 >= a.N) return;
     const int groups = a.K / MX4_GROUP;
-    const int first = blockIdx.y * a.steps_per_slice, end = min(groups / 4, first + a.steps_per_slice);
+    const int first = blockIdx.y * a.steps_per_slice, end = min((groups + 3) / 4, first + a.steps_per_slice);
     const int rows = min(BN, a.N - n0);
     const auto c_desc = mp_desc(a.codes + (int64_t)n0 * (a.K / 2), (int64_t)rows * (a.K / 2));
-    const auto s_desc = mp_desc(a.scales + (int64_t)n0 * groups, (int64_t)rows * groups);
+    const int s_bytes = (rows * groups + 3) & ~3;            // (whole words)
+    const auto s_desc = mp_desc(a.scales + (int64_t)n0 * groups, s_bytes);
     const auto x_desc = mp_desc(a.x + m0 * a.x_stride, ((a.M - m0 - 1) * a.x_stride + a.K) * 2);
-    const unsigned c_off = (unsigned)(16 * wv + lane / 4) * (unsigned)(a.K / 2) + 16 * (lane % 4 ^ (lane >> 4));
+    const int c_grp = lane % 4 ^ (lane >> 4);
+    const unsigned c_off = (unsigned)(16 * wv + lane / 4) * (unsigned)(a.K / 2) + 16 * c_grp;
     unsigned x_off[XL];
+    int x_grp[XL];
 #pragma unroll
     for (int q = 0; q < XL; ++q) {
-        const int row = 4 * (XL * wv + q) + lane / 16;
-        x_off[q] = m0 + row < a.M ? (unsigned)(row * a.x_stride * 2) + 16 * (lane % 16 ^ (row & 15)) : MP_OUTSIDE;
+        const int row = 4 * (XL * wv + q) + lane / 16, piece = lane % 16 ^ (row & 15);
+        x_grp[q] = piece >> 2;
+        x_off[q] = m0 + row < a.M ? (unsigned)(row * a.x_stride * 2) + 16 * piece : MP_OUTSIDE;
     }
     auto load = [&](int slot, int step) __attribute__((always_inline)) {
         char* const to = mp_lds + slot * SLOT;
-        const unsigned past = step < end ? 0u : MP_OUTSIDE;
-        mp_load(c_desc, to + BM * 256 + wv * 1024, (c_off + 64 * step) | past);
+        auto past = [&](int grp) __attribute__((always_inline)) {
+            return step < end && (WHOLE || 4 * step + grp < groups) ? 0u : MP_OUTSIDE;
+        };
+        mp_load(c_desc, to + BM * 256 + wv * 1024, (c_off + 64 * step) | past(c_grp));
 #pragma unroll
-        for (int q = 0; q < XL; ++q) mp_load(x_desc, to + (XL * wv + q) * 1024, (x_off[q] + 256 * step) | past);
+        for (int q = 0; q < XL; ++q) mp_load(x_desc, to + (XL * wv + q) * 1024, (x_off[q] + 256 * step) | past(x_grp[q]));
     };
-    // Exponents come in units, 16 bytes of a row a lane: four steps (a row's last unit ends with it).  Two are asked for here, and
-    // during a unit's steps a quarter each of the one after the next.
+    // Exponents come in units, 16 bytes of a row a lane: those of four steps, a row's last unit ending with it, or where rows do not
+    // start at whole words of three, from the word on that holds the first.  Two are asked for here, and with every step of a
+    // unit some rows of the one after the next.
+    constexpr int UNIT = WHOLE ? 4 : 3, ROWS = WHOLE ? BN / 4 / MT_WAVES : 6;                // steps; rows a wavefront and step
+    static_assert(MT_EXPS == 2048 && MT_WAVES >= 4 && ROWS * MT_WAVES * UNIT >= BN, "two loads a unit");
     char* const scales = mp_lds + NS * SLOT;
-    auto unit_at = [&](int unit) __attribute__((always_inline)) { return min(4 * first + 16 * unit, groups - 16); };
-    static_assert(MT_EXPS == 2048 && MT_WAVES >= 4, "two loads a unit");
-    if (wv < 4)
-        mp_load(s_desc, scales + wv * 1024, (unsigned)(wv % 2 * 64 + lane) * (unsigned)groups + unit_at(wv / 2));
+    auto unit_at = [&](int row, int unit) __attribute__((always_inline)) {
+        return WHOLE ? row * groups + min(4 * first + 16 * unit, groups - 16)
+                     : min((row * groups + 4 * first + 12 * unit) & ~3, s_bytes - 16);
+    };
+    if (wv < 4) mp_load(s_desc, scales + wv * 1024, (unsigned)unit_at(wv % 2 * 64 + lane, wv / 2));
     f32x4 acc[RT][MB];
 #pragma unroll
     for (int r = 0; r < RT; ++r)
@@ -198,7 +208,7 @@ __global__ __launch_bounds__(64 * MT_WAVES) void mx4_tile_kernel(MpArgs a) {
         for (int j = 0; j < MB; ++j) acc[r][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < NS - 1; ++i) load(i, first + i);     // (past the last step: nothing is fetched)
-    int slot = 0, ahead = NS - 1, exp_slot = 0;
+    int slot = 0, ahead = NS - 1, unit = 0, exp_slot = 0, phase = 0;
     for (int step = first; step < end; ++step) {
         // everybody's loads for this step are there (at least NL for each later one were issued after them), and everybody has
         // read the slots that are filled next
@@ -206,27 +216,30 @@ __global__ __launch_bounds__(64 * MT_WAVES) void mx4_tile_kernel(MpArgs a) {
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         const char* const from = mp_lds + slot * SLOT;
-        const int unit = (step - first) >> 2, quarter = (step - first) & 3;
-        const char* const exps = scales + exp_slot * MT_EXPS + 4 * step + g4 - unit_at(unit);
+        const char* const exps = scales + exp_slot * MT_EXPS;
+        const int grp = WHOLE ? 4 * step + g4 : min(4 * step + g4, groups - 1);
         u32x4 cc[RT], xx[MB][4];
         uint32_t ee[RT];
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             const int row = 16 * (RT * wn + r) + l16;
             cc[r] = *reinterpret_cast<const u32x4*>(from + BM * 256 + row * 64 + (g4 ^ (l16 >> 2)) * 16);
-            ee[r] = *reinterpret_cast<const uint8_t*>(exps + row * 16);
+            ee[r] = *reinterpret_cast<const uint8_t*>(exps + row * 16 + ((row * groups + grp - unit_at(row, unit)) & 15));
         }
 #pragma unroll
         for (int j = 0; j < MB; ++j)
 #pragma unroll
             for (int c = 0; c < 4; ++c)
                 xx[j][c] = *reinterpret_cast<const u32x4*>(from + (16 * (MB * wm + j) + l16) * 256 + ((4 * g4 + c) ^ l16) * 16);
-        const int e_row = BN / 4 * quarter + BN / 32 * wv;
-        if (lane < BN / 32)
-            mp_load(s_desc, scales + (exp_slot == 0 ? 2 : exp_slot - 1) * MT_EXPS + e_row * 16,
-                    (unsigned)(e_row + lane) * (unsigned)groups + unit_at(unit + 2));
+        const int e_row = ROWS * (MT_WAVES * phase + wv);
+        if (lane < ROWS && e_row + lane < BN)
+            mp_load(s_desc, scales + (exp_slot == 0 ? 2 : exp_slot - 1) * MT_EXPS + e_row * 16, (unsigned)unit_at(e_row + lane, unit + 2));
         load(ahead, step + NS - 1);
-        if (quarter == 3) exp_slot = exp_slot == 2 ? 0 : exp_slot + 1;
+        if (++phase == UNIT) {
+            phase = 0;
+            ++unit;
+            exp_slot = exp_slot == 2 ? 0 : exp_slot + 1;
+        }
 #pragma unroll
         for (int c = 0; c < 4; ++c)
 #pragma unroll
@@ -259,21 +272,26 @@ __global__ __launch_bounds__(64 * MT_WAVES) void mx4_tile_kernel(MpArgs a) {
         }
 }
 
-template <int MB, int NS>
-static int launch_tiles(const MpArgs& a, int slices, hipStream_t s) {
+template <int MB, int NS, bool WHOLE>
+static int launch_tiles_of(const MpArgs& a, int slices, hipStream_t s) {
     const int tiles = ((a.N + MT_BN - 1) / MT_BN + 7) / 8 * 8 * ((a.M + 32 * MB - 1) / (32 * MB));
     constexpr int lds = mp_tile_bytes<MB, NS>();
     static_assert(lds <= 160 * 1024, "LDS of a CU");
     static std::atomic<bool> raised{false};          // (per instantiation; a second thread repeating the call is harmless)
     if (lds > 65536 && !raised.load()) {
-        const int rc = hip_status(hipFuncSetAttribute(reinterpret_cast<const void*>(&mx4_tile_kernel<MB, NS>),
+        const int rc = hip_status(hipFuncSetAttribute(reinterpret_cast<const void*>(&mx4_tile_kernel<MB, NS, WHOLE>),
                                                       hipFuncAttributeMaxDynamicSharedMemorySize, lds),
                                   "hipFuncSetAttribute(mx4_tile)");
         if (rc) return rc;
         raised.store(true);
     }
-    hipLaunchKernelGGL((mx4_tile_kernel<MB, NS>), dim3(tiles, slices), dim3(64 * MT_WAVES), lds, s, a);
+    hipLaunchKernelGGL((mx4_tile_kernel<MB, NS, WHOLE>), dim3(tiles, slices), dim3(64 * MT_WAVES), lds, s, a);
     return launch_status("mx4_tile");
+}
+
+template <int MB, int NS>
+static int launch_tiles(const MpArgs& a, int slices, hipStream_t s) {
+    return a.K % 128 == 0 ? launch_tiles_of<MB, NS, true>(a, slices, s) : launch_tiles_of<MB, NS, false>(a, slices, s);
 }
 
 // y = the slices' sums added up in their order (+ residual): four columns of a row a thread, eight slices' loads and the
@@ -313,7 +331,7 @@ struct MpPlan {
 };
 static MpPlan mp_plan(int M, int N, int K) {
     const int64_t again = (M - 1) / 16;      // times that the matrix would be read again
-    if (again * N * K <= (1 << 25) || K % 128 != 0 || K < 512) return {0, 1, 0};
+    if (again * N * K <= (1 << 25) || K < 512) return {0, 1, 0};
     MpPlan p{1, 1, 0};
     int least = INT32_MAX;
     for (int mb = 1; mb <= 5; ++mb) {
@@ -324,7 +342,7 @@ static MpPlan mp_plan(int M, int N, int K) {
         }
     }
     const int64_t tiles = (int64_t)((N + MT_BN - 1) / MT_BN) * ((M + 32 * p.mb - 1) / (32 * p.mb));
-    const int steps = K / 128;
+    const int steps = (K + 127) / 128;
     p.slices = (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, steps / 4));
     p.steps_per_slice = (steps + p.slices - 1) / p.slices;
     p.slices = (steps + p.steps_per_slice - 1) / p.steps_per_slice;          // (none of them empty)
@@ -349,7 +367,7 @@ int launch_project_mx4(const uint16_t* x, int64_t x_stride, const uint8_t* codes
         return M <= 8 ? launch_few<2, 4, 2>(a, s) : launch_few<4, 4, 3>(a, s);
     }
     if (p.slices > 1 && ws_bytes < project_mx4_workspace_bytes(M, N, K)) p.slices = 1;
-    a.steps_per_slice = p.slices > 1 ? p.steps_per_slice : K / 128;
+    a.steps_per_slice = p.slices > 1 ? p.steps_per_slice : (K + 127) / 128;
     if (p.slices > 1) a.part = static_cast<float*>(ws);
     int rc = 0;
     switch (p.mb) {

@@ -340,9 +340,9 @@ def test_projection(vc, M, N, K):
 
 
 # whole tiles, of 32 rows of x to 160, in slices of k of different lengths and in one; N not a whole number of tiles; K not a
-# whole number of four steps
+# whole number of four steps, and not of one: its rows of exponents start at every byte of a word
 @pytest.mark.parametrize("M,N,K", [(20, 8208, 4352), (49, 4096, 4224), (90, 2064, 4480), (200, 2448, 1152), (160, 4112, 1664),
-                                   (317, 16384, 512)])
+                                   (317, 16384, 512), (130, 4112, 1120), (48, 6160, 2912), (300, 2064, 1184), (70, 3600, 3232)])
 def test_projection_on_tiles(vc, M, N, K):
     project_check(vc, M, N, K, residual=M % 2 == 0, seed=7, one_slice=True)
 
