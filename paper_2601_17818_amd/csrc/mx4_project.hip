@@ -319,34 +319,37 @@ __global__ __launch_bounds__(256) void mx4_sum_kernel(MpArgs a, int slices) {
     *reinterpret_cast<uint2*>(a.y + m * a.y_stride + n) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
 }
 
-// Sixteen rows of x at a time, or whole tiles?  The former read the matrix and x again for every sixteen, in about 2.7 us for
-// 2^24 values; a tile of 32 rows and its slices' sum take 3.2 and 64 rows 4 us, and 4 more (us, sixteen at a time and tiles
-// with the sum: 32 x 4096 x 4096 7.7, 10; 32 x 4096 x 11008 16.7, 14; 64 x 1024 x 4096 4.4, 9; 48 x 4096 x 4096 10, 11).
-// A launch on tiles.  Rows of x a tile, 32 mb: what reads the least x and products in vain, of a step's time, which is
-// about 2 + mb.  Slices of K: as many as there are workgroups for on the 256 CUs, of at least four steps (64 x 11008 x 4096,
-// 86 tiles, in one slice, two and four 23.4, 14.6, 15.8 us; 64 x 4096 x 11008, 32 tiles, in four, eight and sixteen 15.1, 12.6,
-// 14.0 us; each without the reduction).
+// Which launch: sixteen rows of x at a time, or tiles of 32 mb, with k in how many slices.  By estimated time, us, fitted to
+// eighteen sizes of 20 to 512 rows with weights from HBM and within 10 % of each but two:
+//  - sixteen rows at a time: 2.5 and 2.7 for every 2^24 values of the matrix, which is read again for every sixteen;
+//  - tiles: 4 + 0.5 mb for the launch, the first loads and the end, then rounds of 256 workgroups (a CU holds two of mb = 1, a further round costs 0.8) over the
+//    slice's steps; slices cost 3 for the kernel that adds them up and 0.2 a MB.
+// Measured: 48 x 4096 x 4096 sixteen at a time 11.0, tiles 11.3 (mb = 1, four slices), 64 rows 12.5, 11.7; 64 x 4096 x 11008 in eight slices
+// 16.9 (mb = 2), in four 18.1 (mb = 1); 64 x 11008 x 4096 in one 19.2 (mb = 1), in two 20.4 (mb = 2); 200 x 4096 x 4096 in one 19.2
+// (mb = 1), in two 20.4, in four 22.4 (mb = 2); 300 x 4096 x 4096 in four 23.4 (mb = 5), in two 24.4 (mb = 3), in one 24.6 (mb = 2).
 struct MpPlan {
-    int mb, slices, steps_per_slice;     // mb == 0: mx4_few_kernel, 16 rows of x at a time
+    int mb, slices, steps_per_slice;     // mb == 0: mx4_few_kernel
 };
 static MpPlan mp_plan(int M, int N, int K) {
-    const int64_t again = (M - 1) / 16;      // times that the matrix would be read again
-    if (again * N * K <= (1 << 25) || K < 512) return {0, 1, 0};
-    MpPlan p{1, 1, 0};
-    int least = INT32_MAX;
+    constexpr float step_us[6] = {0.f, 0.46f, 0.66f, 0.93f, 1.14f, 1.34f};
+    MpPlan best{0, 1, 0};
+    if (M <= 16 || K < 512) return best;
+    const int steps = (K + 127) / 128;
+    float least = 2.5f + 2.7f * (float)((M + 15) / 16) * ((float)N * (float)K / 16777216.f);
     for (int mb = 1; mb <= 5; ++mb) {
-        const int cost = (M + 32 * mb - 1) / (32 * mb) * (2 + mb);
-        if (cost < least) {
-            least = cost;
-            p.mb = mb;
+        const int64_t tiles = (int64_t)((N + MT_BN - 1) / MT_BN) * ((M + 32 * mb - 1) / (32 * mb));
+        for (int want = 1; want <= 16 && want <= steps / 4; ++want) {
+            const int per = (steps + want - 1) / want, slices = (steps + per - 1) / per;       // (none of them empty)
+            const int64_t rounds = (tiles * slices + 255) / 256;
+            float us = 4.f + 0.5f * mb + (float)rounds * (rounds > 1 && mb == 1 ? 0.84f : 1.f) * per * step_us[mb] + 0.8f * (rounds - 1);
+            if (slices > 1) us += 3.f + 0.8e-6f * slices * (float)M * (float)N;
+            if (us < least) {
+                least = us;
+                best = {mb, slices, per};
+            }
         }
     }
-    const int64_t tiles = (int64_t)((N + MT_BN - 1) / MT_BN) * ((M + 32 * p.mb - 1) / (32 * p.mb));
-    const int steps = (K + 127) / 128;
-    p.slices = (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, steps / 4));
-    p.steps_per_slice = (steps + p.slices - 1) / p.slices;
-    p.slices = (steps + p.steps_per_slice - 1) / p.steps_per_slice;          // (none of them empty)
-    return p;
+    return best;
 }
 
 size_t project_mx4_workspace_bytes(int M, int N, int K) {
@@ -358,7 +361,7 @@ int launch_project_mx4(const uint16_t* x, int64_t x_stride, const uint8_t* codes
                        int64_t y_stride, const uint16_t* res, int64_t res_stride, int M, int N, int K, void* ws,
                        size_t ws_bytes, hipStream_t s) {
     MpArgs a{x, codes, scales, y, res, x_stride, y_stride, res_stride, M, N, K, nullptr, 0};
-    MpPlan p = mp_plan(M, N, K);
+    const MpPlan p = mp_plan(M, N, K);
     if (p.mb == 0) {
         // with more tiles than two for every CU four wavefronts each, which fit side by side (1 x 11008 x 4096 6.4, 7.1 us with
         // eight; 1 x 4096 x 11008 7.1, 6.5); more rows keep more in flight
@@ -366,19 +369,20 @@ int launch_project_mx4(const uint16_t* x, int64_t x_stride, const uint8_t* codes
         if (M <= 4) return many ? launch_few<1, 4, 2>(a, s) : launch_few<1, 8, 3>(a, s);
         return M <= 8 ? launch_few<2, 4, 2>(a, s) : launch_few<4, 4, 3>(a, s);
     }
-    if (p.slices > 1 && ws_bytes < project_mx4_workspace_bytes(M, N, K)) p.slices = 1;
-    a.steps_per_slice = p.slices > 1 ? p.steps_per_slice : (K + 127) / 128;
-    if (p.slices > 1) a.part = static_cast<float*>(ws);
+    const bool cut = p.slices > 1 && ws_bytes >= project_mx4_workspace_bytes(M, N, K);
+    const int slices = cut ? p.slices : 1;
+    a.steps_per_slice = cut ? p.steps_per_slice : (K + 127) / 128;
+    if (cut) a.part = static_cast<float*>(ws);
     int rc = 0;
     switch (p.mb) {
-        case 1: rc = launch_tiles<1, 4>(a, p.slices, s); break;
-        case 2: rc = launch_tiles<2, 4>(a, p.slices, s); break;
-        case 3: rc = launch_tiles<3, 3>(a, p.slices, s); break;
-        case 4: rc = launch_tiles<4, 3>(a, p.slices, s); break;
-        default: rc = launch_tiles<5, 3>(a, p.slices, s); break;
+        case 1: rc = launch_tiles<1, 4>(a, slices, s); break;
+        case 2: rc = launch_tiles<2, 4>(a, slices, s); break;
+        case 3: rc = launch_tiles<3, 3>(a, slices, s); break;
+        case 4: rc = launch_tiles<4, 3>(a, slices, s); break;
+        default: rc = launch_tiles<5, 3>(a, slices, s); break;
     }
-    if (rc || p.slices == 1) return rc;
-    hipLaunchKernelGGL(mx4_sum_kernel, dim3((unsigned)(((int64_t)M * (N / 4) + 255) / 256)), dim3(256), 0, s, a, p.slices);
+    if (rc || !cut) return rc;
+    hipLaunchKernelGGL(mx4_sum_kernel, dim3((unsigned)(((int64_t)M * (N / 4) + 255) / 256)), dim3(256), 0, s, a, slices);
     return launch_status("mx4_sum");
 }
 

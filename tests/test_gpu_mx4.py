@@ -339,10 +339,12 @@ def test_projection(vc, M, N, K):
     project_check(vc, M, N, K, residual=(M + N // 16) % 2 == 0)
 
 
-# whole tiles, of 32 rows of x to 160, in slices of k of different lengths and in one; N not a whole number of tiles; K not a
-# whole number of four steps, and not of one: its rows of exponents start at every byte of a word
-@pytest.mark.parametrize("M,N,K", [(20, 8208, 4352), (49, 4096, 4224), (90, 2064, 4480), (200, 2448, 1152), (160, 4112, 1664),
-                                   (317, 16384, 512), (130, 4112, 1120), (48, 6160, 2912), (300, 2064, 1184), (70, 3600, 3232)])
+# tiles of 32 rows of x to 160 (one, two, three, four, five times 32, as the sizes are listed), in one slice of k and in several, with
+# K a whole number of steps of 128 and not (its rows of exponents then start at every byte of a word), N no whole number of tiles
+@pytest.mark.parametrize("M,N,K", [
+    (317, 2272, 608), (316, 640, 4448), (306, 464, 6784), (323, 608, 5632), (20, 8208, 4352), (294, 3392, 640), (313, 448, 6976),
+    (320, 672, 4864), (328, 6288, 544), (323, 1472, 3168), (284, 1040, 6656), (329, 1424, 6208), (322, 1520, 6144),
+    (297, 2256, 4448), (318, 2304, 4480)])
 def test_projection_on_tiles(vc, M, N, K):
     project_check(vc, M, N, K, residual=M % 2 == 0, seed=7, one_slice=True)
 
