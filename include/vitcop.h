@@ -558,12 +558,13 @@ int vitcop_decode_attn_mx4(const uint16_t* q, const vitcop_cache_mx4_t* C, uint1
                            const int32_t* n_samples, int Hq, float scale, void* ws, size_t ws_bytes, void* stream);
 
 /* vitcop_project with a matrix in 4 bits: y[m,n] = bf16( sum_k x[m,k] * w[n,k] (+ residual[m,n]) ), fp32
- * accumulate, for the few rows of a decoding step and up to the hundreds that survive pruning.
+ * accumulate, for the few rows of a decoding step and up to those that survive pruning.  y may be the residual.
  *   x [M,K] bf16, w_codes [N,K/2], w_scales [N,K/32] (vitcop_mx4_quantize of w [N,K]), y [M,N] bf16;
  *   residual: NULL, or [M,N] bf16; row strides in elements, multiples of 8
  *   ws: NULL, or device scratch of ws_bytes >= vitcop_project_mx4_workspace_bytes(M,N,K) (16-byte aligned, 0 for
  *   at most 16 rows): some more rows leave most of the chip idle unless k is cut into slices, whose fp32 sums live
- *   there and are added in a fixed order; without scratch, or with too little, one slice does it all
+ *   there and are added in a fixed order, and for thousands of rows the matrix goes to bf16 there first; without
+ *   scratch, or with too little, one slice does it all
  * K % 32 == 0, N % 16 == 0, K <= 2^16, M <= 2^19, M*x_row_stride < 2^30, N*K < 2^31. */
 size_t vitcop_project_mx4_workspace_bytes(int M, int N, int K);
 int vitcop_project_mx4(const uint16_t* x, int64_t x_row_stride, const uint8_t* w_codes, const uint8_t* w_scales,

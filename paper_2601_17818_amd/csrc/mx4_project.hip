@@ -1,6 +1,7 @@
 // Projections by a matrix held in 4 bits (format: mx4_device.h): y = x W^T (+ residual), for the few rows of a decoding step's
-// new tokens and up to the rows that survive pruning.  Bound by the matrix' bytes, 17/32 of one a value, until there are some
-// ten rows; then by x, which every workgroup reads, and from some hundred rows on by the matrix cores.
+// new tokens and up to the rows that survive pruning (for thousands, see the choice of the launch below).  Bound by the matrix'
+// bytes, 17/32 of one a value, until there are some ten rows; then by x, which every workgroup reads, and from some hundred
+// rows on by the matrix cores.
 //
 // The codes go to LDS as they are, and only an operand of a product is turned into bf16 (one instruction for two values, the
 // group's power of two included; W's rows are the product's rows, x's rows its columns, 16x16x32).  A lane's 16 bytes of
@@ -145,7 +146,7 @@ static int launch_few(const MpArgs& a, hipStream_t s) {
 // into it at 128 bytes a cycle (MB = 5: 1750 cycles) and multiplies 8 MB times a wavefront (1280 cycles a SIMD); without loads
 // from memory it takes 2250, with them some 3000.  Reading a step ahead into registers, between the products, gains nothing
 // (64 x 4096 x 11008 13.4, 14.0 us; 317 x 3584 x 14336 43.1, 42.8), nor do four wavefronts with twice the columns each and fewer
-// reads (14.3, 48.1), nor different starts in k (13.6, 48).  K >= 512; WHOLE: whole steps.  The slices' sums are added up by mx4_sum_kernel.
+// reads (14.3, 48.1), nor different starts in k (13.6, 48).  K >= 512; WHOLE: whole steps.  The slices' sums are added by mx4_sum_kernel.
 // Measured without it, us: 32 x 4096 x 11008 10.4, 64 x 4096 x 11008 13.4, 64 x 11008 x 4096 15.8, 317 x 3584 x 14336 43.1 (0.76 PFLOP/s).
 constexpr int MT_WM = 2, MT_WN = 4, MT_RT = 2, MT_WAVES = MT_WM * MT_WN, MT_BN = 16 * MT_RT * MT_WN;
 constexpr int MT_EXPS = MT_BN * 16;                  // bytes of a unit of exponents
@@ -319,20 +320,24 @@ __global__ __launch_bounds__(256) void mx4_sum_kernel(MpArgs a, int slices) {
     *reinterpret_cast<uint2*>(a.y + m * a.y_stride + n) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
 }
 
-// Which launch: sixteen rows of x at a time, or tiles of 32 mb, with k in how many slices.  By estimated time, us, fitted to
-// eighteen sizes of 20 to 512 rows with weights from HBM and within 10 % of each but two:
+// Which launch: sixteen rows of x at a time, tiles of 32 mb with k in how many slices, or the matrix to bf16 and the bf16
+// projection.  By estimated time, us, fitted to twenty-odd sizes of 20 to 4096 rows with weights from HBM:
 //  - sixteen rows at a time: 2.5 and 2.7 for every 2^24 values of the matrix, which is read again for every sixteen;
-//  - tiles: 4 + 0.5 mb for the launch, the first loads and the end, then rounds of 256 workgroups (a CU holds two of mb = 1, a further round costs 0.8) over the
-//    slice's steps; slices cost 3 for the kernel that adds them up and 0.2 a MB.
-// Measured: 48 x 4096 x 4096 sixteen at a time 11.0, tiles 11.3 (mb = 1, four slices), 64 rows 12.5, 11.7; 64 x 4096 x 11008 in eight slices
-// 16.9 (mb = 2), in four 18.1 (mb = 1); 64 x 11008 x 4096 in one 19.2 (mb = 1), in two 20.4 (mb = 2); 200 x 4096 x 4096 in one 19.2
-// (mb = 1), in two 20.4, in four 22.4 (mb = 2); 300 x 4096 x 4096 in four 23.4 (mb = 5), in two 24.4 (mb = 3), in one 24.6 (mb = 2).
+//  - tiles: 4 + 0.5 mb for the launch, the first loads and the end, then rounds of 256 workgroups over the slice's steps (a CU
+//    holds two of mb = 1, which overlap); a further round costs 0.8, slices 3 for the kernel that adds them up and 0.2 a MB;
+//  - by way of bf16: 11 for two launches, 0.41 for a million values of the matrix (written and read again), 1.17 PFLOP/s.
+// Measured: 48 x 4096 x 4096 sixteen at a time 11.0, tiles 11.3 (mb = 1, four slices), 64 rows 12.5, 11.7; 64 x 4096 x 11008 in
+// eight slices 16.9 (mb = 2), in four 18.1 (mb = 1); 64 x 11008 x 4096 in one 19.2 (mb = 1), in two 20.4 (mb = 2); 200 x 4096 x
+// 4096 in one 19.2 (mb = 1), in two 20.4, in four 22.4 (mb = 2); 300 x 4096 x 4096 in four 23.4 (mb = 5), in two 24.4 (mb = 3),
+// in one 24.6 (mb = 2).  Tiles against bf16: 1536 x 4096 x 4096 67.6, 61.2; 2048 rows 81.2, 68.4; 4096 rows 171, 106; 1024 x
+// 11008 x 4096 116.7, 99.0; 2048 x 11008 x 4096 228, 163; 1024 x 3584 x 14336 123, 113; tiles stay at 1024 x 4096 x 4096 (43).
 struct MpPlan {
     int mb, slices, steps_per_slice;     // mb == 0: mx4_few_kernel
+    bool unpack;                         // the matrix to bf16 first, if there is scratch for it
 };
 static MpPlan mp_plan(int M, int N, int K) {
     constexpr float step_us[6] = {0.f, 0.46f, 0.66f, 0.93f, 1.14f, 1.34f};
-    MpPlan best{0, 1, 0};
+    MpPlan best{0, 1, 0, false};
     if (M <= 16 || K < 512) return best;
     const int steps = (K + 127) / 128;
     float least = 2.5f + 2.7f * (float)((M + 15) / 16) * ((float)N * (float)K / 16777216.f);
@@ -341,19 +346,23 @@ static MpPlan mp_plan(int M, int N, int K) {
         for (int want = 1; want <= 16 && want <= steps / 4; ++want) {
             const int per = (steps + want - 1) / want, slices = (steps + per - 1) / per;       // (none of them empty)
             const int64_t rounds = (tiles * slices + 255) / 256;
-            float us = 4.f + 0.5f * mb + (float)rounds * (rounds > 1 && mb == 1 ? 0.84f : 1.f) * per * step_us[mb] + 0.8f * (rounds - 1);
+            const float overlap = rounds > 1 && mb == 1 ? 0.84f : 1.f;
+            float us = 4.f + 0.5f * mb + (float)rounds * overlap * per * step_us[mb] + 0.8f * (rounds - 1);
             if (slices > 1) us += 3.f + 0.8e-6f * slices * (float)M * (float)N;
             if (us < least) {
                 least = us;
-                best = {mb, slices, per};
+                best = {mb, slices, per, false};
             }
         }
     }
+    const float values = (float)N * (float)K;
+    best.unpack = 11.f + 0.41e-6f * values + 1.71e-9f * (float)M * values < least;
     return best;
 }
 
 size_t project_mx4_workspace_bytes(int M, int N, int K) {
     const MpPlan p = mp_plan(M, N, K);
+    if (p.unpack) return up256((size_t)N * K * 2) + gemm_workspace_bytes(M, N, K);
     return p.slices > 1 ? up256((size_t)p.slices * M * N * 4) : 0;
 }
 
@@ -362,6 +371,15 @@ int launch_project_mx4(const uint16_t* x, int64_t x_stride, const uint8_t* codes
                        size_t ws_bytes, hipStream_t s) {
     MpArgs a{x, codes, scales, y, res, x_stride, y_stride, res_stride, M, N, K, nullptr, 0};
     const MpPlan p = mp_plan(M, N, K);
+    const bool scratch = ws_bytes >= project_mx4_workspace_bytes(M, N, K);
+    if (p.unpack && scratch) {
+        uint16_t* w = static_cast<uint16_t*>(ws);
+        const size_t own = up256((size_t)N * K * 2);
+        const int rc = launch_mx4_dequantize(codes, scales, N, K, w, K, s);
+        if (rc) return rc;
+        return launch_gemm_ws(x, x_stride, w, y, y_stride, res, res_stride, M, N, K, nullptr,
+                              ws_bytes > own ? static_cast<char*>(ws) + own : nullptr, ws_bytes - own, s);
+    }
     if (p.mb == 0) {
         // with more tiles than two for every CU four wavefronts each, which fit side by side (1 x 11008 x 4096 6.4, 7.1 us with
         // eight; 1 x 4096 x 11008 7.1, 6.5); more rows keep more in flight
@@ -369,7 +387,7 @@ int launch_project_mx4(const uint16_t* x, int64_t x_stride, const uint8_t* codes
         if (M <= 4) return many ? launch_few<1, 4, 2>(a, s) : launch_few<1, 8, 3>(a, s);
         return M <= 8 ? launch_few<2, 4, 2>(a, s) : launch_few<4, 4, 3>(a, s);
     }
-    const bool cut = p.slices > 1 && ws_bytes >= project_mx4_workspace_bytes(M, N, K);
+    const bool cut = p.slices > 1 && scratch && !p.unpack;
     const int slices = cut ? p.slices : 1;
     a.steps_per_slice = cut ? p.steps_per_slice : (K + 127) / 128;
     if (cut) a.part = static_cast<float*>(ws);

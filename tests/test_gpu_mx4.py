@@ -219,7 +219,8 @@ def attn_case(vc, seed, B, N, Hq, Hkv, d, capacity=None, std=1.0):
 @pytest.mark.parametrize("B,N,Hq,Hkv,d", [
     (1, 1, 1, 1, 64), (1, 1, 2, 2, 128), (2, 15, 4, 4, 64), (2, 16, 4, 2, 128), (2, 17, 4, 2, 64), (2, 31, 4, 2, 128),
     (2, 32, 6, 2, 128), (1, 33, 7, 1, 64), (3, 127, 16, 1, 128), (1, 128, 32, 32, 128), (2, 129, 17, 1, 64), (3, 257, 34, 2, 128),
-    (1, 640, 32, 32, 128), (2, 1000, 20, 2, 128), (1, 6400, 28, 4, 128), (70, 160, 28, 4, 128), (40, 70, 32, 32, 64), (12, 300, 32, 32, 128), (400, 33, 4, 2, 64), (52, 1100, 15, 15, 64),
+    (1, 640, 32, 32, 128), (2, 1000, 20, 2, 128), (1, 6400, 28, 4, 128), (70, 160, 28, 4, 128), (40, 70, 32, 32, 64),
+    (12, 300, 32, 32, 128), (400, 33, 4, 2, 64), (52, 1100, 15, 15, 64),
     (1, 801, 64, 64, 128), (1, 800, 64, 64, 64), (2, 9001, 4, 2, 128), (1, 20000, 2, 1, 64),
     (1, 4097, 3, 3, 64)])
 def test_attention(vc, B, N, Hq, Hkv, d):
@@ -347,6 +348,27 @@ def test_projection(vc, M, N, K):
     (297, 2256, 4448), (318, 2304, 4480)])
 def test_projection_on_tiles(vc, M, N, K):
     project_check(vc, M, N, K, residual=M % 2 == 0, seed=7, one_slice=True)
+
+
+# many rows over a short matrix: tiles in several rounds; over a larger one: the matrix to bf16 first, and the same
+# with no scratch, tiles in several rounds
+@pytest.mark.parametrize("M,N,K,unpacked", [(8192, 1024, 1024, False), (5003, 2064, 1056, True)])
+def test_projection_of_many_rows(vc, M, N, K, unpacked):
+    assert (vc.lib.vitcop_project_mx4_workspace_bytes(M, N, K) >= 2 * N * K) == unpacked
+    project_check(vc, M, N, K, residual=M % 2 == 1, seed=9, one_slice=True)
+
+
+def test_projection_of_many_rows_strided_and_in_place(vc):
+    M, N, K = 2600, 2064, 2080
+    assert vc.lib.vitcop_project_mx4_workspace_bytes(M, N, K) >= 2 * N * K
+    codes, scales = vc.vitcop_mx4_quantize(dev(I.normal_bf16(1110, 0, (N, K))))
+    x = torch.full((M, K + 64), float("nan"), dtype=torch.bfloat16, device="cuda")
+    y = torch.full((M, N + 16), 5.0, dtype=torch.bfloat16, device="cuda")
+    xb, rb = I.normal_bf16(1111, 0, (M, K)), I.normal_bf16(1112, 0, (M, N))
+    x[:, 32:32 + K], y[:, 8:8 + N] = dev(xb), dev(rb)
+    vc.vitcop_project_mx4(x[:, 32:32 + K], codes, scales, residual=y[:, 8:8 + N], out=y[:, 8:8 + N])
+    want = vc.vitcop_project_mx4(dev(xb), codes, scales, residual=dev(rb))
+    assert torch.equal(y[:, 8:8 + N], want) and (y[:, :8] == 5).all() and (y[:, 8 + N:] == 5).all()
 
 
 def test_projection_strided(vc):
