@@ -506,7 +506,8 @@ int vitcop_decode_attn(const uint16_t* q, const uint16_t* k, const uint16_t* v, 
  * To 4 bits: s - 127 is the least exponent in [-125,125] for which no magnitude of the group is above
  * 7 * 2^(s-127); the code is the nearest value, ties going to the even code, what is above 6 to 6, and a zero
  * keeps its sign.  A group that holds an infinity or a NaN gets s = 255 and reads back as NaN (here inputs
- * need not be finite).  s = 253 and 254, which these calls never write, may stand for infinities.
+ * need not be finite).  s = 253 and 254, which these calls never write, may stand for infinities, and an
+ * attention over such rows may give NaN.
  */
 #define VITCOP_MX4_GROUP 32
 

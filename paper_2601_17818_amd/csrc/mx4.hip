@@ -1,8 +1,9 @@
 // Rows of bf16 to 4 bits and back (format: mx4_device.h), as matrices (weights) and as the rows of a KV cache.  Single
 // passes: 2 bytes a value on one side, 17/32 on the other, and a few instructions for eight values, so HBM-bound.
-// Eight values to a thread, 16 bytes of bf16 and one dword of codes: a group is a quad of lanes.  The bf16 side, read or written
-// once, goes past the caches: with rows from HBM a cache of 4 x 2944 x 32 x 128 (244 MB with its bf16 rows, K and V inside QKV rows)
-// to 4 bits 42.8 us, 5.7 TB/s, through the caches 46.6; back 34.7, through them 45; a matrix of 11776 x 4096 20.8 and 17.9 us.
+// Eight values to a thread, 16 bytes of bf16 and one dword of codes: a group is a quad of lanes.  The bf16 side, read or
+// written once, goes past the caches: with rows from HBM a cache of 4 x 2944 x 32 x 128 (244 MB with its bf16 rows, K and V
+// inside QKV rows) to 4 bits 42.8 us, 5.7 TB/s, through the caches 46.6; back 34.7, through them 45; a matrix of 11776 x 4096
+// 20.8 and 17.9 us.
 #include "vitcop_internal.h"
 #include "mx4_device.h"
 

@@ -43,6 +43,19 @@ __device__ __forceinline__ void mp_load(__amdgpu_buffer_rsrc_t from, char* to, u
 #endif
 }
 
+// More than 64 KB of dynamic LDS for a kernel, once for every device (`raised`: a bit for each, one such word an instantiation;
+// a second thread that repeats the call does no harm).
+static int mp_raise_lds(const void* kernel, int bytes, std::atomic<uint64_t>& raised) {
+    int device = 0;
+    int rc = hip_status(hipGetDevice(&device), "hipGetDevice");
+    const uint64_t bit = device < 64 ? (uint64_t)1 << device : 0;
+    if (rc || (raised.load(std::memory_order_acquire) & bit)) return rc;
+    rc = hip_status(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes),
+                    "hipFuncSetAttribute(project_mx4)");
+    if (rc == VITCOP_OK) raised.fetch_or(bit, std::memory_order_release);
+    return rc;
+}
+
 // At most 16 rows of x (or any number, 16 at a time): a workgroup takes 16 rows of W, and its wavefronts take turns at their
 // columns, 128 at a time, each with DEPTH steps in flight in an LDS ring of its own; their sums meet at the end, in a fixed
 // order.  XI: loads of four rows of x a step.  Measured with weights from HBM, us (of which 2.5 are the launch): 1 x 4096 x 4096
@@ -129,13 +142,11 @@ __global__ __launch_bounds__(64 * WAVES) void mx4_few_kernel(MpArgs a) {
 template <int XI, int WAVES, int DEPTH>
 static int launch_few(const MpArgs& a, hipStream_t s) {
     const size_t lds = mp_ring_bytes<XI, WAVES, DEPTH>() + ((size_t)a.K / 2 + 1023) / 1024 * 1024;
-    static std::atomic<size_t> raised_to{65536};     // (per instantiation) dynamic LDS the kernel may use so far
-    if (lds > raised_to.load()) {
-        const int rc = hip_status(hipFuncSetAttribute(reinterpret_cast<const void*>(&mx4_few_kernel<XI, WAVES, DEPTH>),
-                                                      hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds),
-                                  "hipFuncSetAttribute(mx4_few)");
+    constexpr int most = mp_ring_bytes<XI, WAVES, DEPTH>() + 32768;          // (K = 2^16)
+    static std::atomic<uint64_t> raised{0};
+    if (lds > 65536) {
+        const int rc = mp_raise_lds(reinterpret_cast<const void*>(&mx4_few_kernel<XI, WAVES, DEPTH>), most, raised);
         if (rc) return rc;
-        raised_to.store(lds);
     }
     hipLaunchKernelGGL((mx4_few_kernel<XI, WAVES, DEPTH>), dim3(a.N / 16, (a.M + 15) / 16), dim3(64 * WAVES), lds, s, a);
     return launch_status("mx4_few");
@@ -146,8 +157,9 @@ static int launch_few(const MpArgs& a, hipStream_t s) {
 // into it at 128 bytes a cycle (MB = 5: 1750 cycles) and multiplies 8 MB times a wavefront (1280 cycles a SIMD); without loads
 // from memory it takes 2250, with them some 3000.  Reading a step ahead into registers, between the products, gains nothing
 // (64 x 4096 x 11008 13.4, 14.0 us; 317 x 3584 x 14336 43.1, 42.8), nor do four wavefronts with twice the columns each and fewer
-// reads (14.3, 48.1), nor different starts in k (13.6, 48).  K >= 512; WHOLE: whole steps.  The slices' sums are added by mx4_sum_kernel.
-// Measured without it, us: 32 x 4096 x 11008 10.4, 64 x 4096 x 11008 13.4, 64 x 11008 x 4096 15.8, 317 x 3584 x 14336 43.1 (0.76 PFLOP/s).
+// reads (14.3, 48.1), nor different starts in k (13.6, 48).  K >= 512; WHOLE: whole steps.  The slices' sums are added by
+// mx4_sum_kernel.  Measured without it, us: 32 x 4096 x 11008 10.4, 64 x 4096 x 11008 13.4, 64 x 11008 x 4096 15.8, 317 x 3584 x
+// 14336 43.1 (0.76 PFLOP/s).
 constexpr int MT_WM = 2, MT_WN = 4, MT_RT = 2, MT_WAVES = MT_WM * MT_WN, MT_BN = 16 * MT_RT * MT_WN;
 constexpr int MT_EXPS = MT_BN * 16;                  // bytes of a unit of exponents
 template <int MB, int NS>
@@ -156,7 +168,8 @@ constexpr int mp_tile_bytes() { return NS * (16 * MB * MT_WM * 256 + MT_BN * 64)
 template <int MB, int NS, bool WHOLE>
 __global__ __launch_bounds__(64 * MT_WAVES) void mx4_tile_kernel(MpArgs a) {
     constexpr int BM = 16 * MB * MT_WM, BN = MT_BN, RT = MT_RT;
-    constexpr int XL = BM / (4 * MT_WAVES), NL = XL + 1, SLOT = BM * 256 + BN * 64;        // loads of x, of x and codes a wavefront and step
+    // loads of x, of x and codes a wavefront and step, bytes of a step
+    constexpr int XL = BM / (4 * MT_WAVES), NL = XL + 1, SLOT = BM * 256 + BN * 64;
     static_assert(XL * 4 * MT_WAVES == BM && 16 * MT_WAVES == BN, "whole loads for every wavefront");
     extern __shared__ __attribute__((aligned(16))) char mp_lds[];
     const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4;
@@ -191,9 +204,9 @@ __global__ __launch_bounds__(64 * MT_WAVES) void mx4_tile_kernel(MpArgs a) {
 #pragma unroll
         for (int q = 0; q < XL; ++q) mp_load(x_desc, to + (XL * wv + q) * 1024, (x_off[q] + 256 * step) | past(x_grp[q]));
     };
-    // Exponents come in units, 16 bytes of a row a lane: those of four steps, a row's last unit ending with it, or where rows do not
-    // start at whole words of three, from the word on that holds the first.  Two are asked for here, and with every step of a
-    // unit some rows of the one after the next.
+    // Exponents come in units, 16 bytes of a row a lane: those of four steps, a row's last unit ending with it, or where rows
+    // do not start at whole words of three, from the word on that holds the first.  Two are asked for here, and with every
+    // step of a unit some rows of the one after the next.
     constexpr int UNIT = WHOLE ? 4 : 3, ROWS = WHOLE ? BN / 4 / MT_WAVES : 6;                // steps; rows a wavefront and step
     static_assert(MT_EXPS == 2048 && MT_WAVES >= 4 && ROWS * MT_WAVES * UNIT >= BN, "two loads a unit");
     char* const scales = mp_lds + NS * SLOT;
@@ -234,7 +247,8 @@ __global__ __launch_bounds__(64 * MT_WAVES) void mx4_tile_kernel(MpArgs a) {
                 xx[j][c] = *reinterpret_cast<const u32x4*>(from + (16 * (MB * wm + j) + l16) * 256 + ((4 * g4 + c) ^ l16) * 16);
         const int e_row = ROWS * (MT_WAVES * phase + wv);
         if (lane < ROWS && e_row + lane < BN)
-            mp_load(s_desc, scales + (exp_slot == 0 ? 2 : exp_slot - 1) * MT_EXPS + e_row * 16, (unsigned)unit_at(e_row + lane, unit + 2));
+            mp_load(s_desc, scales + (exp_slot == 0 ? 2 : exp_slot - 1) * MT_EXPS + e_row * 16,
+                    (unsigned)unit_at(e_row + lane, unit + 2));
         load(ahead, step + NS - 1);
         if (++phase == UNIT) {
             phase = 0;
@@ -278,14 +292,10 @@ static int launch_tiles_of(const MpArgs& a, int slices, hipStream_t s) {
     const int tiles = ((a.N + MT_BN - 1) / MT_BN + 7) / 8 * 8 * ((a.M + 32 * MB - 1) / (32 * MB));
     constexpr int lds = mp_tile_bytes<MB, NS>();
     static_assert(lds <= 160 * 1024, "LDS of a CU");
-    static std::atomic<bool> raised{false};          // (per instantiation; a second thread repeating the call is harmless)
-    if (lds > 65536 && !raised.load()) {
-        const int rc = hip_status(hipFuncSetAttribute(reinterpret_cast<const void*>(&mx4_tile_kernel<MB, NS, WHOLE>),
-                                                      hipFuncAttributeMaxDynamicSharedMemorySize, lds),
-                                  "hipFuncSetAttribute(mx4_tile)");
-        if (rc) return rc;
-        raised.store(true);
-    }
+    static_assert(lds > 65536, "raised for all of them");
+    static std::atomic<uint64_t> raised{0};
+    const int rc = mp_raise_lds(reinterpret_cast<const void*>(&mx4_tile_kernel<MB, NS, WHOLE>), lds, raised);
+    if (rc) return rc;
     hipLaunchKernelGGL((mx4_tile_kernel<MB, NS, WHOLE>), dim3(tiles, slices), dim3(64 * MT_WAVES), lds, s, a);
     return launch_status("mx4_tile");
 }
