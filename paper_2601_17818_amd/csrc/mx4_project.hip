@@ -29,7 +29,7 @@ struct MpArgs {
     int64_t x_stride, y_stride, res_stride;
     int M, N, K;
     float* part;                         // slices of K: [slices][M][N] sums, left to be added up; or nullptr
-    int steps_per_slice;
+    int slices, steps_per_slice;
 };
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t mp_desc(const void* base, int64_t bytes) {
@@ -174,12 +174,15 @@ __global__ __launch_bounds__(64 * MT_WAVES) void mx4_tile_kernel(MpArgs a) {
     extern __shared__ __attribute__((aligned(16))) char mp_lds[];
     const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wv % MT_WM, wn = wv / MT_WM;
-    // tiles of the same rows of W go to the same XCD, one after the other: they share its L2
-    const int tiles_m = (a.M + BM - 1) / BM, nth = blockIdx.x >> 3;
-    const int n0 = ((nth / tiles_m) * 8 + (blockIdx.x & 7)) * BN, m0 = nth % tiles_m * BM;
+    // an XCD takes an eighth of the tiles, one after the other, so that none has more than its CUs while others have fewer
+    // (75 x 4272 x 9856, 34 columns of tiles and seven slices: 20.4 us; columns dealt out whole 31.5); those of the same rows
+    // of W together, which share its L2, all slices of them: parts of rows a power of two apart would share its channels
+    const unsigned tiles_m = (a.M + BM - 1) / BM;
+    const unsigned id = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3), col = id / tiles_m;
+    const int slice = col % a.slices, n0 = col / a.slices * BN, m0 = id % tiles_m * BM;
     if (n0 >= a.N) return;
     const int groups = a.K / MX4_GROUP;
-    const int first = blockIdx.y * a.steps_per_slice, end = min((groups + 3) / 4, first + a.steps_per_slice);
+    const int first = slice * a.steps_per_slice, end = min((groups + 3) / 4, first + a.steps_per_slice);
     const int rows = min(BN, a.N - n0);
     const auto c_desc = mp_desc(a.codes + (int64_t)n0 * (a.K / 2), (int64_t)rows * (a.K / 2));
     const int s_bytes = (rows * groups + 3) & ~3;            // (whole words)
@@ -276,7 +279,7 @@ __global__ __launch_bounds__(64 * MT_WAVES) void mx4_tile_kernel(MpArgs a) {
             if (n >= a.N || m >= a.M) continue;
             f32x4 v = acc[r][j];
             if (a.part) {
-                *reinterpret_cast<f32x4*>(a.part + ((int64_t)blockIdx.y * a.M + m) * a.N + n) = v;
+                *reinterpret_cast<f32x4*>(a.part + ((int64_t)slice * a.M + m) * a.N + n) = v;
                 continue;
             }
             if (a.res) {
@@ -288,27 +291,27 @@ __global__ __launch_bounds__(64 * MT_WAVES) void mx4_tile_kernel(MpArgs a) {
 }
 
 template <int MB, int NS, bool WHOLE>
-static int launch_tiles_of(const MpArgs& a, int slices, hipStream_t s) {
-    const int tiles = ((a.N + MT_BN - 1) / MT_BN + 7) / 8 * 8 * ((a.M + 32 * MB - 1) / (32 * MB));
+static int launch_tiles_of(const MpArgs& a, hipStream_t s) {
+    const int tiles = (a.N + MT_BN - 1) / MT_BN * ((a.M + 32 * MB - 1) / (32 * MB)) * a.slices;
     constexpr int lds = mp_tile_bytes<MB, NS>();
     static_assert(lds <= 160 * 1024, "LDS of a CU");
     static_assert(lds > 65536, "raised for all of them");
     static std::atomic<uint64_t> raised{0};
     const int rc = mp_raise_lds(reinterpret_cast<const void*>(&mx4_tile_kernel<MB, NS, WHOLE>), lds, raised);
     if (rc) return rc;
-    hipLaunchKernelGGL((mx4_tile_kernel<MB, NS, WHOLE>), dim3(tiles, slices), dim3(64 * MT_WAVES), lds, s, a);
+    hipLaunchKernelGGL((mx4_tile_kernel<MB, NS, WHOLE>), dim3((tiles + 7) / 8 * 8), dim3(64 * MT_WAVES), lds, s, a);
     return launch_status("mx4_tile");
 }
 
 template <int MB, int NS>
-static int launch_tiles(const MpArgs& a, int slices, hipStream_t s) {
-    return a.K % 128 == 0 ? launch_tiles_of<MB, NS, true>(a, slices, s) : launch_tiles_of<MB, NS, false>(a, slices, s);
+static int launch_tiles(const MpArgs& a, hipStream_t s) {
+    return a.K % 128 == 0 ? launch_tiles_of<MB, NS, true>(a, s) : launch_tiles_of<MB, NS, false>(a, s);
 }
 
 // y = the slices' sums added up in their order (+ residual): four columns of a row a thread, eight slices' loads and the
 // residual's in flight at once, since it is a chain of round trips and little else (64 x 4096 x 11008 in eight slices 17.3 us in
 // all; with launch_partial_reduce, whose threads take eight columns and four slices at a time, 17.8).
-__global__ __launch_bounds__(256) void mx4_sum_kernel(MpArgs a, int slices) {
+__global__ __launch_bounds__(256) void mx4_sum_kernel(MpArgs a) {
     const int quads = a.N / 4;
     const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (id >= (int64_t)a.M * quads) return;
@@ -317,30 +320,32 @@ __global__ __launch_bounds__(256) void mx4_sum_kernel(MpArgs a, int slices) {
     uint2 res = make_uint2(0, 0);
     if (a.res) res = *reinterpret_cast<const uint2*>(a.res + m * a.res_stride + n);
     f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 < slices; s0 += 8) {
+    for (int s0 = 0; s0 < a.slices; s0 += 8) {
         f32x4 t[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (s0 + i < slices) t[i] = *reinterpret_cast<const f32x4*>(p + (s0 + i) * slice);
+            if (s0 + i < a.slices) t[i] = *reinterpret_cast<const f32x4*>(p + (s0 + i) * slice);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (s0 + i < slices) v += t[i];
+            if (s0 + i < a.slices) v += t[i];
     }
     v += f32x4{bf16_lo(res.x), bf16_hi(res.x), bf16_lo(res.y), bf16_hi(res.y)};
     *reinterpret_cast<uint2*>(a.y + m * a.y_stride + n) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
 }
 
 // Which launch: sixteen rows of x at a time, tiles of 32 mb with k in how many slices, or the matrix to bf16 and the bf16
-// projection.  By estimated time, us, fitted to twenty-odd sizes of 20 to 4096 rows with weights from HBM:
+// projection.  By estimated time, us, fitted to fifty-odd sizes of 20 to 5500 rows with weights from HBM; on 26 others, of 300
+// to 4000 rows, it took the faster of tiles and bf16 each time but where they were within 1 %:
 //  - sixteen rows at a time: 2.5 and 2.7 for every 2^24 values of the matrix, which is read again for every sixteen;
 //  - tiles: 4 + 0.5 mb for the launch, the first loads and the end, then rounds of 256 workgroups over the slice's steps (a CU
-//    holds two of mb = 1, which overlap); a further round costs 0.8, slices 3 for the kernel that adds them up and 0.2 a MB;
-//  - by way of bf16: 11 for two launches, 0.41 for a million values of the matrix (written and read again), 1.17 PFLOP/s.
+//    holds two of mb = 1, which overlap); a further round costs 1 + 0.8 mb, slices 3 for the kernel that adds them up and 0.2 a MB;
+//  - by way of bf16: 8.1 for two launches, for a million values of the matrix 0.27, of y 1.4, for a thousand columns 3.6, and
+//    1.7 PFLOP/s.
 // Measured: 48 x 4096 x 4096 sixteen at a time 11.0, tiles 11.3 (mb = 1, four slices), 64 rows 12.5, 11.7; 64 x 4096 x 11008 in
 // eight slices 16.9 (mb = 2), in four 18.1 (mb = 1); 64 x 11008 x 4096 in one 19.2 (mb = 1), in two 20.4 (mb = 2); 200 x 4096 x
 // 4096 in one 19.2 (mb = 1), in two 20.4, in four 22.4 (mb = 2); 300 x 4096 x 4096 in four 23.4 (mb = 5), in two 24.4 (mb = 3),
-// in one 24.6 (mb = 2).  Tiles against bf16: 1536 x 4096 x 4096 67.6, 61.2; 2048 rows 81.2, 68.4; 4096 rows 171, 106; 1024 x
-// 11008 x 4096 116.7, 99.0; 2048 x 11008 x 4096 228, 163; 1024 x 3584 x 14336 123, 113; tiles stay at 1024 x 4096 x 4096 (43).
+// in one 24.6 (mb = 2).  Tiles against bf16: 1024 x 4096 x 4096 40.6, 50.3; 1536 rows 66.6, 60.2; 2048 rows 80.0, 69.9; 1024 x
+// 11008 x 4096 116, 103; 2251 x 6112 x 7968 264, 200; 634 x 1904 x 9984 37, 48; 3978 x 1088 x 4192 52.7, 55.3.
 struct MpPlan {
     int mb, slices, steps_per_slice;     // mb == 0: mx4_few_kernel
     bool unpack;                         // the matrix to bf16 first, if there is scratch for it
@@ -357,7 +362,7 @@ static MpPlan mp_plan(int M, int N, int K) {
             const int per = (steps + want - 1) / want, slices = (steps + per - 1) / per;       // (none of them empty)
             const int64_t rounds = (tiles * slices + 255) / 256;
             const float overlap = rounds > 1 && mb == 1 ? 0.84f : 1.f;
-            float us = 4.f + 0.5f * mb + (float)rounds * overlap * per * step_us[mb] + 0.8f * (rounds - 1);
+            float us = 4.f + 0.5f * mb + (float)rounds * overlap * per * step_us[mb] + (1.f + 0.8f * mb) * (rounds - 1);
             if (slices > 1) us += 3.f + 0.8e-6f * slices * (float)M * (float)N;
             if (us < least) {
                 least = us;
@@ -365,8 +370,8 @@ static MpPlan mp_plan(int M, int N, int K) {
             }
         }
     }
-    const float values = (float)N * (float)K;
-    best.unpack = 11.f + 0.41e-6f * values + 1.71e-9f * (float)M * values < least;
+    const float m = (float)M, n = (float)N, k = (float)K;
+    best.unpack = 8.1f + 0.274e-6f * n * k + 1.38e-6f * m * n + 3.55e-3f * k + 1.19e-9f * m * n * k < least;
     return best;
 }
 
@@ -379,7 +384,7 @@ size_t project_mx4_workspace_bytes(int M, int N, int K) {
 int launch_project_mx4(const uint16_t* x, int64_t x_stride, const uint8_t* codes, const uint8_t* scales, uint16_t* y,
                        int64_t y_stride, const uint16_t* res, int64_t res_stride, int M, int N, int K, void* ws,
                        size_t ws_bytes, hipStream_t s) {
-    MpArgs a{x, codes, scales, y, res, x_stride, y_stride, res_stride, M, N, K, nullptr, 0};
+    MpArgs a{x, codes, scales, y, res, x_stride, y_stride, res_stride, M, N, K, nullptr, 1, 0};
     const MpPlan p = mp_plan(M, N, K);
     const bool scratch = ws_bytes >= project_mx4_workspace_bytes(M, N, K);
     if (p.unpack && scratch) {
@@ -398,19 +403,19 @@ int launch_project_mx4(const uint16_t* x, int64_t x_stride, const uint8_t* codes
         return M <= 8 ? launch_few<2, 4, 2>(a, s) : launch_few<4, 4, 3>(a, s);
     }
     const bool cut = p.slices > 1 && scratch && !p.unpack;
-    const int slices = cut ? p.slices : 1;
+    a.slices = cut ? p.slices : 1;
     a.steps_per_slice = cut ? p.steps_per_slice : (K + 127) / 128;
     if (cut) a.part = static_cast<float*>(ws);
     int rc = 0;
     switch (p.mb) {
-        case 1: rc = launch_tiles<1, 4>(a, slices, s); break;
-        case 2: rc = launch_tiles<2, 4>(a, slices, s); break;
-        case 3: rc = launch_tiles<3, 3>(a, slices, s); break;
-        case 4: rc = launch_tiles<4, 3>(a, slices, s); break;
-        default: rc = launch_tiles<5, 3>(a, slices, s); break;
+        case 1: rc = launch_tiles<1, 4>(a, s); break;
+        case 2: rc = launch_tiles<2, 4>(a, s); break;
+        case 3: rc = launch_tiles<3, 3>(a, s); break;
+        case 4: rc = launch_tiles<4, 3>(a, s); break;
+        default: rc = launch_tiles<5, 3>(a, s); break;
     }
     if (rc || !cut) return rc;
-    hipLaunchKernelGGL(mx4_sum_kernel, dim3((unsigned)(((int64_t)M * (N / 4) + 255) / 256)), dim3(256), 0, s, a, slices);
+    hipLaunchKernelGGL(mx4_sum_kernel, dim3((unsigned)(((int64_t)M * (N / 4) + 255) / 256)), dim3(256), 0, s, a);
     return launch_status("mx4_sum");
 }
 
