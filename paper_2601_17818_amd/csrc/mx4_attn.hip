@@ -179,28 +179,30 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 3) void mx4_attn_kerne
         for (int i = 0; i < BLOCKS; ++i) *reinterpret_cast<f32x4*>(&so[wv][l16][16 * i + 4 * g4]) = o[i];
     }
     __syncthreads();
-    // the wavefronts' states combined by threads (head, channel): this slice's partial, or with `out` the output
-    for (int idx = threadIdx.x; idx < G * D; idx += 64 * WAVES) {
-        const int g = idx / D, ch = idx - g * D;
+    // the wavefronts' states combined by threads (head, four channels): this slice's partial, or with `out` the output
+    for (int idx = threadIdx.x; idx < G * (D / 4); idx += 64 * WAVES) {
+        const int g = idx / (D / 4), ch = idx % (D / 4) * 4;
         float mn = -INFINITY;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) mn = fmaxf(mn, sm[w][g][0]);
-        float lt = 0.f, ot = 0.f;
+        float lt = 0.f;
+        f32x4 ot = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
             const float a = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(sm[w][g][0] - mn);
             lt += sm[w][g][1] * a;
-            ot += so[w][g][ch] * a;
+            ot += *reinterpret_cast<const f32x4*>(&so[w][g][ch]) * a;
         }
+        const int64_t bh = (int64_t)b * Hq + h0 + g;
         if (out != nullptr) {
-            const int64_t bh = (int64_t)b * Hq + h0 + g;
-            const float r = mx4_quotient(ot, lt), r1 = __shfl_down(r, 1, 64);        // (a wavefront's lanes share g: D >= 64)
-            if ((ch & 1) == 0) *reinterpret_cast<uint32_t*>(out + bh * D + ch) = pack_bf16(r, r1);
+            *reinterpret_cast<uint2*>(out + bh * D + ch) =
+                make_uint2(pack_bf16(mx4_quotient(ot.x, lt), mx4_quotient(ot.y, lt)),
+                           pack_bf16(mx4_quotient(ot.z, lt), mx4_quotient(ot.w, lt)));
             if (lse && ch == 0) lse[bh] = mx4_lse(mn, lt);
             continue;
         }
-        const int64_t slot = ((int64_t)b * Hq + h0 + g) * n_splits + split;
-        part_o[slot * D + ch] = ot;
+        const int64_t slot = bh * n_splits + split;
+        *reinterpret_cast<f32x4*>(part_o + slot * D + ch) = ot;
         if (ch == 0) {
             part_ml[slot * 2] = mn;
             part_ml[slot * 2 + 1] = lt;
@@ -264,27 +266,47 @@ __global__ __launch_bounds__(MM_THREADS) void mx4_merge_kernel(const float* __re
 }
 
 // How many slices of the keys and wavefronts to a slice.  A workgroup costs some two microseconds before its first and after
-// its last key, the merge of slices three, and 256 workgroups of eight wavefronts draw what the memory gives.  Measured, us
-// (samples x keys x KV heads of 128):
-//  - from 129 pairs of a sample and a KV head on, and up to 800 keys, one slice: 4 x 1000 x 32 8.7, in two and four 9.5, 9.3;
-//    1 x 640 x 32 6.4, in three 7.3; but 4 x 2000 x 32 13.2, in four 12.4; 1 x 2000 x 32 in two, four and eight 9.6, 8.8, 7.9.
-//  - slices of up to 512 keys take four wavefronts (1 x 1500 x 32 in six, with four and eight wavefronts 7.7, 7.9), longer ones
-//    eight and half as many (4 x 65536 x 4 in 32 and in 16 30.0, 29.5; 1 x 131072 x 4 in 128 and in 64 21.7, 20.0).
-//  - of one slice the more pairs there are, the fewer wavefronts: two, four and eight 8 x 640 x 32 14.0, 8.3, 7.6; 12 x 640 x 32
-//    13.7, 10.0, 11.3; 20 x 640 x 32 14.9, 14.4, 15.9; 28 x 640 x 32 17.0, 20.0, 20.7; 64 x 352 x 32 20.6, 23.3, 24.5; long ones
-//    want four again, 64 x 1536 x 32 69.3, 68.6, 74.1 (428 MB: 6.2 TB/s); and none of them to be without a key.
+// its last key, the merge of slices three to four; a CU draws 31 KB/us (rows of 64: 22) with eight wavefronts on it, the chip
+// 6.2 TB/s, 24 KB/us a CU.  Measured, us (pairs of a sample and a KV head x keys, of 128 or of 64):
+//  - up to 128 pairs, one slice for up to 800 keys (128 x 1000 9.5 in four, 9.2 in one; 32 x 640 6.4, in three 7.3); above, slices
+//    of 256 to 512 keys take four wavefronts (32 x 1500 in six, with four and eight wavefronts 7.7, 7.9); longer ones, of fewer
+//    than 32 pairs, eight, one workgroup to a CU (16 x 65536 in 32 with four and in 16 with eight 30.0, 29.5), and of more
+//    pairs four, three to a CU, which come out even where 256 is no multiple of the pairs (96 x 15000 in two, eight wavefronts
+//    47.4, in eight, four 37.8; 64 x 40000 63.1, 58.9; of 64 43.9, 39.9).
+//  - up to 512 pairs, slices of four wavefronts where some CUs would have a workgroup more than others for long enough to pay
+//    for the merge (one slice, sliced: 132 x 1800 12.6, 13.0; x 7200 36.6, 29.7; 232 x 7200 40.5, 42.3; 280 x 3600 35.0, 31.8;
+//    340 x 14400 129, 110; of 64 86, 69; 512 x 14400 159, 159).
+//  - of one slice the more pairs there are, the fewer wavefronts, and the more keys, the more: two, four, eight 640 x 150 7.0, 7.3,
+//    9.5; 640 x 650 17.8, 14.8, 16.5; 1500 x 300 16.2, 16.5, 18.9; 1500 x 650 29.8, 26.7, 30.1; 3000 x 450 36.2, 37.5, 45.1;
+//    3000 x 1000 73.5, 67.2, 76.4; four, eight 280 x 900 13.0, 13.4; 420 x 7200 76.8, 70.7; of 64 760 x 7200 76.3, 69.9; and none
+//    of them to be without a key.
 struct AttnPlan {
     int waves, keys_per_split, splits;
 };
-static AttnPlan attn_plan(int B, int N, int Hkv) {
+static AttnPlan attn_plan(int B, int N, int Hkv, int d) {
     const int64_t pairs = (int64_t)B * Hkv;
     AttnPlan p{8, 0, 1};
     if (pairs <= 128 && N > 800) {
         p.waves = 4;
         p.splits = (int)std::min<int64_t>(512 / pairs, (N + 255) / 256);
-        if ((N + p.splits - 1) / p.splits > 512) p = AttnPlan{8, 0, (int)(256 / pairs)};
-    } else {
-        if (pairs > 320) p.waves = pairs <= 768 || N > 1024 ? 4 : 2;
+        if ((N + p.splits - 1) / p.splits > 512)
+            p = pairs < 32 ? AttnPlan{8, 0, (int)(256 / pairs)} : AttnPlan{4, 0, (int)(768 / pairs)};
+    } else if (pairs <= 512 && N > 800) {
+        const float pair_us = (float)N * (float)(d * 17 / 16) / (d == 64 ? 22e3f : 31e3f);          // of a CU
+        const float chip_us = (float)pairs * (float)N * (float)(d * 17 / 16) / 6.2e6f;
+        float least = 1e30f;
+        for (int s = 1; s <= 4; ++s) {
+            const float us = std::max(chip_us, pair_us / s * (float)((pairs * s + 255) / 256)) + (s > 1 ? 4.f : 0.f);
+            if (us < least) {
+                least = us;
+                p.splits = s;
+            }
+        }
+        if (p.splits > 1) p.waves = 4;
+    }
+    if (p.splits == 1) {
+        if (pairs > 256 && (N <= 1500 || pairs > (d == 64 ? 1024 : 512))) p.waves = 4;
+        if ((pairs > 768 && N <= (pairs > 2048 ? 800 : 400)) || (pairs > 512 && N <= 160)) p.waves = 2;
         while (p.waves > 2 && (p.waves / 2) * MA_KEYS >= N) p.waves /= 2;
     }
     const int64_t unit = p.waves * MA_KEYS, keys = (N + p.splits - 1) / p.splits;
@@ -294,7 +316,7 @@ static AttnPlan attn_plan(int B, int N, int Hkv) {
 }
 
 size_t decode_mx4_workspace_bytes(int B, int N, int Hq, int Hkv, int d) {
-    const size_t s = attn_plan(B, N, Hkv).splits;
+    const size_t s = attn_plan(B, N, Hkv, d).splits;
     return s == 1 ? 0 : up256((size_t)B * Hq * s * d * 4) + up256((size_t)B * Hq * s * 2 * 4);
 }
 
@@ -302,7 +324,7 @@ template <int D>
 static int launch_attn_d(const uint16_t* q, const vitcop_cache_mx4_t& C, uint16_t* out, float* lse, int N,
                          const int32_t* n_samples, int Hq, float scale, void* ws, hipStream_t s) {
     const int B = C.B, group = Hq / C.Hkv;
-    const AttnPlan p = attn_plan(B, N, C.Hkv);
+    const AttnPlan p = attn_plan(B, N, C.Hkv, D);
     float* po = static_cast<float*>(ws);
     float* pml = reinterpret_cast<float*>(static_cast<char*>(ws) + up256((size_t)B * Hq * p.splits * D * 4));
     auto* kernel = p.waves == 8 ? mx4_attn_kernel<D, 8> : (p.waves == 4 ? mx4_attn_kernel<D, 4> : mx4_attn_kernel<D, 2>);

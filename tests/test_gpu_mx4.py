@@ -220,7 +220,8 @@ def attn_case(vc, seed, B, N, Hq, Hkv, d, capacity=None, std=1.0):
     (1, 1, 1, 1, 64), (1, 1, 2, 2, 128), (2, 15, 4, 4, 64), (2, 16, 4, 2, 128), (2, 17, 4, 2, 64), (2, 31, 4, 2, 128),
     (2, 32, 6, 2, 128), (1, 33, 7, 1, 64), (3, 127, 16, 1, 128), (1, 128, 32, 32, 128), (2, 129, 17, 1, 64), (3, 257, 34, 2, 128),
     (1, 640, 32, 32, 128), (2, 1000, 20, 2, 128), (1, 6400, 28, 4, 128), (70, 160, 28, 4, 128), (40, 70, 32, 32, 64),
-    (12, 300, 32, 32, 128), (400, 33, 4, 2, 64), (52, 1100, 15, 15, 64),
+    (12, 300, 32, 32, 128), (400, 33, 4, 2, 64), (52, 1100, 15, 15, 64), (9, 3500, 16, 16, 128), (12, 13001, 4, 4, 64),
+    (40, 1610, 16, 16, 64), (20, 7001, 28, 14, 64), (96, 900, 28, 14, 128),
     (1, 801, 64, 64, 128), (1, 800, 64, 64, 64), (2, 9001, 4, 2, 128), (1, 20000, 2, 1, 64),
     (1, 4097, 3, 3, 64)])
 def test_attention(vc, B, N, Hq, Hkv, d):
