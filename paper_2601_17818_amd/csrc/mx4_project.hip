@@ -56,36 +56,37 @@ static int mp_raise_lds(const void* kernel, int bytes, std::atomic<uint64_t>& ra
     return rc;
 }
 
-// At most 16 rows of x (or any number, 16 at a time): a workgroup takes 16 rows of W, and its wavefronts take turns at their
+// At most 16 rows of x (or any number, 16 at a time): a workgroup takes 16 R rows of W, and its wavefronts take turns at their
 // columns, 128 at a time, each with DEPTH steps in flight in an LDS ring of its own; their sums meet at the end, in a fixed
 // order.  XI: loads of four rows of x a step.  Measured with weights from HBM, us (of which 2.5 are the launch): 1 x 4096 x 4096
-// 4.1, x 11008 6.5, 1 x 11008 x 4096 6.4 (23.9 MB in 3.9 us: 6 TB/s), 7 x 11008 x 4096 8.4, 16 x 4096 x 4096 5.3.
-template <int XI, int WAVES, int DEPTH>
-constexpr int mp_ring_bytes() { return WAVES * DEPTH * (1 + XI) * 1024; }
+// 4.3, x 14336 7.6, 1 x 11008 x 4096 6.6 (23.9 MB in 4 us: 6 TB/s), 8 x 11008 x 4096 7.4, 16 x 11008 x 4096 8.7.
+template <int R, int XI, int WAVES, int DEPTH>
+constexpr int mp_ring_bytes() { return WAVES * DEPTH * (R + XI) * 1024; }
 
-template <int XI, int WAVES, int DEPTH>
+template <int R, int XI, int WAVES, int DEPTH>
 __global__ __launch_bounds__(64 * WAVES) void mx4_few_kernel(MpArgs a) {
-    constexpr int NL = 1 + XI, SLOT = NL * 1024;             // loads a step, bytes of a step in the ring
+    constexpr int NL = R + XI, SLOT = NL * 1024;             // loads a step, bytes of a step in the ring
+    static_assert(R <= WAVES, "a wavefront for every 16 rows at the end");
     extern __shared__ __attribute__((aligned(16))) char mp_lds[];
     const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16;
-    const int groups = a.K / MX4_GROUP, steps = (groups + 3) / 4;
-    const auto c_desc = mp_desc(a.codes + (int64_t)n0 * (a.K / 2), 16 * (a.K / 2));
-    const auto s_desc = mp_desc(a.scales + (int64_t)n0 * groups, 16 * groups);
+    const int n0 = blockIdx.x * (16 * R), m0 = blockIdx.y * 16;
+    const int groups = a.K / MX4_GROUP, steps = (groups + 3) / 4, rows = min(16 * R, a.N - n0);
+    const auto c_desc = mp_desc(a.codes + (int64_t)n0 * (a.K / 2), rows * (a.K / 2));
+    const auto s_desc = mp_desc(a.scales + (int64_t)n0 * groups, rows * groups);
     const auto x_desc = mp_desc(a.x + m0 * a.x_stride, ((a.M - m0 - 1) * a.x_stride + a.K) * 2);
     char* const ring = mp_lds + wv * (DEPTH * SLOT);
-    char* const exps = mp_lds + mp_ring_bytes<XI, WAVES, DEPTH>();
-    // the epilogue's part of the first wavefront: four neighbouring columns of a row of y a lane
-    const int n = n0 + 4 * g4, m = m0 + l16;
-    const bool mine = wv == 0 && m < a.M;
+    char* const exps = mp_lds + mp_ring_bytes<R, XI, WAVES, DEPTH>();
+    // the epilogue's part of the first R wavefronts: four neighbouring columns of a row of y a lane
+    const int n = n0 + 16 * wv + 4 * g4, m = m0 + l16;
+    const bool mine = wv < R && n < a.N && m < a.M;
     uint2 res = make_uint2(0, 0);
     if (a.res && mine) res = *reinterpret_cast<const uint2*>(a.res + m * a.res_stride + n);
-    // the exponents of these rows: one contiguous run of 16 * groups bytes
-    for (int u = 64 * wv; u < groups; u += 64 * WAVES) mp_load(s_desc, exps + u * 16, (u + lane) * 16);
+    // the exponents of these rows: one contiguous run
+    for (int u = 64 * wv; u < R * groups; u += 64 * WAVES) mp_load(s_desc, exps + u * 16, (u + lane) * 16);
     // where this lane's 16 bytes of a load come from
     const int c_grp = lane % 4 ^ (lane >> 4);
-    const unsigned c_off = (unsigned)(lane / 4) * (unsigned)(a.K / 2) + 16 * c_grp;
+    const unsigned c_off = (unsigned)(lane / 4) * (unsigned)(a.K / 2) + 16 * c_grp, c_next = 16 * (unsigned)(a.K / 2);
     unsigned x_off[XI];
     int x_slot[XI];
 #pragma unroll
@@ -96,14 +97,19 @@ __global__ __launch_bounds__(64 * WAVES) void mx4_few_kernel(MpArgs a) {
     }
     auto load = [&](int slot, int step) __attribute__((always_inline)) {
         char* const to = ring + slot * SLOT;
-        mp_load(c_desc, to, (c_off + 64 * step) | (4 * step + c_grp < groups ? 0u : MP_OUTSIDE));
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            mp_load(c_desc, to + r * 1024, (c_off + r * c_next + 64 * step) | (4 * step + c_grp < groups ? 0u : MP_OUTSIDE));
 #pragma unroll
         for (int q = 0; q < XI; ++q)
-            mp_load(x_desc, to + (1 + q) * 1024, (x_off[q] + 256 * step) | (4 * step + (x_slot[q] >> 2) < groups ? 0u : MP_OUTSIDE));
+            mp_load(x_desc, to + (R + q) * 1024,
+                    (x_off[q] + 256 * step) | (4 * step + (x_slot[q] >> 2) < groups ? 0u : MP_OUTSIDE));
     };
 #pragma unroll
     for (int i = 0; i < DEPTH; ++i) load(i, wv + i * WAVES);         // (past the last step: nothing is fetched)
-    f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+    f32x4 acc[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(DEPTH * NL) : "memory");
     __builtin_amdgcn_s_barrier();                            // everybody's exponents are there
     asm volatile("" ::: "memory");
@@ -112,44 +118,90 @@ __global__ __launch_bounds__(64 * WAVES) void mx4_few_kernel(MpArgs a) {
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"((DEPTH - 1) * NL) : "memory");
         const char* const from = ring + slot * SLOT;
         const int row = min(l16, 4 * XI - 1);                // (rows past M: whatever the last loaded one gives, not stored)
-        u32x4 xx[4];
-        const u32x4 cc = *reinterpret_cast<const u32x4*>(from + l16 * 64 + (g4 ^ (l16 >> 2)) * 16);
-        const uint32_t e = *reinterpret_cast<const uint8_t*>(exps + l16 * groups + min(4 * step + g4, groups - 1));
+        u32x4 cc[R], xx[4];
+        uint32_t ee[R];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) xx[c] = *reinterpret_cast<const u32x4*>(from + 1024 + row * 256 + ((4 * g4 + c) ^ row) * 16);
+        for (int r = 0; r < R; ++r) {
+            cc[r] = *reinterpret_cast<const u32x4*>(from + r * 1024 + l16 * 64 + (g4 ^ (l16 >> 2)) * 16);
+            ee[r] = *reinterpret_cast<const uint8_t*>(exps + (16 * r + l16) * groups + min(4 * step + g4, groups - 1));
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            xx[c] = *reinterpret_cast<const u32x4*>(from + R * 1024 + row * 256 + ((4 * g4 + c) ^ row) * 16);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         load(slot, step + DEPTH * WAVES);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int c = 0; c < 4; ++c)
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, mx4_values(cc[c], mx4_scale(e))),
-                                                          __builtin_bit_cast(bf16x8, xx[c]), acc, 0, 0, 0);
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, mx4_values(cc[r][c], mx4_scale(ee[r]))),
+                                                                 __builtin_bit_cast(bf16x8, xx[c]), acc[r], 0, 0, 0);
         slot = slot + 1 == DEPTH ? 0 : slot + 1;
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");          // no load may outlive the ring
     __syncthreads();
-    f32x4 (*sums)[64] = reinterpret_cast<f32x4 (*)[64]>(mp_lds);
-    sums[wv][lane] = acc;
+    f32x4 (*sums)[R][64] = reinterpret_cast<f32x4 (*)[R][64]>(mp_lds);
+#pragma unroll
+    for (int r = 0; r < R; ++r) sums[wv][r][lane] = acc[r];
     __syncthreads();
     if (!mine) return;
-    f32x4 v = sums[0][lane];
+    f32x4 v = sums[0][wv][lane];
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) v += sums[w][lane];
+    for (int w = 1; w < WAVES; ++w) v += sums[w][wv][lane];
     v += f32x4{bf16_lo(res.x), bf16_hi(res.x), bf16_lo(res.y), bf16_hi(res.y)};
     *reinterpret_cast<uint2*>(a.y + m * a.y_stride + n) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
 }
 
-template <int XI, int WAVES, int DEPTH>
+template <int R, int XI, int WAVES, int DEPTH>
 static int launch_few(const MpArgs& a, hipStream_t s) {
-    const size_t lds = mp_ring_bytes<XI, WAVES, DEPTH>() + ((size_t)a.K / 2 + 1023) / 1024 * 1024;
-    constexpr int most = mp_ring_bytes<XI, WAVES, DEPTH>() + 32768;          // (K = 2^16)
+    constexpr int ring = mp_ring_bytes<R, XI, WAVES, DEPTH>(), most = ring + R * (R == 4 ? 16384 : 32768);
+    static_assert(most <= 160 * 1024, "LDS of a CU: K = 2^16, and 2^15 with 64 rows of W");
+    const size_t lds = ring + ((size_t)a.K / 2 * R + 1023) / 1024 * 1024;
     static std::atomic<uint64_t> raised{0};
     if (lds > 65536) {
-        const int rc = mp_raise_lds(reinterpret_cast<const void*>(&mx4_few_kernel<XI, WAVES, DEPTH>), most, raised);
+        const int rc = mp_raise_lds(reinterpret_cast<const void*>(&mx4_few_kernel<R, XI, WAVES, DEPTH>), most, raised);
         if (rc) return rc;
     }
-    hipLaunchKernelGGL((mx4_few_kernel<XI, WAVES, DEPTH>), dim3(a.N / 16, (a.M + 15) / 16), dim3(64 * WAVES), lds, s, a);
+    hipLaunchKernelGGL((mx4_few_kernel<R, XI, WAVES, DEPTH>), dim3((a.N + 16 * R - 1) / (16 * R), (a.M + 15) / 16),
+                       dim3(64 * WAVES), lds, s, a);
     return launch_status("mx4_few");
+}
+
+// Which of them.  A workgroup reads its rows of x whatever it takes of W, so of more than four rows it takes as many blocks of 16
+// rows of W, up to four, as give the CUs' rounds the least cost: one up to 256 blocks, two up to 512, three (11008 rows) up to 768.
+// Up to four rows of x are cheap.  Eight wavefronts where a CU has one workgroup, columns enough for them and no more of x than
+// of W.  Measured, us, 16, 32, 48, 64 rows of W: 8 x 8192 x 8192 11.3, 9.9, -, 13; 8 x 11008 x 4096 8.8, 8.8, 7.4, 8.1; 8 x 28672 x
+// 4096 18.7, 15.8, -, 15.0; 16 x 4096 x 4096 5.4, 6.4; 16 x 8192 x 4096 8.7, 7.1, -, 8.6; 16 x 11008 x 4096 13.6, 10.7, 8.7, 9.1;
+// 16 x 14336 x 4096 15.0, 11.0, -, 9.6; 4 x 8192 x 8192 9.7, 9.5, -, 13; 4 x 11008 x 4096 7.1, 7.7, -, 7.8; 4 x 14336 x 14336 26.3,
+// 22.4, -, 22.0.  Four and eight wavefronts: 1 x 4096 x 1024 2.8, 2.9; 1 x 4096 x 8192 8.0, 6.0; 8 x 4096 x 2048 3.8, 3.7; 8 x 4096 x
+// 14336 12.3, 10.4; 16 x 4096 x 4096 5.4, 5.7.
+static float few_us(int64_t tiles, int blocks, int K) {          // of the CUs' rounds: a workgroup's x, and its rows of W
+    return (float)(((tiles + blocks - 1) / blocks + 255) / 256) * (0.234f * blocks + 0.27f) * (1e-3f * (float)K);
+}
+static int few_blocks(int64_t tiles, int K) {                // of 16 rows of W, for more than four rows of x
+    int best = 1;
+    for (int blocks = 2; blocks <= (K <= 32768 ? 4 : 3); ++blocks)           // (the rows' exponents are in LDS, too)
+        if (few_us(tiles, blocks, K) < few_us(tiles, best, K)) best = blocks;
+    return best;
+}
+
+static int launch_few_rows(const MpArgs& a, hipStream_t s) {
+    const int tiles = a.N / 16;
+    if (a.M <= 4) {
+        if (tiles <= 256) return a.K <= 1024 ? launch_few<1, 1, 4, 2>(a, s) : launch_few<1, 1, 8, 3>(a, s);
+        if (tiles <= 512 && a.K > 2048) return launch_few<2, 1, 4, 3>(a, s);
+        return tiles >= 768 && a.M > 1 ? launch_few<2, 1, 4, 2>(a, s) : launch_few<1, 1, 4, 2>(a, s);
+    }
+    const int blocks = few_blocks(tiles, a.K);
+    if (a.M <= 8) {
+        if (blocks == 1) return a.K <= 2048 ? launch_few<1, 2, 4, 2>(a, s) : launch_few<1, 2, 8, 2>(a, s);
+        if (blocks == 2) return launch_few<2, 2, 4, 3>(a, s);
+        return blocks == 3 ? launch_few<3, 2, 4, 2>(a, s) : launch_few<4, 2, 4, 2>(a, s);
+    }
+    if (blocks == 1) return launch_few<1, 4, 4, 3>(a, s);
+    if (blocks == 2) return launch_few<2, 4, 4, 2>(a, s);
+    return blocks == 3 ? launch_few<3, 4, 4, 2>(a, s) : launch_few<4, 4, 4, 2>(a, s);
 }
 
 // More rows: eight wavefronts, MT_WM by MT_WN, take 32 MB rows of x and 128 rows of W over a slice of K, 128 columns at a time,
@@ -336,12 +388,14 @@ __global__ __launch_bounds__(256) void mx4_sum_kernel(MpArgs a) {
 // Which launch: sixteen rows of x at a time, tiles of 32 mb with k in how many slices, or the matrix to bf16 and the bf16
 // projection.  By estimated time, us, fitted to fifty-odd sizes of 20 to 5500 rows with weights from HBM; on 26 others, of 300
 // to 4000 rows, it took the faster of tiles and bf16 each time but where they were within 1 %:
-//  - sixteen rows at a time: 2.5 and 2.7 for every 2^24 values of the matrix, which is read again for every sixteen;
+//  - sixteen rows at a time: 2.2, 0.5 for every 256 workgroups and for each of them a CU takes 0.5, 0.74 or 1.2 for a thousand
+//    columns (16, 32 or 64 rows of W, few_us); W is read again for every sixteen rows of x;
 //  - tiles: 4 + 0.5 mb for the launch, the first loads and the end, then rounds of 256 workgroups over the slice's steps (a CU
 //    holds two of mb = 1, which overlap); a further round costs 1 + 0.8 mb, slices 3 for the kernel that adds them up and 0.2 a MB;
 //  - by way of bf16: 8.1 for two launches, for a million values of the matrix 0.27, of y 1.4, for a thousand columns 3.6, and
 //    1.7 PFLOP/s.
-// Measured: 48 x 4096 x 4096 sixteen at a time 11.0, tiles 11.3 (mb = 1, four slices), 64 rows 12.5, 11.7; 64 x 4096 x 11008 in
+// Measured, sixteen at a time, tiles: 48 x 4096 x 4096 11.7, 12.4; 80 rows 15.8, 16.8; 24 x 4096 x 14336 20.0, 15.1; 48 x 11008 x
+// 4096 17.8, 19.5; 64 x 8192 x 4096 15.7, 14.4; 80 x 4096 x 512 6.9, 5.1 (the worst choice of 300 sizes).  64 x 4096 x 11008 in
 // eight slices 16.9 (mb = 2), in four 18.1 (mb = 1); 64 x 11008 x 4096 in one 19.2 (mb = 1), in two 20.4 (mb = 2); 200 x 4096 x
 // 4096 in one 19.2 (mb = 1), in two 20.4, in four 22.4 (mb = 2); 300 x 4096 x 4096 in four 23.4 (mb = 5), in two 24.4 (mb = 3),
 // in one 24.6 (mb = 2).  Tiles against bf16: 1024 x 4096 x 4096 40.6, 50.3; 1536 rows 66.6, 60.2; 2048 rows 80.0, 69.9; 1024 x
@@ -353,10 +407,12 @@ struct MpPlan {
 static MpPlan mp_plan(int M, int N, int K) {
     constexpr float step_us[6] = {0.f, 0.46f, 0.66f, 0.93f, 1.14f, 1.34f};
     MpPlan best{0, 1, 0, false};
-    if (M <= 16 || K < 512) return best;
+    if (M <= 16) return best;
     const int steps = (K + 127) / 128;
-    float least = 2.5f + 2.7f * (float)((M + 15) / 16) * ((float)N * (float)K / 16777216.f);
-    for (int mb = 1; mb <= 5; ++mb) {
+    const int few = few_blocks(N / 16, K);
+    const int64_t few_groups = (int64_t)((N / 16 + few - 1) / few) * ((M + 15) / 16);
+    float least = 2.24f + few_us(few_groups * few, few, K) + 0.544f * few_groups / 256;
+    for (int mb = 1; mb <= 5 && K >= 512; ++mb) {
         const int64_t tiles = (int64_t)((N + MT_BN - 1) / MT_BN) * ((M + 32 * mb - 1) / (32 * mb));
         for (int want = 1; want <= 16 && want <= steps / 4; ++want) {
             const int per = (steps + want - 1) / want, slices = (steps + per - 1) / per;       // (none of them empty)
@@ -396,11 +452,7 @@ int launch_project_mx4(const uint16_t* x, int64_t x_stride, const uint8_t* codes
                               ws_bytes > own ? static_cast<char*>(ws) + own : nullptr, ws_bytes - own, s);
     }
     if (p.mb == 0) {
-        // with more tiles than two for every CU four wavefronts each, which fit side by side (1 x 11008 x 4096 6.4, 7.1 us with
-        // eight; 1 x 4096 x 11008 7.1, 6.5); more rows keep more in flight
-        const bool many = N / 16 > 512;
-        if (M <= 4) return many ? launch_few<1, 4, 2>(a, s) : launch_few<1, 8, 3>(a, s);
-        return M <= 8 ? launch_few<2, 4, 2>(a, s) : launch_few<4, 4, 3>(a, s);
+        return launch_few_rows(a, s);
     }
     const bool cut = p.slices > 1 && scratch && !p.unpack;
     a.slices = cut ? p.slices : 1;

@@ -341,6 +341,28 @@ def test_projection(vc, M, N, K):
     project_check(vc, M, N, K, residual=(M + N // 16) % 2 == 0)
 
 
+# sixteen rows of x at a time over a matrix of more 16-row blocks than 256, 512 and 768, of which workgroups take one, two,
+# three or four (a last one that is not full), with four and eight wavefronts; and fewer than 512 columns for many rows of x
+@pytest.mark.parametrize("M,N,K", [
+    (2, 1040, 1056), (3, 4112, 2080), (4, 4112, 96), (2, 12304, 96), (1, 8224, 160), (4, 12320, 544), (7, 2064, 2080),
+    (6, 4112, 96), (8, 8240, 288), (8, 12320, 96), (16, 12304, 160), (16, 4112, 160), (13, 8272, 224), (40, 8272, 96), (31, 4144, 480),
+    (700, 4096, 256)])
+def test_projection_of_long_matrices(vc, M, N, K):
+    project_check(vc, M, N, K, residual=M % 2 == 0, seed=8)
+
+
+def test_projection_of_wide_and_long_matrices(vc):
+    # too many columns for the exponents of 64 rows: each row of the matrix as in a short one, whose sums run in the same order
+    M, N, K = 9, 12320, 32800
+    gen = torch.Generator("cuda").manual_seed(5)
+    codes = torch.randint(0, 256, (N, K // 2), dtype=torch.uint8, device="cuda", generator=gen)
+    scales = torch.randint(118, 124, (N, K // 32), dtype=torch.uint8, device="cuda", generator=gen)
+    x = dev(I.normal_bf16(1150, 0, (M, K)))
+    y = vc.vitcop_project_mx4(x, codes, scales)
+    for n in (0, 4096, N - 32):
+        assert torch.equal(y[:, n:n + 32], vc.vitcop_project_mx4(x, codes[n:n + 32], scales[n:n + 32]))
+
+
 # tiles of 32 rows of x to 160 (one, two, three, four, five times 32, as the sizes are listed), in one slice of k and in several, with
 # K a whole number of steps of 128 and not (its rows of exponents then start at every byte of a word), N no whole number of tiles
 @pytest.mark.parametrize("M,N,K", [
