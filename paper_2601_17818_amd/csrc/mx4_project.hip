@@ -174,8 +174,8 @@ static int launch_few(const MpArgs& a, hipStream_t s) {
 // of W.  Measured, us, 16, 32, 48, 64 rows of W: 8 x 8192 x 8192 11.3, 9.9, -, 13; 8 x 11008 x 4096 8.8, 8.8, 7.4, 8.1; 8 x 28672 x
 // 4096 18.7, 15.8, -, 15.0; 16 x 4096 x 4096 5.4, 6.4; 16 x 8192 x 4096 8.7, 7.1, -, 8.6; 16 x 11008 x 4096 13.6, 10.7, 8.7, 9.1;
 // 16 x 14336 x 4096 15.0, 11.0, -, 9.6; 4 x 8192 x 8192 9.7, 9.5, -, 13; 4 x 11008 x 4096 7.1, 7.7, -, 7.8; 4 x 14336 x 14336 26.3,
-// 22.4, -, 22.0.  Four and eight wavefronts: 1 x 4096 x 1024 2.8, 2.9; 1 x 4096 x 8192 8.0, 6.0; 8 x 4096 x 2048 3.8, 3.7; 8 x 4096 x
-// 14336 12.3, 10.4; 16 x 4096 x 4096 5.4, 5.7.
+// 22.4, -, 22.0.  Four and eight wavefronts: 1 x 4096 x 1024 2.8, 2.9; 1 x 4096 x 8192 8.0, 6.0; 8 x 4096 x 2048 3.8, 3.7; x 14336
+// 12.3, 10.4; 16 x 4096 x 4096 5.4, 5.7.
 static float few_us(int64_t tiles, int blocks, int K) {          // of the CUs' rounds: a workgroup's x, and its rows of W
     return (float)(((tiles + blocks - 1) / blocks + 255) / 256) * (0.234f * blocks + 0.27f) * (1e-3f * (float)K);
 }
@@ -204,25 +204,24 @@ static int launch_few_rows(const MpArgs& a, hipStream_t s) {
     return blocks == 3 ? launch_few<3, 4, 4, 2>(a, s) : launch_few<4, 4, 4, 2>(a, s);
 }
 
-// More rows: eight wavefronts, MT_WM by MT_WN, take 32 MB rows of x and 128 rows of W over a slice of K, 128 columns at a time,
-// both operands through a ring of NS steps in LDS that all of them read.  A step moves 8 (MB 4 + 2) KB from LDS and MB 8 + 8 KB
-// into it at 128 bytes a cycle (MB = 5: 1750 cycles) and multiplies 8 MB times a wavefront (1280 cycles a SIMD); without loads
-// from memory it takes 2250, with them some 3000.  Reading a step ahead into registers, between the products, gains nothing
-// (64 x 4096 x 11008 13.4, 14.0 us; 317 x 3584 x 14336 43.1, 42.8), nor do four wavefronts with twice the columns each and fewer
-// reads (14.3, 48.1), nor different starts in k (13.6, 48).  K >= 512; WHOLE: whole steps.  The slices' sums are added by
-// mx4_sum_kernel.  Measured without it, us: 32 x 4096 x 11008 10.4, 64 x 4096 x 11008 13.4, 64 x 11008 x 4096 15.8, 317 x 3584 x
-// 14336 43.1 (0.76 PFLOP/s).
-constexpr int MT_WM = 2, MT_WN = 4, MT_RT = 2, MT_WAVES = MT_WM * MT_WN, MT_BN = 16 * MT_RT * MT_WN;
-constexpr int MT_EXPS = MT_BN * 16;                  // bytes of a unit of exponents
-template <int MB, int NS>
-constexpr int mp_tile_bytes() { return NS * (16 * MB * MT_WM * 256 + MT_BN * 64) + 3 * MT_EXPS; }
+// More rows: eight wavefronts, MT_WM by MT_WN, take 32 MB rows of x and 64 RT rows of W over a slice of K, 128 columns at a time,
+// both operands through a ring of NS steps in LDS that all of them read.  A step moves 8 (4 MB + RT) KB from LDS and 8 MB + 4 RT
+// KB into it at 128 bytes a cycle (MB = 5, RT = 2: 1730 cycles) and multiplies 4 MB RT times a wavefront (1280 cycles a SIMD);
+// without loads from memory it takes 2250, with them some 3000.  RT = 4 reads x half as often (MB = 4: 1630 and 2048 cycles) and
+// reaches 1.04 PFLOP/s at 1024 x 4096 x 11008, where the chip's best is 1.2; without its reads of x, its loads, its conversions it
+// takes 8, 3 and 0 % less.  Reading a step ahead into registers, between the products, gains nothing (64 x 4096 x 11008 13.4, 14.0
+// us; 317 x 3584 x 14336 43.1, 42.8), nor do four wavefronts with twice the columns each (14.3, 48.1), nor different starts in k
+// (13.6, 48).  K >= 512; WHOLE: whole steps.  The slices' sums are added by mx4_sum_kernel.
+constexpr int MT_WM = 2, MT_WN = 4, MT_WAVES = MT_WM * MT_WN;
+template <int MB, int RT, int NS>
+constexpr int mp_tile_bytes() { return NS * (16 * MB * MT_WM * 256 + 16 * RT * MT_WN * 64) + 3 * 16 * RT * MT_WN * 16; }
 
-template <int MB, int NS, bool WHOLE>
+template <int MB, int RT, int NS, bool WHOLE>
 __global__ __launch_bounds__(64 * MT_WAVES) void mx4_tile_kernel(MpArgs a) {
-    constexpr int BM = 16 * MB * MT_WM, BN = MT_BN, RT = MT_RT;
-    // loads of x, of x and codes a wavefront and step, bytes of a step
-    constexpr int XL = BM / (4 * MT_WAVES), NL = XL + 1, SLOT = BM * 256 + BN * 64;
-    static_assert(XL * 4 * MT_WAVES == BM && 16 * MT_WAVES == BN, "whole loads for every wavefront");
+    constexpr int BM = 16 * MB * MT_WM, BN = 16 * RT * MT_WN, EXPS = BN * 16;                // (EXPS: bytes of a unit of exponents)
+    // loads of x, of codes, of both a wavefront and step, bytes of a step
+    constexpr int XL = BM / (4 * MT_WAVES), CL = BN / (16 * MT_WAVES), NL = XL + CL, SLOT = BM * 256 + BN * 64;
+    static_assert(XL * 4 * MT_WAVES == BM && CL * 16 * MT_WAVES == BN, "whole loads for every wavefront");
     extern __shared__ __attribute__((aligned(16))) char mp_lds[];
     const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wv % MT_WM, wn = wv / MT_WM;
@@ -241,7 +240,8 @@ __global__ __launch_bounds__(64 * MT_WAVES) void mx4_tile_kernel(MpArgs a) {
     const auto s_desc = mp_desc(a.scales + (int64_t)n0 * groups, s_bytes);
     const auto x_desc = mp_desc(a.x + m0 * a.x_stride, ((a.M - m0 - 1) * a.x_stride + a.K) * 2);
     const int c_grp = lane % 4 ^ (lane >> 4);
-    const unsigned c_off = (unsigned)(16 * wv + lane / 4) * (unsigned)(a.K / 2) + 16 * c_grp;
+    const unsigned c_off = (unsigned)(16 * CL * wv + lane / 4) * (unsigned)(a.K / 2) + 16 * c_grp;
+    const unsigned c_next = 16 * (unsigned)(a.K / 2);
     unsigned x_off[XL];
     int x_grp[XL];
 #pragma unroll
@@ -255,21 +255,23 @@ __global__ __launch_bounds__(64 * MT_WAVES) void mx4_tile_kernel(MpArgs a) {
         auto past = [&](int grp) __attribute__((always_inline)) {
             return step < end && (WHOLE || 4 * step + grp < groups) ? 0u : MP_OUTSIDE;
         };
-        mp_load(c_desc, to + BM * 256 + wv * 1024, (c_off + 64 * step) | past(c_grp));
+#pragma unroll
+        for (int i = 0; i < CL; ++i)
+            mp_load(c_desc, to + BM * 256 + (CL * wv + i) * 1024, (c_off + i * c_next + 64 * step) | past(c_grp));
 #pragma unroll
         for (int q = 0; q < XL; ++q) mp_load(x_desc, to + (XL * wv + q) * 1024, (x_off[q] + 256 * step) | past(x_grp[q]));
     };
     // Exponents come in units, 16 bytes of a row a lane: those of four steps, a row's last unit ending with it, or where rows
     // do not start at whole words of three, from the word on that holds the first.  Two are asked for here, and with every
     // step of a unit some rows of the one after the next.
-    constexpr int UNIT = WHOLE ? 4 : 3, ROWS = WHOLE ? BN / 4 / MT_WAVES : 6;                // steps; rows a wavefront and step
-    static_assert(MT_EXPS == 2048 && MT_WAVES >= 4 && ROWS * MT_WAVES * UNIT >= BN, "two loads a unit");
+    constexpr int UNIT = WHOLE ? 4 : 3, ROWS = (BN + UNIT * MT_WAVES - 1) / (UNIT * MT_WAVES);       // steps; rows a wavefront
+    static_assert(2 * BN / 64 <= MT_WAVES && ROWS <= 64, "two units in one load each");
     char* const scales = mp_lds + NS * SLOT;
     auto unit_at = [&](int row, int unit) __attribute__((always_inline)) {
         return WHOLE ? row * groups + min(4 * first + 16 * unit, groups - 16)
                      : min((row * groups + 4 * first + 12 * unit) & ~3, s_bytes - 16);
     };
-    if (wv < 4) mp_load(s_desc, scales + wv * 1024, (unsigned)unit_at(wv % 2 * 64 + lane, wv / 2));
+    if (wv < 2 * BN / 64) mp_load(s_desc, scales + wv * 1024, (unsigned)unit_at(wv % (BN / 64) * 64 + lane, wv / (BN / 64)));
     f32x4 acc[RT][MB];
 #pragma unroll
     for (int r = 0; r < RT; ++r)
@@ -285,7 +287,7 @@ __global__ __launch_bounds__(64 * MT_WAVES) void mx4_tile_kernel(MpArgs a) {
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         const char* const from = mp_lds + slot * SLOT;
-        const char* const exps = scales + exp_slot * MT_EXPS;
+        const char* const exps = scales + exp_slot * EXPS;
         const int grp = WHOLE ? 4 * step + g4 : min(4 * step + g4, groups - 1);
         u32x4 cc[RT], xx[MB][4];
         uint32_t ee[RT];
@@ -302,7 +304,7 @@ __global__ __launch_bounds__(64 * MT_WAVES) void mx4_tile_kernel(MpArgs a) {
                 xx[j][c] = *reinterpret_cast<const u32x4*>(from + (16 * (MB * wm + j) + l16) * 256 + ((4 * g4 + c) ^ l16) * 16);
         const int e_row = ROWS * (MT_WAVES * phase + wv);
         if (lane < ROWS && e_row + lane < BN)
-            mp_load(s_desc, scales + (exp_slot == 0 ? 2 : exp_slot - 1) * MT_EXPS + e_row * 16,
+            mp_load(s_desc, scales + (exp_slot == 0 ? 2 : exp_slot - 1) * EXPS + e_row * 16,
                     (unsigned)unit_at(e_row + lane, unit + 2));
         load(ahead, step + NS - 1);
         if (++phase == UNIT) {
@@ -342,22 +344,22 @@ __global__ __launch_bounds__(64 * MT_WAVES) void mx4_tile_kernel(MpArgs a) {
         }
 }
 
-template <int MB, int NS, bool WHOLE>
+template <int MB, int RT, int NS, bool WHOLE>
 static int launch_tiles_of(const MpArgs& a, hipStream_t s) {
-    const int tiles = (a.N + MT_BN - 1) / MT_BN * ((a.M + 32 * MB - 1) / (32 * MB)) * a.slices;
-    constexpr int lds = mp_tile_bytes<MB, NS>();
+    const int tiles = (a.N + 16 * RT * MT_WN - 1) / (16 * RT * MT_WN) * ((a.M + 32 * MB - 1) / (32 * MB)) * a.slices;
+    constexpr int lds = mp_tile_bytes<MB, RT, NS>();
     static_assert(lds <= 160 * 1024, "LDS of a CU");
     static_assert(lds > 65536, "raised for all of them");
     static std::atomic<uint64_t> raised{0};
-    const int rc = mp_raise_lds(reinterpret_cast<const void*>(&mx4_tile_kernel<MB, NS, WHOLE>), lds, raised);
+    const int rc = mp_raise_lds(reinterpret_cast<const void*>(&mx4_tile_kernel<MB, RT, NS, WHOLE>), lds, raised);
     if (rc) return rc;
-    hipLaunchKernelGGL((mx4_tile_kernel<MB, NS, WHOLE>), dim3((tiles + 7) / 8 * 8), dim3(64 * MT_WAVES), lds, s, a);
+    hipLaunchKernelGGL((mx4_tile_kernel<MB, RT, NS, WHOLE>), dim3((tiles + 7) / 8 * 8), dim3(64 * MT_WAVES), lds, s, a);
     return launch_status("mx4_tile");
 }
 
-template <int MB, int NS>
+template <int MB, int RT, int NS>
 static int launch_tiles(const MpArgs& a, hipStream_t s) {
-    return a.K % 128 == 0 ? launch_tiles_of<MB, NS, true>(a, s) : launch_tiles_of<MB, NS, false>(a, s);
+    return a.K % 128 == 0 ? launch_tiles_of<MB, RT, NS, true>(a, s) : launch_tiles_of<MB, RT, NS, false>(a, s);
 }
 
 // y = the slices' sums added up in their order (+ residual): four columns of a row a thread, eight slices' loads and the
@@ -386,43 +388,55 @@ __global__ __launch_bounds__(256) void mx4_sum_kernel(MpArgs a) {
 }
 
 // Which launch: sixteen rows of x at a time, tiles of 32 mb with k in how many slices, or the matrix to bf16 and the bf16
-// projection.  By estimated time, us, fitted to fifty-odd sizes of 20 to 5500 rows with weights from HBM; on 26 others, of 300
-// to 4000 rows, it took the faster of tiles and bf16 each time but where they were within 1 %:
+// projection.  By estimated time, us, fitted to some 400 sizes of 17 to 5500 rows with weights from HBM, where it loses
+// 0.7 % against the better of the three:
 //  - sixteen rows at a time: 2.2, 0.5 for every 256 workgroups and for each of them a CU takes 0.5, 0.74 or 1.2 for a thousand
 //    columns (16, 32 or 64 rows of W, few_us); W is read again for every sixteen rows of x;
-//  - tiles: 4 + 0.5 mb for the launch, the first loads and the end, then rounds of 256 workgroups over the slice's steps (a CU
-//    holds two of mb = 1, which overlap); a further round costs 1 + 0.8 mb, slices 3 for the kernel that adds them up and 0.2 a MB;
+//  - tiles: 2 + rt + 0.5 mb for the launch, the first loads and the end, then rounds of 256 workgroups over the slice's steps (a
+//    CU holds two of the smallest, which overlap); a further round costs 1 + 0.4 mb rt, a MB of y 0.15, slices 3 for the kernel
+//    that adds them up and 0.2 a MB;
 //  - by way of bf16: 8.1 for two launches, for a million values of the matrix 0.27, of y 1.4, for a thousand columns 3.6, and
 //    1.7 PFLOP/s.
 // Measured, sixteen at a time, tiles: 48 x 4096 x 4096 11.7, 12.4; 80 rows 15.8, 16.8; 24 x 4096 x 14336 20.0, 15.1; 48 x 11008 x
-// 4096 17.8, 19.5; 64 x 8192 x 4096 15.7, 14.4; 80 x 4096 x 512 6.9, 5.1 (the worst choice of 300 sizes).  64 x 4096 x 11008 in
-// eight slices 16.9 (mb = 2), in four 18.1 (mb = 1); 64 x 11008 x 4096 in one 19.2 (mb = 1), in two 20.4 (mb = 2); 200 x 4096 x
-// 4096 in one 19.2 (mb = 1), in two 20.4, in four 22.4 (mb = 2); 300 x 4096 x 4096 in four 23.4 (mb = 5), in two 24.4 (mb = 3),
-// in one 24.6 (mb = 2).  Tiles against bf16: 1024 x 4096 x 4096 40.6, 50.3; 1536 rows 66.6, 60.2; 2048 rows 80.0, 69.9; 1024 x
-// 11008 x 4096 116, 103; 2251 x 6112 x 7968 264, 200; 634 x 1904 x 9984 37, 48; 3978 x 1088 x 4192 52.7, 55.3.
+// 4096 17.8, 19.5; 64 x 8192 x 4096 15.7, 14.4; 80 x 4096 x 512 6.9, 5.1 (the worst choice of 300 sizes).  Tiles of 128 and of 256
+// rows of W: 317 x 3584 x 14336 48.4, 47.7; 128 x 4096 x 4096 16.5, 21.6; 640 x 4096 x 11008 68.7, 63.7; 1024 x 4096 x 4096 37.3,
+// 43.8; x 11008 95.1, 88.2; 1536 x 4096 x 4096 58.9, 48.7; 1024 x 3584 x 14336 120, 106.  64 x 4096 x 11008 in eight slices 16.9,
+// in four 18.1; 64 x 11008 x 4096 in one 19.2, in two 20.4; 200 x 4096 x 4096 in one 19.2, in two 20.4; 300 x 4096 x 4096 in four
+// 23.4, in two 24.4, in one 24.6.  Tiles, bf16: 1024 x 4096 x 4096 40.1, 50.1; 2048 rows 64.7, 67.9; 2251 x 6112 x 7968 236, 199;
+// 3955 x 2128 x 12352 225, 185; 634 x 1904 x 9984 37, 47; 3978 x 1088 x 4192 54.7, 55.1.
+struct MpKind {                          // of tiles: 32 mb rows of x by 64 rt rows of W, us a step of 128 columns
+    int mb, rt;
+    float step_us;
+};
+constexpr MpKind mp_kinds[] = {{1, 2, 0.46f}, {2, 2, 0.66f}, {3, 2, 0.93f}, {4, 2, 1.14f}, {5, 2, 1.34f},
+                               {3, 4, 1.35f}, {4, 4, 1.72f}, {5, 4, 2.15f}};
 struct MpPlan {
-    int mb, slices, steps_per_slice;     // mb == 0: mx4_few_kernel
+    int kind, slices, steps_per_slice;   // kind < 0: mx4_few_kernel
     bool unpack;                         // the matrix to bf16 first, if there is scratch for it
 };
 static MpPlan mp_plan(int M, int N, int K) {
-    constexpr float step_us[6] = {0.f, 0.46f, 0.66f, 0.93f, 1.14f, 1.34f};
-    MpPlan best{0, 1, 0, false};
+    MpPlan best{-1, 1, 0, false};
     if (M <= 16) return best;
     const int steps = (K + 127) / 128;
     const int few = few_blocks(N / 16, K);
     const int64_t few_groups = (int64_t)((N / 16 + few - 1) / few) * ((M + 15) / 16);
     float least = 2.24f + few_us(few_groups * few, few, K) + 0.544f * few_groups / 256;
-    for (int mb = 1; mb <= 5 && K >= 512; ++mb) {
-        const int64_t tiles = (int64_t)((N + MT_BN - 1) / MT_BN) * ((M + 32 * mb - 1) / (32 * mb));
-        for (int want = 1; want <= 16 && want <= steps / 4; ++want) {
-            const int per = (steps + want - 1) / want, slices = (steps + per - 1) / per;       // (none of them empty)
+    for (int kind = 0; kind < 8 && K >= 512; ++kind) {
+        const int mb = mp_kinds[kind].mb, rt = mp_kinds[kind].rt;
+        const int64_t tiles = (int64_t)((N + 64 * rt - 1) / (64 * rt)) * ((M + 32 * mb - 1) / (32 * mb));
+        const float fixed = 2.f + rt + 0.5f * mb + 0.3e-6f * (float)M * (float)N;
+        for (int want = 1, last = 0; want <= 16 && want <= steps / 4 && (want == 1 || tiles * want <= 1024); ++want) {
+            const int per = (steps + want - 1) / want;
+            if (per == last) continue;
+            last = per;
+            const int slices = (steps + per - 1) / per;                                        // (none of them empty)
             const int64_t rounds = (tiles * slices + 255) / 256;
             const float overlap = rounds > 1 && mb == 1 ? 0.84f : 1.f;
-            float us = 4.f + 0.5f * mb + (float)rounds * overlap * per * step_us[mb] + (1.f + 0.8f * mb) * (rounds - 1);
+            float us = fixed + (float)rounds * overlap * per * mp_kinds[kind].step_us + (1.f + 0.4f * mb * rt) * (rounds - 1);
             if (slices > 1) us += 3.f + 0.8e-6f * slices * (float)M * (float)N;
             if (us < least) {
                 least = us;
-                best = {mb, slices, per, false};
+                best = {kind, slices, per, false};
             }
         }
     }
@@ -431,18 +445,18 @@ static MpPlan mp_plan(int M, int N, int K) {
     return best;
 }
 
-size_t project_mx4_workspace_bytes(int M, int N, int K) {
-    const MpPlan p = mp_plan(M, N, K);
+static size_t plan_bytes(const MpPlan& p, int M, int N, int K) {
     if (p.unpack) return up256((size_t)N * K * 2) + gemm_workspace_bytes(M, N, K);
     return p.slices > 1 ? up256((size_t)p.slices * M * N * 4) : 0;
 }
+size_t project_mx4_workspace_bytes(int M, int N, int K) { return plan_bytes(mp_plan(M, N, K), M, N, K); }
 
 int launch_project_mx4(const uint16_t* x, int64_t x_stride, const uint8_t* codes, const uint8_t* scales, uint16_t* y,
                        int64_t y_stride, const uint16_t* res, int64_t res_stride, int M, int N, int K, void* ws,
                        size_t ws_bytes, hipStream_t s) {
     MpArgs a{x, codes, scales, y, res, x_stride, y_stride, res_stride, M, N, K, nullptr, 1, 0};
     const MpPlan p = mp_plan(M, N, K);
-    const bool scratch = ws_bytes >= project_mx4_workspace_bytes(M, N, K);
+    const bool scratch = ws_bytes >= plan_bytes(p, M, N, K);
     if (p.unpack && scratch) {
         uint16_t* w = static_cast<uint16_t*>(ws);
         const size_t own = up256((size_t)N * K * 2);
@@ -451,20 +465,21 @@ int launch_project_mx4(const uint16_t* x, int64_t x_stride, const uint8_t* codes
         return launch_gemm_ws(x, x_stride, w, y, y_stride, res, res_stride, M, N, K, nullptr,
                               ws_bytes > own ? static_cast<char*>(ws) + own : nullptr, ws_bytes - own, s);
     }
-    if (p.mb == 0) {
-        return launch_few_rows(a, s);
-    }
+    if (p.kind < 0) return launch_few_rows(a, s);
     const bool cut = p.slices > 1 && scratch && !p.unpack;
     a.slices = cut ? p.slices : 1;
     a.steps_per_slice = cut ? p.steps_per_slice : (K + 127) / 128;
     if (cut) a.part = static_cast<float*>(ws);
     int rc = 0;
-    switch (p.mb) {
-        case 1: rc = launch_tiles<1, 4>(a, s); break;
-        case 2: rc = launch_tiles<2, 4>(a, s); break;
-        case 3: rc = launch_tiles<3, 3>(a, s); break;
-        case 4: rc = launch_tiles<4, 3>(a, s); break;
-        default: rc = launch_tiles<5, 3>(a, s); break;
+    switch (p.kind) {
+        case 0: rc = launch_tiles<1, 2, 4>(a, s); break;
+        case 1: rc = launch_tiles<2, 2, 4>(a, s); break;
+        case 2: rc = launch_tiles<3, 2, 3>(a, s); break;
+        case 3: rc = launch_tiles<4, 2, 3>(a, s); break;
+        case 4: rc = launch_tiles<5, 2, 3>(a, s); break;
+        case 5: rc = launch_tiles<3, 4, 3>(a, s); break;
+        case 6: rc = launch_tiles<4, 4, 3>(a, s); break;
+        default: rc = launch_tiles<5, 4, 2>(a, s); break;
     }
     if (rc || !cut) return rc;
     hipLaunchKernelGGL(mx4_sum_kernel, dim3((unsigned)(((int64_t)M * (N / 4) + 255) / 256)), dim3(256), 0, s, a);

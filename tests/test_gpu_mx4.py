@@ -345,8 +345,8 @@ def test_projection(vc, M, N, K):
 # three or four (a last one that is not full), with four and eight wavefronts; and fewer than 512 columns for many rows of x
 @pytest.mark.parametrize("M,N,K", [
     (2, 1040, 1056), (3, 4112, 2080), (4, 4112, 96), (2, 12304, 96), (1, 8224, 160), (4, 12320, 544), (7, 2064, 2080),
-    (6, 4112, 96), (8, 8240, 288), (8, 12320, 96), (16, 12304, 160), (16, 4112, 160), (13, 8272, 224), (40, 8272, 96), (31, 4144, 480),
-    (700, 4096, 256)])
+    (6, 4112, 96), (8, 8240, 288), (8, 12320, 96), (16, 12304, 160), (16, 4112, 160), (13, 8272, 224), (40, 8272, 96),
+    (31, 4144, 480), (700, 4096, 256)])
 def test_projection_of_long_matrices(vc, M, N, K):
     project_check(vc, M, N, K, residual=M % 2 == 0, seed=8)
 
@@ -363,26 +363,30 @@ def test_projection_of_wide_and_long_matrices(vc):
         assert torch.equal(y[:, n:n + 32], vc.vitcop_project_mx4(x, codes[n:n + 32], scales[n:n + 32]))
 
 
-# tiles of 32 rows of x to 160 (one, two, three, four, five times 32, as the sizes are listed), in one slice of k and in several, with
-# K a whole number of steps of 128 and not (its rows of exponents then start at every byte of a word), N no whole number of tiles
+# tiles of 32 rows of x to 160 by 128 and by 256 rows of the matrix, in one slice of k and in several, with K a whole number of
+# steps of 128 and not (its rows of exponents then start at every byte of a word), N no whole number of tiles
 @pytest.mark.parametrize("M,N,K", [
     (317, 2272, 608), (316, 640, 4448), (306, 464, 6784), (323, 608, 5632), (20, 8208, 4352), (294, 3392, 640), (313, 448, 6976),
     (320, 672, 4864), (328, 6288, 544), (323, 1472, 3168), (284, 1040, 6656), (329, 1424, 6208), (322, 1520, 6144),
-    (297, 2256, 4448), (318, 2304, 4480)])
+    (297, 2256, 4448), (318, 2304, 4480), (298, 8224, 512), (259, 3696, 544), (328, 5440, 512), (524, 6736, 544), (388, 8240, 512),
+    (210, 1488, 512), (399, 6624, 544), (99, 5584, 3840), (109, 5424, 4512), (101, 5408, 4608), (130, 3088, 7296),
+    (99, 4160, 5056), (132, 2848, 7008), (129, 6720, 5760), (690, 8208, 576), (674, 8240, 640), (131, 8272, 4320),
+    (65, 6640, 5728), (489, 8208, 512), (67, 6560, 5760), (516, 8272, 544), (110, 8304, 4480), (100, 8208, 4416),
+    (129, 6608, 6784), (141, 8240, 5152)])
 def test_projection_on_tiles(vc, M, N, K):
     project_check(vc, M, N, K, residual=M % 2 == 0, seed=7, one_slice=True)
 
 
 # many rows over a short matrix: tiles in several rounds; over a larger one: the matrix to bf16 first, and the same
 # with no scratch, tiles in several rounds
-@pytest.mark.parametrize("M,N,K,unpacked", [(8192, 1024, 1024, False), (5003, 2064, 1056, True)])
+@pytest.mark.parametrize("M,N,K,unpacked", [(8192, 1024, 1024, False), (5003, 2064, 1056, True), (5003, 2064, 2080, True)])
 def test_projection_of_many_rows(vc, M, N, K, unpacked):
     assert (vc.lib.vitcop_project_mx4_workspace_bytes(M, N, K) >= 2 * N * K) == unpacked
     project_check(vc, M, N, K, residual=M % 2 == 1, seed=9, one_slice=True)
 
 
 def test_projection_of_many_rows_strided_and_in_place(vc):
-    M, N, K = 2600, 2064, 2080
+    M, N, K = 2600, 4112, 2080
     assert vc.lib.vitcop_project_mx4_workspace_bytes(M, N, K) >= 2 * N * K
     codes, scales = vc.vitcop_mx4_quantize(dev(I.normal_bf16(1110, 0, (N, K))))
     x = torch.full((M, K + 64), float("nan"), dtype=torch.bfloat16, device="cuda")
