@@ -564,7 +564,7 @@ int vitcop_decode_attn_mx4(const uint16_t* q, const vitcop_cache_mx4_t* C, uint1
  *   residual: NULL, or [M,N] bf16; row strides in elements, multiples of 8
  *   ws: NULL, or device scratch of ws_bytes >= vitcop_project_mx4_workspace_bytes(M,N,K) (16-byte aligned, 0 for
  *   at most 16 rows): some more rows leave most of the chip idle unless k is cut into slices, whose fp32 sums live
- *   there and are added in a fixed order, and for thousands of rows the matrix goes to bf16 there first; without
+ *   there and are added in a fixed order, and of many rows the matrix may go to bf16 there first; without
  *   scratch, or with too little, one slice does it all
  * K % 32 == 0, N % 16 == 0, K <= 2^16, M <= 2^19, M*x_row_stride < 2^30, N*K < 2^31. */
 size_t vitcop_project_mx4_workspace_bytes(int M, int N, int K);

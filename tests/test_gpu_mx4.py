@@ -551,6 +551,44 @@ def test_captured_and_on_another_stream(vc):
         assert torch.equal(layer(hs[i]), want[i])
 
 
+def test_two_graphs_of_calls_with_workspaces(vc):
+    # sliced attention, a sliced projection and one by way of bf16, in two graphs on inputs of their own, replayed in turn and
+    # at once on two streams, with eager calls between
+    B, N, Hq, Hkv, d = 3, 2000, 8, 2, 128
+    t = I.qkv_tensors(1600, B, N, Hq, Hkv, d)
+    cache = vc.CacheMx4.empty(B, N, Hkv, d)
+    vc.vitcop_cache_mx4_write(cache, dev(t["k"]), dev(t["v"]))
+    matrices = [vc.vitcop_mx4_quantize(dev(I.normal_bf16(1601, i, shape, std=0.02)))
+                for i, shape in enumerate([(640, 4448), (4096, 256)])]
+    rows = (316, 700)
+    assert vc.lib.vitcop_decode_attn_mx4_workspace_bytes(B, N, Hq, Hkv, d) > 0
+    assert all(vc.lib.vitcop_project_mx4_workspace_bytes(m, c.shape[0], 2 * c.shape[1]) > 0 for m, (c, _) in zip(rows, matrices))
+
+    def calls(q, xs):
+        return [vc.vitcop_decode_attn_mx4(q, cache, N)[0]] + [vc.vitcop_project_mx4(x, *w) for x, w in zip(xs, matrices)]
+
+    inputs = [(dev(I.normal_bf16(1610 + i, 0, (B, Hq, d))),
+               [dev(I.normal_bf16(1620 + i, j, (m, 2 * matrices[j][0].shape[1]))) for j, m in enumerate(rows)]) for i in range(2)]
+    want = [[y.clone() for y in calls(*x)] for x in inputs]
+    graphs, outputs, streams = [], [], [torch.cuda.Stream() for _ in range(2)]
+    for x in inputs:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            outputs.append(calls(*x))
+    torch.cuda.synchronize()
+    for turn in range(4):
+        for g, side in zip(graphs, streams):
+            if turn % 2 == 0:
+                g.replay()
+            else:
+                with torch.cuda.stream(side):
+                    g.replay()
+        eager = calls(*inputs[turn % 2])
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for got, ref in zip(outputs, want) for a, b in zip(got, ref)), turn
+        assert all(torch.equal(a, b) for a, b in zip(eager, want[turn % 2])), turn
+
+
 def test_the_binding_refuses(vc):
     x = torch.zeros((4, 64), dtype=torch.bfloat16, device="cuda")
     codes, scales = vc.vitcop_mx4_quantize(x)
