@@ -10,8 +10,11 @@
 //  - V has to be turned (a product's operand holds one channel of several keys): its bf16 rows go through LDS and come back
 //    transposed (ds_read_b64_tr_b16).  The key of element 4 t + r of a lane's 8 is 16 t + 4 (lane / 16) + r, which is where
 //    the scores are.
-//  - A probability is the sum of two bf16 (16 bits, off by at most 2^-16 of itself), one product for each: one alone would add an
-//    error as large as the rounding of the output.
+//  - The probabilities stay 32-bit: each is the sum of three bf16, its first, second and last eight bits.  Up to five heads have
+//    them side by side in the columns of one product (heads in columns 0 to 4, 5 to 9 and 10 to 14, which otherwise would repeat
+//    one), up to eight in those of two, more in one product for each; the columns' sums meet at the end.
+//    (us, by this rule and with three products: 64 x 1536 keys x 32 heads 74.3, 88.9; 4 x 65536 x 28 / 4 31.3, 35.0; 4 x 60000 x 16
+//    heads of 64 56.4, 66.5.)
 //  - The running reference of the softmax moves only when a score exceeds it by 2^8, which is rare after the first tiles; until
 //    then no lane needs to know another's scores.  Sums, references and outputs are fp32.
 // mx4_merge_kernel combines the slices; a single slice is finished on the spot.
@@ -25,21 +28,38 @@ namespace vitcop {
 constexpr int MA_MAX_G = 16, MA_KEYS = 32;
 constexpr float MA_SLACK = 8.f;              // log2
 
+// The first eight bits of a positive number (those `kept`), the rest, and the first eight of two numbers as a pair of bf16.
+__device__ __forceinline__ float ma_first(float x, uint32_t kept = 0xFFFF0000u) {
+    return __uint_as_float(__float_as_uint(x) & kept);
+}
+__device__ __forceinline__ float ma_rest(float x) { return x - ma_first(x); }
+__device__ __forceinline__ uint32_t ma_pair(float x, float y) {
+    return __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
+}
+// x + the value of the lane COLUMNS to the right in the row of 16
+template <int COLUMNS>
+__device__ __forceinline__ float ma_plus(float x, float of) {
+    return x + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(of), 0x100 + COLUMNS, 0xF, 0xF, true));      // row_shl
+}
+
 // what a head without any key gives: zeros, and minus infinity as the logarithm of its sum
 __device__ __forceinline__ float mx4_quotient(float o, float l) { return l == 0.f ? 0.f : o / l; }
 __device__ __forceinline__ float mx4_lse(float m, float l) {
     return l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
-// WAVES wavefronts, 32 keys at a time each, share the slice (attn_plan: how many).  Registers for three workgroups of four on a
-// CU, two of eight.
-template <int D, int WAVES>
+// the columns of a product that a part of the probabilities takes, by the number of products
+constexpr int ma_columns(int products) { return products == 1 ? 5 : (products == 2 ? 8 : 16); }
+
+// WAVES wavefronts, 32 keys at a time each, share the slice (attn_plan: how many), PRODUCTS: of a tile's probabilities with V.
+// Registers for three workgroups of four on a CU, two of eight.
+template <int D, int WAVES, int PRODUCTS>
 __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 3) void mx4_attn_kernel(
     const uint16_t* __restrict__ q, const uint8_t* __restrict__ k_codes, const uint8_t* __restrict__ k_scales,
     const uint8_t* __restrict__ v_codes, const uint8_t* __restrict__ v_scales, float* __restrict__ part_o,
     float* __restrict__ part_ml, int capacity, int N, int Hq, int Hkv, int g0, int G, float scale_log2e, int keys_per_split,
     int n_splits, const int32_t* __restrict__ n_samples, uint16_t* __restrict__ out, float* __restrict__ lse) {
-    constexpr int STEPS = D / 32, BLOCKS = D / 16;
+    constexpr int STEPS = D / 32, BLOCKS = D / 16, COLUMNS = ma_columns(PRODUCTS);
     constexpr int ROW = D / 2, GROUPS = D / MX4_GROUP;               // bytes of a row of codes, of exponents
     constexpr int VROW = 2 * D + 32;                                 // bytes of a V row in LDS: the pad keeps eight rows apart
     constexpr int LPR = ROW / 16, RPL = 64 / LPR, VL = MA_KEYS / RPL;         // V: lanes a row, rows a load, loads a tile
@@ -81,15 +101,17 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 3) void mx4_attn_kerne
         }
     };
     if (first < slice_end) load(first);                      // (before it is known how many rows the sample has)
-    bf16x8 qf[STEPS];                                        // Q^T of head l16 (heads past G: head G - 1), channels as K's
+    const int head = l16 % COLUMNS, part0 = l16 / COLUMNS;   // of this lane's column; the part of a probability it takes first
+    const uint32_t past0 = part0 > 0 ? 0xFFFF0000u : 0u, past1 = part0 > 1 ? 0xFFFF0000u : 0u;
+    bf16x8 qf[STEPS];                                        // Q^T of the head (heads past G: head G - 1), channels as K's
 #pragma unroll
     for (int c = 0; c < STEPS; ++c)
-        qf[c] = *reinterpret_cast<const bf16x8*>(q + ((int64_t)b * Hq + h0 + min(l16, G - 1)) * D + D / 4 * g4 + 8 * c);
+        qf[c] = *reinterpret_cast<const bf16x8*>(q + ((int64_t)b * Hq + h0 + min(head, G - 1)) * D + D / 4 * g4 + 8 * c);
     const int key_end = n_samples ? min(slice_end, max(n_samples[b], 0)) : slice_end;
     f32x4 o[BLOCKS];
 #pragma unroll
     for (int i = 0; i < BLOCKS; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.f;                            // of head l16 (m for all its keys, l over this lane's)
+    float m = -INFINITY, l = 0.f;                            // of the head (m for all its keys, l over this lane's)
     typedef __attribute__((ext_vector_type(4))) short s16x4;
     typedef __attribute__((ext_vector_type(8))) short s16x8;
     char* const mine = vt[wv];
@@ -141,15 +163,21 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 3) void mx4_attn_kerne
                 for (int r = 0; r < 4; ++r) o[i][r] *= alpha;
         }
         const float base = m == -INFINITY ? 0.f : m;         // (nothing but -inf so far: 0, not NaN)
-        u32x4 part[2];
+        u32x4 part[PRODUCTS];                                // of each pair of probabilities
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const float a = __builtin_amdgcn_exp2f(p[2 * e] - base), c = __builtin_amdgcn_exp2f(p[2 * e + 1] - base);
             l += a;
             l += c;
-            const uint32_t w = pack_bf16(a, c);
-            part[0][e] = w;
-            part[1][e] = pack_bf16(a - bf16_lo(w), c - bf16_hi(w));
+            const float a1 = ma_rest(a), c1 = ma_rest(c);
+            if constexpr (PRODUCTS == 1) {
+                const float ar = a - ma_first(a, past0), cr = c - ma_first(c, past0);
+                part[0][e] = ma_pair(ar - ma_first(ar, past1), cr - ma_first(cr, past1));
+            } else {
+                part[0][e] = PRODUCTS == 2 && part0 ? ma_pair(a1, c1) : ma_pair(a, c);
+                if constexpr (PRODUCTS == 3) part[1][e] = ma_pair(a1, c1);
+                part[PRODUCTS - 1][e] = PRODUCTS == 2 && part0 ? 0u : ma_pair(ma_rest(a1), ma_rest(c1));
+            }
         }
         __builtin_amdgcn_wave_barrier();                     // (one wavefront's LDS accesses stay in order)
 #pragma unroll
@@ -160,13 +188,20 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 3) void mx4_attn_kerne
                 (__attribute__((address_space(3))) s16x4*)(uintptr_t)(tr + i * 32 + 16 * VROW));
             const bf16x8 vf = __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
+            for (int n = 0; n < PRODUCTS; ++n)
                 o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, part[n]), o[i], 0, 0, 0);
         }
         __builtin_amdgcn_wave_barrier();                     // the next tile's rows replace these
     }
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
+    if constexpr (PRODUCTS < 3) {                            // the parts' columns, least first
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                o[i][r] = PRODUCTS == 1 ? ma_plus<5>(o[i][r], ma_plus<5>(o[i][r], o[i][r])) : ma_plus<8>(o[i][r], o[i][r]);
+    }
     __shared__ float sm[WAVES][MA_MAX_G][2];
     float (&so)[WAVES][MA_MAX_G][D] = *reinterpret_cast<float (*)[WAVES][MA_MAX_G][D]>(&vt[0][0]);
     __syncthreads();                                         // all are done with V
@@ -320,6 +355,12 @@ size_t decode_mx4_workspace_bytes(int B, int N, int Hq, int Hkv, int d) {
     return s == 1 ? 0 : up256((size_t)B * Hq * s * d * 4) + up256((size_t)B * Hq * s * 2 * 4);
 }
 
+template <int D, int PRODUCTS>
+static auto* attn_kernel(int waves) {
+    return waves == 8 ? mx4_attn_kernel<D, 8, PRODUCTS>
+                      : (waves == 4 ? mx4_attn_kernel<D, 4, PRODUCTS> : mx4_attn_kernel<D, 2, PRODUCTS>);
+}
+
 template <int D>
 static int launch_attn_d(const uint16_t* q, const vitcop_cache_mx4_t& C, uint16_t* out, float* lse, int N,
                          const int32_t* n_samples, int Hq, float scale, void* ws, hipStream_t s) {
@@ -327,10 +368,12 @@ static int launch_attn_d(const uint16_t* q, const vitcop_cache_mx4_t& C, uint16_
     const AttnPlan p = attn_plan(B, N, C.Hkv, D);
     float* po = static_cast<float*>(ws);
     float* pml = reinterpret_cast<float*>(static_cast<char*>(ws) + up256((size_t)B * Hq * p.splits * D * 4));
-    auto* kernel = p.waves == 8 ? mx4_attn_kernel<D, 8> : (p.waves == 4 ? mx4_attn_kernel<D, 4> : mx4_attn_kernel<D, 2>);
     for (int g0 = 0; g0 < group; g0 += MA_MAX_G) {
+        const int G = std::min(MA_MAX_G, group - g0);
+        auto* kernel = G <= ma_columns(1) ? attn_kernel<D, 1>(p.waves)
+                                          : (G <= ma_columns(2) ? attn_kernel<D, 2>(p.waves) : attn_kernel<D, 3>(p.waves));
         hipLaunchKernelGGL(kernel, dim3(p.splits, C.Hkv, B), dim3(64 * p.waves), 0, s, q, C.k_codes, C.k_scales, C.v_codes,
-                           C.v_scales, po, pml, C.capacity, N, Hq, C.Hkv, g0, std::min(MA_MAX_G, group - g0),
+                           C.v_scales, po, pml, C.capacity, N, Hq, C.Hkv, g0, G,
                            scale * 1.4426950408889634f, p.keys_per_split, p.splits, n_samples, p.splits == 1 ? out : nullptr, lse);
         const int rc = launch_status("mx4_attn");
         if (rc) return rc;
