@@ -32,6 +32,9 @@ int launch_status(const char* kernel_name) { return hip_status(hipGetLastError()
 
 static inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// n * stride <= most, of non-negative n and stride whose product may not fit 64 bits
+static inline bool at_most(int64_t n, int64_t stride, int64_t most) { return n == 0 || stride <= most / n; }
+
 struct Carver {   // hands out 256-byte aligned pieces of the caller's workspace
     char* base;
     size_t used = 0;
@@ -249,7 +252,7 @@ int vitcop_project(const uint16_t* x, int64_t x_row_stride, const uint16_t* w, u
             VITCOP_EINVAL, "project: strides (%lld, %lld)", (long long)x_row_stride, (long long)y_row_stride);
     REQUIRE(!residual || (res_row_stride >= N && res_row_stride % 8 == 0), VITCOP_EINVAL,
             "project: residual stride %lld", (long long)res_row_stride);
-    REQUIRE((int64_t)M * x_row_stride < ((int64_t)1 << 31) && (int64_t)N * K < ((int64_t)1 << 31),
+    REQUIRE(at_most(M, x_row_stride, INT32_MAX) && (int64_t)N * K < ((int64_t)1 << 31),
             VITCOP_EUNSUPPORTED, "project: operand larger than 2^31 elements (4 GiB)");
     if (M == 0 || N == 0) return VITCOP_OK;
     REQUIRE(x && w && y, VITCOP_EINVAL, "project: null pointer");
@@ -550,9 +553,9 @@ int vitcop_vic_cluster(const uint16_t* feats, int64_t feat_row_stride, int64_t f
         REQUIRE(aligned16(feats) && aligned16(pos) && aligned16(dist_out), VITCOP_EINVAL,
                 "vic_cluster: feats, pos and dist_out must be 16-byte aligned");
         REQUIRE(feat_row_stride >= D && feat_row_stride % 8 == 0 && feat_batch_stride % 8 == 0 &&
-                    (B == 1 || feat_batch_stride >= (int64_t)n * feat_row_stride),
+                    (B == 1 || at_most(n, feat_row_stride, feat_batch_stride)),
                 VITCOP_EINVAL, "vic_cluster: strides");
-        REQUIRE((int64_t)n * feat_row_stride < (1LL << 31), VITCOP_EUNSUPPORTED,
+        REQUIRE(at_most(n, feat_row_stride, INT32_MAX), VITCOP_EUNSUPPORTED,
                 "vic_cluster: one image's features must stay below 2^31 elements");
         const size_t need = vic_workspace_bytes(B, n);
         REQUIRE(ws && ws_bytes >= need, VITCOP_EWORKSPACE, "vic_cluster: workspace %zu < %zu", ws_bytes, need);
@@ -587,7 +590,7 @@ int vitcop_collab_prune_merge(const uint16_t* feats, int64_t feat_row_stride, in
         REQUIRE(aligned16(feats) && aligned16(out_feats), VITCOP_EINVAL,
                 "collab_prune_merge: feats and out_feats must be 16-byte aligned");
         REQUIRE(feat_row_stride >= D && feat_row_stride % 8 == 0 && feat_batch_stride % 8 == 0 &&
-                    (B == 1 || feat_batch_stride >= (int64_t)n * feat_row_stride),
+                    (B == 1 || at_most(n, feat_row_stride, feat_batch_stride)),
                 VITCOP_EINVAL, "collab_prune_merge: strides");
     }
     const size_t need = collab_workspace_bytes(B, n);
@@ -1447,7 +1450,7 @@ int vitcop_project_mx4(const uint16_t* x, int64_t x_row_stride, const uint8_t* w
             "project_mx4: strides (%lld, %lld)", (long long)x_row_stride, (long long)y_row_stride);
     REQUIRE(!residual || (res_row_stride >= N && res_row_stride % 8 == 0), VITCOP_EINVAL, "project_mx4: residual stride %lld",
             (long long)res_row_stride);
-    REQUIRE((int64_t)M * x_row_stride < ((int64_t)1 << 30), VITCOP_EUNSUPPORTED, "project_mx4: x of 2^30 elements and more");
+    REQUIRE(at_most(M, x_row_stride, (1 << 30) - 1), VITCOP_EUNSUPPORTED, "project_mx4: x of 2^30 elements and more");
     if (M == 0 || N == 0) return VITCOP_OK;
     REQUIRE(x && w_codes && w_scales && y, VITCOP_EINVAL, "project_mx4: null pointer");
     REQUIRE(aligned16(x) && aligned16(w_codes) && aligned16(w_scales) && aligned16(y) && aligned16(residual) && aligned16(ws),
