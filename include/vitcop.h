@@ -537,7 +537,7 @@ typedef struct {
  *        (clamped to [0,T]) rows of sample b are written: a right-padded batch.
  * All other rows of the cache stay as they were.  start + T <= capacity is checked; of start_samples, rows
  * outside [0,capacity) are skipped on the device.  A decoding step appends with T = 1.
- * B*Hkv*(T/8+1) < 2^26, here and when reading. */
+ * B*Hkv*(T/8+1) <= 2^26 - 4, here and when reading. */
 int vitcop_cache_mx4_write(const vitcop_cache_mx4_t* C, const uint16_t* k, const uint16_t* v, int64_t row_stride,
                            int64_t batch_stride, int T, int start, const int32_t* start_samples,
                            const int32_t* n_samples, void* stream);

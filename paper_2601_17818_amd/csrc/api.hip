@@ -1367,8 +1367,9 @@ static int check_cache_mx4_rows(const char* what, const vitcop_cache_mx4_t* C, c
     REQUIRE(T >= 0, VITCOP_EINVAL, "%s: T=%d", what, T);
     REQUIRE(start_samples || (start >= 0 && (int64_t)start + T <= C->capacity), VITCOP_EINVAL,
             "%s: rows [%d,%lld) outside [0,%d)", what, start, (long long)start + T, C->capacity);
-    REQUIRE((int64_t)C->B * C->Hkv * (T / 8 + 1) < ((int64_t)1 << 26), VITCOP_EUNSUPPORTED, "%s: B*Hkv*(T/8+1) of 2^26 and more",
-            what);
+    // (a wavefront each, four to a workgroup: the launch stays below 2^32 threads)
+    REQUIRE((int64_t)C->B * C->Hkv * (T / 8 + 1) <= ((int64_t)1 << 26) - 4, VITCOP_EUNSUPPORTED,
+            "%s: B*Hkv*(T/8+1) above 2^26 - 4", what);
     if (C->B == 0 || T == 0) return VITCOP_OK;
     REQUIRE(k || v, VITCOP_EINVAL, "%s: k and v are both null", what);
     REQUIRE(aligned16(k) && aligned16(v), VITCOP_EINVAL, "%s: k and v must be 16-byte aligned", what);

@@ -35,3 +35,13 @@ def test_features_whose_rows_wrap():
     for call in (cluster, merge):
         assert call(2, 256, 64, 256 * 64) == EWORKSPACE and call(2, 256, 64, 256 * 64 - 8) == EINVAL
         assert call(2, 256, 1 << 56, 64) == EINVAL
+
+
+# Four wavefronts to a workgroup of 256 threads: 2^24 workgroups would be 2^32 threads, one more than a launch may have.
+@pytest.mark.parametrize("B,Hkv,blocks,code", [(1, 1, (1 << 26) - 4, EINVAL), (1, 1, (1 << 26) - 3, EUNSUPPORTED),
+                                               (4, 3, 5592405, EINVAL), (2731, 3, 8191, EUNSUPPORTED), (1, 1, 1 << 26, EUNSUPPORTED)])
+def test_rows_of_a_cache(B, Hkv, blocks, code):
+    C, T = vc.CacheMx4T(B, 64, Hkv, 128, A, A, A, A), 8 * blocks - 1
+    assert T // 8 + 1 == blocks
+    assert lib.vitcop_cache_mx4_write(C, None, None, 384, 1024, T, 0, A, None, None) == code
+    assert lib.vitcop_cache_mx4_read(C, None, None, T, 0, A, None) == code
