@@ -915,6 +915,9 @@ def vitcop_cache_mx4_write(cache: CacheMx4, k, v, start: int = 0, start_samples=
     if k_rows is not None and k_rows != v_rows:
         if k_rows[0] != v_rows[0]:
             raise ValueError("k and v differ in their number of rows")
+        for t, name, (_, row, batch) in ((k, "k", k_rows), (v, "v", v_rows)):        # (before either call writes)
+            if row % 8 or batch % 8 or t.data_ptr() % 16:
+                raise ValueError(f"{name}: strides of {row} and {batch} elements must be multiples of 8, its address of 16 bytes")
         vitcop_cache_mx4_write(cache, k, None, start, start_samples, n_samples)      # strides of their own: two calls
         vitcop_cache_mx4_write(cache, None, v, start, start_samples, n_samples)
         return
