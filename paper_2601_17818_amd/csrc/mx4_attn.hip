@@ -20,12 +20,12 @@
 // mx4_merge_kernel combines the slices; a single slice is finished on the spot.
 #include "vitcop_internal.h"
 #include "mx4_device.h"
+#include "mx4_plan.h"
 
 #include <algorithm>
 
 namespace vitcop {
 
-constexpr int MA_MAX_G = 16, MA_KEYS = 32;
 constexpr float MA_SLACK = 8.f;              // log2
 
 // The first eight bits of a positive number (those `kept`), the rest, and the first eight of two numbers as a pair of bf16.
@@ -47,9 +47,6 @@ __device__ __forceinline__ float mx4_quotient(float o, float l) { return l == 0.
 __device__ __forceinline__ float mx4_lse(float m, float l) {
     return l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
-
-// the columns of a product that a part of the probabilities takes, by the number of products
-constexpr int ma_columns(int products) { return products == 1 ? 5 : (products == 2 ? 8 : 16); }
 
 // WAVES wavefronts, 32 keys at a time each, share the slice (attn_plan: how many), PRODUCTS: of a tile's probabilities with V.
 // Registers for three workgroups of four on a CU, two of eight.
@@ -300,56 +297,6 @@ __global__ __launch_bounds__(MM_THREADS) void mx4_merge_kernel(const float* __re
     if (lse && c == 0) lse[bh] = mx4_lse(mn, l);
 }
 
-// How many slices of the keys and wavefronts to a slice.  A workgroup costs some two microseconds before its first and after
-// its last key, the merge of slices three to four; a CU draws 31 KB/us (rows of 64: 22) with eight wavefronts on it, the chip
-// 6.2 TB/s, 24 KB/us a CU.  Measured, us (pairs of a sample and a KV head x keys, of 128 or of 64):
-//  - up to 128 pairs, one slice for up to 800 keys (128 x 1000 9.5 in four, 9.2 in one; 32 x 640 6.4, in three 7.3); above, slices
-//    of 256 to 512 keys take four wavefronts (32 x 1500 in six, with four and eight wavefronts 7.7, 7.9); longer ones, of fewer
-//    than 32 pairs, eight, one workgroup to a CU (16 x 65536 in 32 with four and in 16 with eight 30.0, 29.5), and of more
-//    pairs four, three to a CU, which come out even where 256 is no multiple of the pairs (96 x 15000 in two, eight wavefronts
-//    47.4, in eight, four 37.8; 64 x 40000 63.1, 58.9; of 64 43.9, 39.9).
-//  - up to 512 pairs, slices of four wavefronts where some CUs would have a workgroup more than others for long enough to pay
-//    for the merge (one slice, sliced: 132 x 1800 12.6, 13.0; x 7200 36.6, 29.7; 232 x 7200 40.5, 42.3; 280 x 3600 35.0, 31.8;
-//    340 x 14400 129, 110; of 64 86, 69; 512 x 14400 159, 159).
-//  - of one slice the more pairs there are, the fewer wavefronts, and the more keys, the more: two, four, eight 640 x 150 7.0, 7.3,
-//    9.5; 640 x 650 17.8, 14.8, 16.5; 1500 x 300 16.2, 16.5, 18.9; 1500 x 650 29.8, 26.7, 30.1; 3000 x 450 36.2, 37.5, 45.1;
-//    3000 x 1000 73.5, 67.2, 76.4; four, eight 280 x 900 13.0, 13.4; 420 x 7200 76.8, 70.7; of 64 760 x 7200 76.3, 69.9; and none
-//    of them to be without a key.
-struct AttnPlan {
-    int waves, keys_per_split, splits;
-};
-static AttnPlan attn_plan(int B, int N, int Hkv, int d) {
-    const int64_t pairs = (int64_t)B * Hkv;
-    AttnPlan p{8, 0, 1};
-    if (pairs <= 128 && N > 800) {
-        p.waves = 4;
-        p.splits = (int)std::min<int64_t>(512 / pairs, (N + 255) / 256);
-        if ((N + p.splits - 1) / p.splits > 512)
-            p = pairs < 32 ? AttnPlan{8, 0, (int)(256 / pairs)} : AttnPlan{4, 0, (int)(768 / pairs)};
-    } else if (pairs <= 512 && N > 800) {
-        const float pair_us = (float)N * (float)(d * 17 / 16) / (d == 64 ? 22e3f : 31e3f);          // of a CU
-        const float chip_us = (float)pairs * (float)N * (float)(d * 17 / 16) / 6.2e6f;
-        float least = 1e30f;
-        for (int s = 1; s <= 4; ++s) {
-            const float us = std::max(chip_us, pair_us / s * (float)((pairs * s + 255) / 256)) + (s > 1 ? 4.f : 0.f);
-            if (us < least) {
-                least = us;
-                p.splits = s;
-            }
-        }
-        if (p.splits > 1) p.waves = 4;
-    }
-    if (p.splits == 1) {
-        if (pairs > 256 && (N <= 1500 || pairs > (d == 64 ? 1024 : 512))) p.waves = 4;
-        if ((pairs > 768 && N <= (pairs > 2048 ? 800 : 400)) || (pairs > 512 && N <= 160)) p.waves = 2;
-        while (p.waves > 2 && (p.waves / 2) * MA_KEYS >= N) p.waves /= 2;
-    }
-    const int64_t unit = p.waves * MA_KEYS, keys = (N + p.splits - 1) / p.splits;
-    p.keys_per_split = (int)std::min<int64_t>(std::max<int64_t>(1, (keys + unit - 1) / unit) * unit, INT32_MAX);
-    p.splits = (int)std::max<int64_t>(1, ((int64_t)N + p.keys_per_split - 1) / p.keys_per_split);
-    return p;
-}
-
 size_t decode_mx4_workspace_bytes(int B, int N, int Hq, int Hkv, int d) {
     const size_t s = attn_plan(B, N, Hkv, d).splits;
     return s == 1 ? 0 : up256((size_t)B * Hq * s * d * 4) + up256((size_t)B * Hq * s * 2 * 4);
@@ -370,8 +317,9 @@ static int launch_attn_d(const uint16_t* q, const vitcop_cache_mx4_t& C, uint16_
     float* pml = reinterpret_cast<float*>(static_cast<char*>(ws) + up256((size_t)B * Hq * p.splits * D * 4));
     for (int g0 = 0; g0 < group; g0 += MA_MAX_G) {
         const int G = std::min(MA_MAX_G, group - g0);
-        auto* kernel = G <= ma_columns(1) ? attn_kernel<D, 1>(p.waves)
-                                          : (G <= ma_columns(2) ? attn_kernel<D, 2>(p.waves) : attn_kernel<D, 3>(p.waves));
+        const int products = attn_products(G);
+        auto* kernel = products == 1 ? attn_kernel<D, 1>(p.waves)
+                                     : (products == 2 ? attn_kernel<D, 2>(p.waves) : attn_kernel<D, 3>(p.waves));
         hipLaunchKernelGGL(kernel, dim3(p.splits, C.Hkv, B), dim3(64 * p.waves), 0, s, q, C.k_codes, C.k_scales, C.v_codes,
                            C.v_scales, po, pml, C.capacity, N, Hq, C.Hkv, g0, G,
                            scale * 1.4426950408889634f, p.keys_per_split, p.splits, n_samples, p.splits == 1 ? out : nullptr, lse);

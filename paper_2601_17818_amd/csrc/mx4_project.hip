@@ -12,6 +12,7 @@
 // lie in different banks.  Columns past K and rows past M or N read as zeros: their offsets lie past the descriptors' ends.
 #include "vitcop_internal.h"
 #include "mx4_device.h"
+#include "mx4_plan.h"
 
 #include <algorithm>
 #include <atomic>
@@ -168,40 +169,22 @@ static int launch_few(const MpArgs& a, hipStream_t s) {
     return launch_status("mx4_few");
 }
 
-// Which of them.  A workgroup reads its rows of x whatever it takes of W, so of more than four rows it takes as many blocks of 16
-// rows of W, up to four, as give the CUs' rounds the least cost: one up to 256 blocks, two up to 512, three (11008 rows) up to 768.
-// Up to four rows of x are cheap.  Eight wavefronts where a CU has one workgroup, columns enough for them and no more of x than
-// of W.  Measured, us, 16, 32, 48, 64 rows of W: 8 x 8192 x 8192 11.3, 9.9, -, 13; 8 x 11008 x 4096 8.8, 8.8, 7.4, 8.1; 8 x 28672 x
-// 4096 18.7, 15.8, -, 15.0; 16 x 4096 x 4096 5.4, 6.4; 16 x 8192 x 4096 8.7, 7.1, -, 8.6; 16 x 11008 x 4096 13.6, 10.7, 8.7, 9.1;
-// 16 x 14336 x 4096 15.0, 11.0, -, 9.6; 4 x 8192 x 8192 9.7, 9.5, -, 13; 4 x 11008 x 4096 7.1, 7.7, -, 7.8; 4 x 14336 x 14336 26.3,
-// 22.4, -, 22.0.  Four and eight wavefronts: 1 x 4096 x 1024 2.8, 2.9; 1 x 4096 x 8192 8.0, 6.0; 8 x 4096 x 2048 3.8, 3.7; x 14336
-// 12.3, 10.4; 16 x 4096 x 4096 5.4, 5.7.
-static float few_us(int64_t tiles, int blocks, int K) {          // of the CUs' rounds: a workgroup's x, and its rows of W
-    return (float)(((tiles + blocks - 1) / blocks + 255) / 256) * (0.234f * blocks + 0.27f) * (1e-3f * (float)K);
+// the kernel of few_plan, which is one of these
+template <int R, int XI, int WAVES, int DEPTH>
+static bool launched(const FewPlan& p, const MpArgs& a, hipStream_t s, int& rc) {
+    if (p.blocks != R || p.x_loads != XI || p.waves != WAVES || p.depth != DEPTH) return false;
+    rc = launch_few<R, XI, WAVES, DEPTH>(a, s);
+    return true;
 }
-static int few_blocks(int64_t tiles, int K) {                // of 16 rows of W, for more than four rows of x
-    int best = 1;
-    for (int blocks = 2; blocks <= (K <= 32768 ? 4 : 3); ++blocks)           // (the rows' exponents are in LDS, too)
-        if (few_us(tiles, blocks, K) < few_us(tiles, best, K)) best = blocks;
-    return best;
-}
-
 static int launch_few_rows(const MpArgs& a, hipStream_t s) {
-    const int tiles = a.N / 16;
-    if (a.M <= 4) {
-        if (tiles <= 256) return a.K <= 1024 ? launch_few<1, 1, 4, 2>(a, s) : launch_few<1, 1, 8, 3>(a, s);
-        if (tiles <= 512 && a.K > 2048) return launch_few<2, 1, 4, 3>(a, s);
-        return tiles >= 768 && a.M > 1 ? launch_few<2, 1, 4, 2>(a, s) : launch_few<1, 1, 4, 2>(a, s);
-    }
-    const int blocks = few_blocks(tiles, a.K);
-    if (a.M <= 8) {
-        if (blocks == 1) return a.K <= 2048 ? launch_few<1, 2, 4, 2>(a, s) : launch_few<1, 2, 8, 2>(a, s);
-        if (blocks == 2) return launch_few<2, 2, 4, 3>(a, s);
-        return blocks == 3 ? launch_few<3, 2, 4, 2>(a, s) : launch_few<4, 2, 4, 2>(a, s);
-    }
-    if (blocks == 1) return launch_few<1, 4, 4, 3>(a, s);
-    if (blocks == 2) return launch_few<2, 4, 4, 2>(a, s);
-    return blocks == 3 ? launch_few<3, 4, 4, 2>(a, s) : launch_few<4, 4, 4, 2>(a, s);
+    const FewPlan p = few_plan(a.M, a.N, a.K);
+    int rc = VITCOP_EUNSUPPORTED;
+    launched<1, 1, 4, 2>(p, a, s, rc) || launched<1, 1, 8, 3>(p, a, s, rc) || launched<2, 1, 4, 3>(p, a, s, rc) ||
+        launched<2, 1, 4, 2>(p, a, s, rc) || launched<1, 2, 4, 2>(p, a, s, rc) || launched<1, 2, 8, 2>(p, a, s, rc) ||
+        launched<2, 2, 4, 3>(p, a, s, rc) || launched<3, 2, 4, 2>(p, a, s, rc) || launched<4, 2, 4, 2>(p, a, s, rc) ||
+        launched<1, 4, 4, 3>(p, a, s, rc) || launched<2, 4, 4, 2>(p, a, s, rc) || launched<3, 4, 4, 2>(p, a, s, rc) ||
+        launched<4, 4, 4, 2>(p, a, s, rc);
+    return rc;
 }
 
 // More rows: eight wavefronts, MT_WM by MT_WN, take 32 MB rows of x and 64 RT rows of W over a slice of K, 128 columns at a time,
@@ -385,64 +368,6 @@ __global__ __launch_bounds__(256) void mx4_sum_kernel(MpArgs a) {
     }
     v += f32x4{bf16_lo(res.x), bf16_hi(res.x), bf16_lo(res.y), bf16_hi(res.y)};
     *reinterpret_cast<uint2*>(a.y + m * a.y_stride + n) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
-}
-
-// Which launch: sixteen rows of x at a time, tiles of 32 mb with k in how many slices, or the matrix to bf16 and the bf16
-// projection.  By estimated time, us, fitted to some 400 sizes of 17 to 5500 rows with weights from HBM, where it loses
-// 0.7 % against the better of the three:
-//  - sixteen rows at a time: 2.2, 0.5 for every 256 workgroups and for each of them a CU takes 0.5, 0.74 or 1.2 for a thousand
-//    columns (16, 32 or 64 rows of W, few_us); W is read again for every sixteen rows of x;
-//  - tiles: 2 + rt + 0.5 mb for the launch, the first loads and the end, then rounds of 256 workgroups over the slice's steps (a
-//    CU holds two of the smallest, which overlap); a further round costs 1 + 0.4 mb rt, a MB of y 0.15, slices 3 for the kernel
-//    that adds them up and 0.2 a MB;
-//  - by way of bf16: 8.1 for two launches, for a million values of the matrix 0.27, of y 1.4, for a thousand columns 3.6, and
-//    1.7 PFLOP/s.
-// Measured, sixteen at a time, tiles: 48 x 4096 x 4096 11.7, 12.4; 80 rows 15.8, 16.8; 24 x 4096 x 14336 20.0, 15.1; 48 x 11008 x
-// 4096 17.8, 19.5; 64 x 8192 x 4096 15.7, 14.4; 80 x 4096 x 512 6.9, 5.1 (the worst choice of 300 sizes).  Tiles of 128 and of 256
-// rows of W: 317 x 3584 x 14336 48.4, 47.7; 128 x 4096 x 4096 16.5, 21.6; 640 x 4096 x 11008 68.7, 63.7; 1024 x 4096 x 4096 37.3,
-// 43.8; x 11008 95.1, 88.2; 1536 x 4096 x 4096 58.9, 48.7; 1024 x 3584 x 14336 120, 106.  64 x 4096 x 11008 in eight slices 16.9,
-// in four 18.1; 64 x 11008 x 4096 in one 19.2, in two 20.4; 200 x 4096 x 4096 in one 19.2, in two 20.4; 300 x 4096 x 4096 in four
-// 23.4, in two 24.4, in one 24.6.  Tiles, bf16: 1024 x 4096 x 4096 40.1, 50.1; 2048 rows 64.7, 67.9; 2251 x 6112 x 7968 236, 199;
-// 3955 x 2128 x 12352 225, 185; 634 x 1904 x 9984 37, 47; 3978 x 1088 x 4192 54.7, 55.1.
-struct MpKind {                          // of tiles: 32 mb rows of x by 64 rt rows of W, us a step of 128 columns
-    int mb, rt;
-    float step_us;
-};
-constexpr MpKind mp_kinds[] = {{1, 2, 0.46f}, {2, 2, 0.66f}, {3, 2, 0.93f}, {4, 2, 1.14f}, {5, 2, 1.34f},
-                               {3, 4, 1.35f}, {4, 4, 1.72f}, {5, 4, 2.15f}};
-struct MpPlan {
-    int kind, slices, steps_per_slice;   // kind < 0: mx4_few_kernel
-    bool unpack;                         // the matrix to bf16 first, if there is scratch for it
-};
-static MpPlan mp_plan(int M, int N, int K) {
-    MpPlan best{-1, 1, 0, false};
-    if (M <= 16) return best;
-    const int steps = (K + 127) / 128;
-    const int few = few_blocks(N / 16, K);
-    const int64_t few_groups = (int64_t)((N / 16 + few - 1) / few) * ((M + 15) / 16);
-    float least = 2.24f + few_us(few_groups * few, few, K) + 0.544f * few_groups / 256;
-    for (int kind = 0; kind < 8 && K >= 512; ++kind) {
-        const int mb = mp_kinds[kind].mb, rt = mp_kinds[kind].rt;
-        const int64_t tiles = (int64_t)((N + 64 * rt - 1) / (64 * rt)) * ((M + 32 * mb - 1) / (32 * mb));
-        const float fixed = 2.f + rt + 0.5f * mb + 0.3e-6f * (float)M * (float)N;
-        for (int want = 1, last = 0; want <= 16 && want <= steps / 4 && (want == 1 || tiles * want <= 1024); ++want) {
-            const int per = (steps + want - 1) / want;
-            if (per == last) continue;
-            last = per;
-            const int slices = (steps + per - 1) / per;                                        // (none of them empty)
-            const int64_t rounds = (tiles * slices + 255) / 256;
-            const float overlap = rounds > 1 && mb == 1 ? 0.84f : 1.f;
-            float us = fixed + (float)rounds * overlap * per * mp_kinds[kind].step_us + (1.f + 0.4f * mb * rt) * (rounds - 1);
-            if (slices > 1) us += 3.f + 0.8e-6f * slices * (float)M * (float)N;
-            if (us < least) {
-                least = us;
-                best = {kind, slices, per, false};
-            }
-        }
-    }
-    const float m = (float)M, n = (float)N, k = (float)K;
-    best.unpack = 8.1f + 0.274e-6f * n * k + 1.38e-6f * m * n + 3.55e-3f * k + 1.19e-9f * m * n * k < least;
-    return best;
 }
 
 static size_t plan_bytes(const MpPlan& p, int M, int N, int K) {

@@ -4,10 +4,12 @@ import pytest
 import torch
 
 import vitcop_inputs as I
+from oracle import mx4_oracle as X
 from oracle import vitcop_oracle as O
 from gpu_util import dev, host_f64
 
 pytestmark = pytest.mark.gpu
+EPS = 2.0 ** -24
 
 
 @pytest.fixture(scope="module")
@@ -65,3 +67,36 @@ def test_a_probability_keeps_its_bits(vc, B, N, Hq, Hkv, d, at, top):
     other, other_lse = vc.vitcop_decode_attn(dev(q), kk, vv, scale=1.0)
     assert (np.abs(host_f64(other) - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -21).all()
     assert torch.equal(torch.isnan(got), torch.isnan(other)) and (lse - other_lse).abs().max() <= 2.0 ** -20
+
+
+# Every number of wavefronts, sliced and not, and of products with V (up to 5, 8 and 16 query heads a pass; 17: two passes).
+# Samples attend over all rows, none, a third (so that slices, and wavefronts of a slice, have no key) and 33 of them.
+@pytest.mark.parametrize("B,N,Hq,Hkv,d", [
+    (4, 50, 12, 1, 64), (4, 60, 8, 1, 128), (4, 61, 9, 1, 128), (4, 100, 6, 1, 64), (4, 110, 32, 2, 64), (4, 300, 14, 2, 64),
+    (4, 300, 6, 1, 128), (4, 1000, 8, 1, 64), (4, 1100, 22, 2, 64), (4, 1030, 7, 1, 128), (31, 8500, 3, 1, 64), (31, 8500, 7, 1, 64),
+    (31, 8500, 17, 1, 64), (7, 9500, 4, 4, 128), (7, 9500, 28, 4, 128), (31, 8500, 17, 1, 128), (15, 9300, 30, 2, 64)])
+def test_slices_and_wavefronts(vc, B, N, Hq, Hkv, d):
+    rows = [I.normal_bf16(N + Hq, i, (4, N, Hkv, d)) for i in range(2)]
+    q4 = I.normal_bf16(N + Hq, 2, (4, Hq, d))
+    of = np.arange(B) % 4
+    q = dev(np.ascontiguousarray(q4[of]))
+    cache = vc.CacheMx4.empty(B, N, Hkv, d)
+    vc.vitcop_cache_mx4_write(cache, dev(rows[0])[of], dev(rows[1])[of])
+    kv = [X.round_trip(x).transpose(0, 2, 1, 3) for x in rows]
+    for lens in (None, [N, 0, N // 3, 33]):
+        if lens is not None:
+            for b in range(B):
+                for t in (cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales):
+                    t[b, :, lens[b % 4]:] = 255                          # not a number, and not looked at
+        n = None if lens is None else torch.tensor([lens[b % 4] for b in range(B)], dtype=torch.int32, device="cuda")
+        o, lse = vc.vitcop_decode_attn_mx4(q, cache, N, n)
+        ref, ref_lse, spread, size = (x[of] for x in X.decode_attention(q4, kv[0], kv[1], lens))
+        # a score is off by (d + 4) 2^-24 of its products' magnitudes, a probability by that and the exponential's last bits
+        p_off = (d + 4) * EPS * size + 2.0 ** -20 + N * EPS
+        got, got_lse, live = host_f64(o), lse.cpu().numpy().astype(np.float64), ~np.isneginf(ref_lse)
+        assert np.array_equal(np.isneginf(got_lse), ~live) and not got[~live].any()
+        assert (np.abs(got - ref) <= 2.0 ** -8 * np.abs(ref) + 2 * p_off[..., None] * spread)[live].all()
+        assert (np.abs(got_lse[live] - ref_lse[live]) <= p_off[live] + 2.0 ** -22 * (1 + np.abs(ref_lse[live]))).all()
+        first, first_lse = o[:4].clone(), lse[:4].clone()
+        for b in range(4, B):                                             # equal samples, equal results
+            assert torch.equal(o[b], first[b % 4]) and torch.equal(lse[b], first_lse[b % 4])
