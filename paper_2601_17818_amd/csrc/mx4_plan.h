@@ -17,30 +17,37 @@ constexpr int attn_products(int heads) { return heads <= ma_columns(1) ? 1 : (he
 
 // How many slices of the keys and wavefronts to a slice.  A workgroup costs some two microseconds before its first and after
 // its last key, the merge of slices three to four; a CU draws 31 KB/us (rows of 64: 22) with eight wavefronts on it, the chip
-// 6.2 TB/s, 24 KB/us a CU.  Measured, us (pairs of a sample and a KV head x keys, of 128 or of 64):
-//  - up to 128 pairs, one slice for up to 800 keys (128 x 1000 9.5 in four, 9.2 in one; 32 x 640 6.4, in three 7.3); above, slices
-//    of 256 to 512 keys take four wavefronts (32 x 1500 in six, with four and eight wavefronts 7.7, 7.9); longer ones, of fewer
-//    than 32 pairs, eight, one workgroup to a CU (16 x 65536 in 32 with four and in 16 with eight 30.0, 29.5), and of more
+// 6.2 TB/s, 24 KB/us a CU.  Measured, us a call of captured ones, over caches of 600 MB in turn (pairs of a sample and a KV head
+// x keys, of 128 or of 64, one query head):
+//  - up to 128 pairs, one slice for up to one_slice_keys (in one, in slices: 32 x 650 7.5, 7.7; 32 x 1000 8.9, 7.8; 128 x 801 8.3,
+//    9.4; 128 x 1200 10.3, 10.6; 128 x 1500 11.6, 10.9; of 64 32 x 1000 7.0, 7.1; 128 x 1200 8.0, 8.9; 128 x 2000 10.5, 9.9); above,
+//    slices of 256 to 512 keys take four wavefronts (32 x 1500 in six, with four and eight wavefronts 7.9, 8.1); longer ones, of
+//    fewer than 32 pairs, eight, one workgroup to a CU (16 x 65536 in 32 with four and in 16 with eight 28.9, 28.5), and of more
 //    pairs four, three to a CU, which come out even where 256 is no multiple of the pairs (96 x 15000 in two, eight wavefronts
-//    47.4, in eight, four 37.8; 64 x 40000 63.1, 58.9; of 64 43.9, 39.9).
+//    45.5, in eight, four 38.2; 64 x 40000 60.9, 60.0; of 64 42.7, 39.2).
 //  - up to 512 pairs, slices of four wavefronts where some CUs would have a workgroup more than others for long enough to pay
-//    for the merge (one slice, sliced: 132 x 1800 12.6, 13.0; x 7200 36.6, 29.7; 232 x 7200 40.5, 42.3; 280 x 3600 35.0, 31.8;
-//    340 x 14400 129, 110; of 64 86, 69; 512 x 14400 159, 159).
-//  - of one slice the more pairs there are, the fewer wavefronts, and the more keys, the more: two, four, eight 640 x 150 7.0, 7.3,
-//    9.5; 640 x 650 17.8, 14.8, 16.5; 1500 x 300 16.2, 16.5, 18.9; 1500 x 650 29.8, 26.7, 30.1; 3000 x 450 36.2, 37.5, 45.1;
-//    3000 x 1000 73.5, 67.2, 76.4; four, eight 280 x 900 13.0, 13.4; 420 x 7200 76.8, 70.7; of 64 760 x 7200 76.3, 69.9; and none
+//    for the merge (one slice, the plan's: 132 x 1800 12.6, 12.6; x 7200 35.8, 29.2; 232 x 7200 40.7, 40.7 (in three 42.5); 280 x 3600
+//    34.8, 31.6; 340 x 14400 131, 113 (in three 108); of 64 87, 68; 512 x 14400 157, 157).
+//  - of one slice the more pairs there are, the fewer wavefronts, and the more keys, the more: two, four, eight 640 x 150 7.1, 7.5,
+//    9.7; 640 x 650 16.5, 14.6, 16.4; 1500 x 300 16.0, 16.6, 19.4; 1500 x 650 27.9, 26.8, 29.5; 3000 x 450 35.9, 35.9, 44.0;
+//    3000 x 1000 71.8, 68.2, 76.8; four, eight 280 x 900 12.9, 13.6; 420 x 7200 78.0, 71.1; of 64 760 x 7200 76.6, 69.9; and none
 //    of them to be without a key.
+inline int64_t one_slice_keys(int64_t pairs, int d) {
+    return d == 64 ? 1000 + 4 * pairs : 750 + std::max<int64_t>(0, pairs - 60) * 15 / 2;
+}
 struct AttnPlan {
     int waves, keys_per_split, splits;
 };
 inline AttnPlan attn_plan(int B, int N, int Hkv, int d) {
     const int64_t pairs = (int64_t)B * Hkv;
     AttnPlan p{8, 0, 1};
-    if (pairs <= 128 && N > 800) {
-        p.waves = 4;
-        p.splits = (int)std::min<int64_t>(512 / pairs, (N + 255) / 256);
-        if ((N + p.splits - 1) / p.splits > 512)
-            p = pairs < 32 ? AttnPlan{8, 0, (int)(256 / pairs)} : AttnPlan{4, 0, (int)(768 / pairs)};
+    if (pairs <= 128) {
+        if (N > one_slice_keys(pairs, d)) {
+            p.waves = 4;
+            p.splits = (int)std::min<int64_t>(512 / pairs, (N + 255) / 256);
+            if ((N + p.splits - 1) / p.splits > 512)
+                p = pairs < 32 ? AttnPlan{8, 0, (int)(256 / pairs)} : AttnPlan{4, 0, (int)(768 / pairs)};
+        }
     } else if (pairs <= 512 && N > 800) {
         const float pair_us = (float)N * (float)(d * 17 / 16) / (d == 64 ? 22e3f : 31e3f);          // of a CU
         const float chip_us = (float)pairs * (float)N * (float)(d * 17 / 16) / 6.2e6f;

@@ -106,3 +106,15 @@ def test_slices_of_k(plan):
             if kind >= 0:
                 total = (K + 127) // 128
                 assert slices * steps >= total and (slices - 1) * steps < total and (slices == 1 or steps >= 4)
+
+
+@pytest.mark.parametrize("pairs,N,d,sliced", [
+    # us in one slice and in slices: 7.6, 7.9; 8.8, 7.5; 8.2, 9.2; 9.1, 9.3; 10.1, 9.4; 10.3, 10.6; 11.6, 10.9
+    (64, 650, 128, False), (16, 1000, 128, True), (96, 801, 128, False), (96, 1000, 128, False), (96, 1200, 128, True),
+    (128, 1200, 128, False), (128, 1500, 128, True),
+    # 6.2, 6.8; 7.6, 7.0; 7.1, 7.4; 8.7, 8.0; 8.0, 8.9; 10.5, 9.9
+    (16, 801, 64, False), (16, 1200, 64, True), (64, 1000, 64, False), (64, 1500, 64, True), (128, 1200, 64, False),
+    (128, 2000, 64, True)])
+def test_few_keys_are_not_sliced(plan, pairs, N, d, sliced):
+    for B, Hkv in ((pairs, 1), (pairs // 8, 8)):
+        assert (walked(plan.attn, 3, B, N, Hkv, d)[1] > 1) == sliced
