@@ -74,14 +74,18 @@ inline AttnPlan attn_plan(int B, int N, int Hkv, int d) {
 
 // ---- projections by a matrix (mx4_project.hip) ------------------------------------------------------------------
 
-// Which of them.  A workgroup reads its rows of x whatever it takes of W, so of more than four rows it takes as many blocks of 16
-// rows of W, up to four, as give the CUs' rounds the least cost: one up to 256 blocks, two up to 512, three (11008 rows) up to 768.
-// Up to four rows of x are cheap.  Eight wavefronts where a CU has one workgroup, columns enough for them and no more of x than
-// of W.  Measured, us, 16, 32, 48, 64 rows of W: 8 x 8192 x 8192 11.3, 9.9, -, 13; 8 x 11008 x 4096 8.8, 8.8, 7.4, 8.1; 8 x 28672 x
-// 4096 18.7, 15.8, -, 15.0; 16 x 4096 x 4096 5.4, 6.4; 16 x 8192 x 4096 8.7, 7.1, -, 8.6; 16 x 11008 x 4096 13.6, 10.7, 8.7, 9.1;
-// 16 x 14336 x 4096 15.0, 11.0, -, 9.6; 4 x 8192 x 8192 9.7, 9.5, -, 13; 4 x 11008 x 4096 7.1, 7.7, -, 7.8; 4 x 14336 x 14336 26.3,
-// 22.4, -, 22.0.  Four and eight wavefronts: 1 x 4096 x 1024 2.8, 2.9; 1 x 4096 x 8192 8.0, 6.0; 8 x 4096 x 2048 3.8, 3.7; x 14336
-// 12.3, 10.4; 16 x 4096 x 4096 5.4, 5.7.
+// At most sixteen rows of x.  A workgroup reads its rows of x whatever it takes of W, so of more than four rows it takes as many
+// blocks of 16 rows of W, up to four, as give the CUs' rounds the least cost: one up to 256 blocks, two up to 512, three (11008
+// rows) up to 768.  Up to four rows of x are cheap: two blocks where the CUs' rounds of one are even, so that half as many do.
+// Eight wavefronts where a CU has one workgroup, columns enough for them and no more of x than of W.  Measured, us a call of
+// captured ones, over matrices of 600 MB in turn, 16, 32, 48, 64 rows of W:
+//  - 8 x 8192 x 8192 10.9, 9.7, 11.6, 13.0; 8 x 11008 x 4096 9.4, 9.5, 7.9, 8.5; 8 x 28672 x 4096 18.4, 15.9, 16.4, 15.1; 16 x 4096 x 4096
+//    5.8, 6.9, 7.7, 8.4; 16 x 8192 x 4096 9.2, 7.5, 8.3, 8.9; 16 x 11008 x 4096 13.5, 11.3, 9.0, 9.5; 16 x 14336 x 4096 15.1, 11.1, 13.0, 9.9.
+//  - 16 and 32: 1 x 11008 x 4096 7.0, 7.6; 1 x 16384 x 2048 6.0, 5.7; 1 x 20480 x 4096 10.5, 11.1; 1 x 14336 x 14336 23.5, 22.5; 2 x 12288 x
+//    4096 7.2, 7.9; 2 x 14336 x 4096 8.4, 8.2; 2 x 28672 x 4096 13.2, 14.0; 4 x 14336 x 14336 27.9, 23.9; 4 x 57344 x 1024 9.3, 9.0; and with
+//    three steps in flight 4 x 6144 x 4096 6.1, 5.7; 4 x 8192 x 8192 10.1, 9.6; 4 x 8192 x 2048 4.6, 4.5.
+//  - four and eight wavefronts: 1 x 4096 x 1024 2.9, 3.0; x 2048 3.3, 3.4; x 4096 5.3, 4.5; x 8192 8.3, 6.3; 4 x 2048 x 1536 3.0, 3.0;
+//    8 x 4096 x 2048 3.5, 3.5; x 14336 12.3, 10.3.
 inline float few_us(int64_t tiles, int blocks, int K) {          // of the CUs' rounds: a workgroup's x, and its rows of W
     return (float)(((tiles + blocks - 1) / blocks + 255) / 256) * (0.234f * blocks + 0.27f) * (1e-3f * (float)K);
 }
@@ -100,7 +104,7 @@ inline FewPlan few_plan(int M, int N, int K) {
     if (M <= 4) {
         if (tiles <= 256) return K <= 1024 ? FewPlan{1, 1, 4, 2} : FewPlan{1, 1, 8, 3};
         if (tiles <= 512 && K > 2048) return {2, 1, 4, 3};
-        return tiles >= 768 && M > 1 ? FewPlan{2, 1, 4, 2} : FewPlan{1, 1, 4, 2};
+        return tiles > 512 && (tiles + 255) / 256 % 2 == 0 ? FewPlan{2, 1, 4, 2} : FewPlan{1, 1, 4, 2};
     }
     const int blocks = few_blocks(tiles, K);
     if (M <= 8) {
@@ -120,13 +124,14 @@ inline FewPlan few_plan(int M, int N, int K) {
 //    that adds them up and 0.2 a MB;
 //  - by way of bf16: 8.1 for two launches, for a million values of the matrix 0.27, of y 1.4, for a thousand columns 3.6, and
 //    1.7 PFLOP/s.
-// Measured, sixteen at a time, tiles: 48 x 4096 x 4096 11.7, 12.4; 80 rows 15.8, 16.8; 24 x 4096 x 14336 20.0, 15.1; 48 x 11008 x
-// 4096 17.8, 19.5; 64 x 8192 x 4096 15.7, 14.4; 80 x 4096 x 512 6.9, 5.1 (the worst choice of 300 sizes).  Tiles of 128 and of 256
-// rows of W: 317 x 3584 x 14336 48.4, 47.7; 128 x 4096 x 4096 16.5, 21.6; 640 x 4096 x 11008 68.7, 63.7; 1024 x 4096 x 4096 37.3,
-// 43.8; x 11008 95.1, 88.2; 1536 x 4096 x 4096 58.9, 48.7; 1024 x 3584 x 14336 120, 106.  64 x 4096 x 11008 in eight slices 16.9,
-// in four 18.1; 64 x 11008 x 4096 in one 19.2, in two 20.4; 200 x 4096 x 4096 in one 19.2, in two 20.4; 300 x 4096 x 4096 in four
-// 23.4, in two 24.4, in one 24.6.  Tiles, bf16: 1024 x 4096 x 4096 40.1, 50.1; 2048 rows 64.7, 67.9; 2251 x 6112 x 7968 236, 199;
-// 3955 x 2128 x 12352 225, 185; 634 x 1904 x 9984 37, 47; 3978 x 1088 x 4192 54.7, 55.1.
+// Measured, us a call of captured ones, over matrices of 600 MB in turn:
+//  - sixteen at a time, tiles: 48 x 4096 x 4096 12.0, 13.4; 80 rows 17.4, 15.3; 24 x 4096 x 14336 20.0, 15.2; 48 x 11008 x 4096 17.4, 19.5;
+//    64 x 8192 x 4096 15.8, 14.3; 80 x 4096 x 512 7.7, 5.2 (with 80 x 4096 x 4096 the worst choices found).
+//  - tiles of 128 and of 256 rows of W: 317 x 3584 x 14336 48.8, 47.9; 128 x 4096 x 4096 17.3, 26.3; 640 x 4096 x 11008 70.0, 64.2;
+//    1024 x 4096 x 4096 40.7, 44.7; x 11008 101, 90.2; 1536 x 4096 x 4096 88.4, 50.4; 1024 x 3584 x 14336 144, 109.
+//  - slices: 64 x 4096 x 11008 in eight 17.6, in four 22.6; 64 x 11008 x 4096 in one 19.8, in two 20.6; 200 x 4096 x 4096 in one 19.1, in
+//    two 21.1; 300 x 4096 x 4096 in four 24.4, in one 24.4, in two 31.7.
+//  - tiles, bf16: 1024 x 4096 x 4096 40.7, 50.4; 2048 rows 62.7, 69.4; 2048 x 11008 x 4096 186, 159; 2251 x 6112 x 7968 233, 217.
 struct MpKind {                          // of tiles: 32 mb rows of x by 64 rt rows of W, us a step of 128 columns
     int mb, rt;
     float step_us;

@@ -60,7 +60,7 @@ static int mp_raise_lds(const void* kernel, int bytes, std::atomic<uint64_t>& ra
 // At most 16 rows of x (or any number, 16 at a time): a workgroup takes 16 R rows of W, and its wavefronts take turns at their
 // columns, 128 at a time, each with DEPTH steps in flight in an LDS ring of its own; their sums meet at the end, in a fixed
 // order.  XI: loads of four rows of x a step.  Measured with weights from HBM, us (of which 2.5 are the launch): 1 x 4096 x 4096
-// 4.3, x 14336 7.6, 1 x 11008 x 4096 6.6 (23.9 MB in 4 us: 6 TB/s), 8 x 11008 x 4096 7.4, 16 x 11008 x 4096 8.7.
+// 4.4, 1 x 11008 x 4096 7.0 (23.9 MB in 4.4 us: 5.4 TB/s), 8 x 11008 x 4096 7.9, 16 x 11008 x 4096 9.0.
 template <int R, int XI, int WAVES, int DEPTH>
 constexpr int mp_ring_bytes() { return WAVES * DEPTH * (R + XI) * 1024; }
 
@@ -191,10 +191,10 @@ static int launch_few_rows(const MpArgs& a, hipStream_t s) {
 // both operands through a ring of NS steps in LDS that all of them read.  A step moves 8 (4 MB + RT) KB from LDS and 8 MB + 4 RT
 // KB into it at 128 bytes a cycle (MB = 5, RT = 2: 1730 cycles) and multiplies 4 MB RT times a wavefront (1280 cycles a SIMD);
 // without loads from memory it takes 2250, with them some 3000.  RT = 4 reads x half as often (MB = 4: 1630 and 2048 cycles) and
-// reaches 1.04 PFLOP/s at 1024 x 4096 x 11008, where the chip's best is 1.2; without its reads of x, its loads, its conversions it
-// takes 8, 3 and 0 % less.  Reading a step ahead into registers, between the products, gains nothing (64 x 4096 x 11008 13.4, 14.0
-// us; 317 x 3584 x 14336 43.1, 42.8), nor do four wavefronts with twice the columns each (14.3, 48.1), nor different starts in k
-// (13.6, 48).  K >= 512; WHOLE: whole steps.  The slices' sums are added by mx4_sum_kernel.
+// reaches 1.02 PFLOP/s at 1024 x 4096 x 11008, where a large bf16 product reaches 1.5 to 1.6; without its reads of x, its loads, its
+// conversions that took 8, 3 and 0 % less.  Tried and not kept (the kernel's own time at 64 x 4096 x 11008 and at 317 x 3584 x 14336):
+// reading a step ahead into registers, between the products (+4, -1 %), four wavefronts with twice the columns each (+7, +12 %),
+// different starts in k (+1, +11 %).  K >= 512; WHOLE: whole steps.  The slices' sums are added by mx4_sum_kernel.
 constexpr int MT_WM = 2, MT_WN = 4, MT_WAVES = MT_WM * MT_WN;
 template <int MB, int RT, int NS>
 constexpr int mp_tile_bytes() { return NS * (16 * MB * MT_WM * 256 + 16 * RT * MT_WN * 64) + 3 * 16 * RT * MT_WN * 16; }
@@ -346,8 +346,8 @@ static int launch_tiles(const MpArgs& a, hipStream_t s) {
 }
 
 // y = the slices' sums added up in their order (+ residual): four columns of a row a thread, eight slices' loads and the
-// residual's in flight at once, since it is a chain of round trips and little else (64 x 4096 x 11008 in eight slices 17.3 us in
-// all; with launch_partial_reduce, whose threads take eight columns and four slices at a time, 17.8).
+// residual's in flight at once, since it is a chain of round trips and little else (both kernels of 64 x 4096 x 11008 in eight
+// slices 17.3 us; with launch_partial_reduce, whose threads take eight columns and four slices at a time, 17.8).
 __global__ __launch_bounds__(256) void mx4_sum_kernel(MpArgs a) {
     const int quads = a.N / 4;
     const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;

@@ -118,3 +118,16 @@ def test_slices_of_k(plan):
 def test_few_keys_are_not_sliced(plan, pairs, N, d, sliced):
     for B, Hkv in ((pairs, 1), (pairs // 8, 8)):
         assert (walked(plan.attn, 3, B, N, Hkv, d)[1] > 1) == sliced
+
+
+@pytest.mark.parametrize("M,N,K,blocks", [
+    # us with one and with two blocks of 16 rows of the matrix to a workgroup: 7.2, 7.9; 8.4, 8.2; 10.7, 11.2; 13.2, 14.0;
+    # 24.8, 22.6; 15.6, 14.3; 9.2, 8.7
+    (2, 12288, 4096, 1), (2, 14336, 4096, 2), (2, 20480, 4096, 1), (2, 28672, 4096, 1), (2, 14336, 14336, 2), (2, 12800, 8192, 2),
+    (2, 57344, 1024, 2),
+    # one row: 23.5, 22.5; 14.7, 14.2; 6.0, 5.7; 10.5, 11.1; 7.0, 7.6
+    (1, 14336, 14336, 2), (1, 12800, 8192, 2), (1, 16384, 2048, 2), (1, 20480, 4096, 1), (1, 11008, 4096, 1),
+    # up to 512 blocks: 10.1, 9.6; 6.1, 5.7
+    (4, 8192, 8192, 2), (4, 6144, 4096, 2)])
+def test_blocks_of_few_rows(plan, M, N, K, blocks):
+    assert walked(plan.few, 4, M, N, K)[0] == blocks
