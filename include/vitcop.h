@@ -504,7 +504,7 @@ int vitcop_decode_attn(const uint16_t* q, const uint16_t* k, const uint16_t* v, 
  * sign is bit 3), two codes to a byte, the lower index in the lower half.  4.25 bits a value; every value is
  * a bf16, and the products below are those of vitcop_decode_attn and vitcop_project on these values.
  * To 4 bits: s - 127 is the least exponent in [-125,125] for which no magnitude of the group is above
- * 7 * 2^(s-127); the code is the nearest value, ties going to the even code, what is above 6 to 6, and a zero
+ * 7 * 2^(s-127), or 125 where one is above that too; the code is the nearest value, ties going to the even code, what is above 6 to 6, and a zero
  * keeps its sign.  A group that holds an infinity or a NaN gets s = 255 and reads back as NaN (here inputs
  * need not be finite).  s = 253 and 254, which these calls never write, may stand for infinities, and an
  * attention over such rows may give NaN.
@@ -564,8 +564,9 @@ int vitcop_decode_attn_mx4(const uint16_t* q, const vitcop_cache_mx4_t* C, uint1
  *   residual: NULL, or [M,N] bf16; row strides in elements, multiples of 8
  *   ws: NULL, or device scratch of ws_bytes >= vitcop_project_mx4_workspace_bytes(M,N,K) (16-byte aligned, 0 for
  *   at most 16 rows): some more rows leave most of the chip idle unless k is cut into slices, whose fp32 sums live
- *   there and are added in a fixed order, and of many rows the matrix may go to bf16 there first; without
- *   scratch, or with too little, one slice does it all
+ *   there (4*M*N bytes a slice, up to 16 of them) and are added in a fixed order, and of many rows, where that is
+ *   quicker, the matrix goes to bf16 there first (2*N*K bytes and what vitcop_project asks for); without scratch, or
+ *   with too little, one slice does it all, of the matrix as it is
  * K % 32 == 0, N % 16 == 0, K <= 2^16, M <= 2^19, M*x_row_stride < 2^30, N*K < 2^31. */
 size_t vitcop_project_mx4_workspace_bytes(int M, int N, int K);
 int vitcop_project_mx4(const uint16_t* x, int64_t x_row_stride, const uint8_t* w_codes, const uint8_t* w_scales,
