@@ -71,3 +71,23 @@ def test_a_refused_write_writes_nothing(vc):
     one = torch.zeros((1, T, Hkv, d), dtype=torch.bfloat16, device="cuda")
     vc.vitcop_cache_mx4_write(cache, k, one.expand(B, T, Hkv, d))                                 # two layouts, both in order
     assert not np.array_equal(tensors(cache)[0], before[0]) and not np.array_equal(tensors(cache)[2], before[2])
+
+
+def test_sizes_past_32_bits_are_refused(vc):
+    # the C calls take 32-bit sizes: 2^32 + n must not be taken for n
+    past = 1 << 32
+    k = dev(I.normal_bf16(2, 0, (1, 1, 2, 64)))
+    cache = filled(vc, 1, 16, 2, 64)
+    before = tensors(cache)
+    q = torch.zeros((1, 2, 64), dtype=torch.bfloat16, device="cuda")
+    long_row = torch.empty((1, past + 32), dtype=torch.bfloat16, device="cuda")
+    long_codes = torch.empty((1, past // 2 + 16), dtype=torch.uint8, device="cuda")
+    long_scales = torch.empty((1, past // 32 + 1), dtype=torch.uint8, device="cuda")
+    for bad in (lambda: vc.vitcop_cache_mx4_write(cache, k, None, past), lambda: vc.vitcop_cache_mx4_write(cache, k, k, 2 - past),
+                lambda: vc.vitcop_cache_mx4_write(cache, k.expand(1, past + 1, 2, 64), None),
+                lambda: vc.vitcop_cache_mx4_read(cache, 1, past), lambda: vc.vitcop_decode_attn_mx4(q, cache, past + 3),
+                lambda: vc.vitcop_mx4_quantize(long_row), lambda: vc.vitcop_mx4_dequantize(long_codes, long_scales),
+                lambda: vc.vitcop_project_mx4(long_row, long_codes, long_scales)):
+        with pytest.raises((ValueError, vc.VitcopError)):
+            bad()
+    assert all(np.array_equal(a, b) for a, b in zip(tensors(cache), before))
