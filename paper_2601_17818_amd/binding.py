@@ -932,7 +932,9 @@ def vitcop_cache_mx4_write(cache: CacheMx4, k, v, start: int = 0, start_samples=
         vitcop_cache_mx4_write(cache, k, None, start, start_samples, n_samples)      # strides of their own: two calls
         vitcop_cache_mx4_write(cache, None, v, start, start_samples, n_samples)
         return
-    T, row, batch = v_rows if v_rows is not None else (0, 0, 0)
+    if v_rows is None:
+        raise ValueError("k and v are both None")
+    T, row, batch = v_rows
     _check(lib.vitcop_cache_mx4_write(cache.desc, _ptr(k), _ptr(v), row, batch, T, start,
                                       cache.per_sample(start_samples, "start_samples"),
                                       cache.per_sample(n_samples, "n_samples"), _stream_of(dev)))

@@ -91,3 +91,8 @@ def test_sizes_past_32_bits_are_refused(vc):
         with pytest.raises((ValueError, vc.VitcopError)):
             bad()
     assert all(np.array_equal(a, b) for a, b in zip(tensors(cache), before))
+
+
+def test_nothing_to_write_is_refused(vc):
+    with pytest.raises(ValueError):
+        vc.vitcop_cache_mx4_write(filled(vc, 1, 16, 2, 64), None, None)
