@@ -872,21 +872,25 @@ def vitcop_mx4_dequantize(codes, scales, out=None):
 
 class CacheMx4:
     """One layer's KV cache in 4 bits: k_codes, v_codes [B,Hkv,capacity,d/2] and k_scales, v_scales [B,Hkv,capacity,d/32],
-    uint8, contiguous.  ``CacheMx4.empty`` allocates one (rows that nothing has been written to hold anything)."""
+    uint8, contiguous; an object keeps the tensors that it was made of.  ``CacheMx4.empty`` allocates one (rows that nothing has
+    been written to hold anything)."""
 
     def __init__(self, k_codes, k_scales, v_codes, v_scales):
-        self.device = _here(k_codes, "k_codes")
+        device = _here(k_codes, "k_codes")
         if k_codes.dim() != 4:
             raise ValueError("k_codes must be [B,Hkv,capacity,d/2]")
         B, Hkv, capacity, half = k_codes.shape
         _size(max(B, Hkv, capacity, 2 * half), "k_codes")
         for t, name, width in ((k_codes, "k_codes", half), (k_scales, "k_scales", half * 2 // MX4_GROUP),
                                (v_codes, "v_codes", half), (v_scales, "v_scales", half * 2 // MX4_GROUP)):
-            _expect(t, name, (B, Hkv, capacity, width), torch.uint8, self.device)
-        self.B, self.Hkv, self.capacity, self.d = B, Hkv, capacity, half * 2
-        self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
-        self.desc = CacheMx4T(B, capacity, Hkv, half * 2, k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(),
-                              v_scales.data_ptr())
+            _expect(t, name, (B, Hkv, capacity, width), torch.uint8, device)
+        desc = CacheMx4T(B, capacity, Hkv, half * 2, k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(),
+                         v_scales.data_ptr())
+        self.__dict__.update(device=device, B=B, Hkv=Hkv, capacity=capacity, d=half * 2, k_codes=k_codes, k_scales=k_scales,
+                             v_codes=v_codes, v_scales=v_scales, desc=desc)
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"{name}: the descriptor holds the tensors' addresses; make another CacheMx4")
 
     @classmethod
     def empty(cls, B: int, capacity: int, Hkv: int, d: int, device="cuda"):

@@ -96,3 +96,11 @@ def test_sizes_past_32_bits_are_refused(vc):
 def test_nothing_to_write_is_refused(vc):
     with pytest.raises(ValueError):
         vc.vitcop_cache_mx4_write(filled(vc, 1, 16, 2, 64), None, None)
+
+
+def test_a_caches_tensors_stay_its_own(vc):
+    # the descriptor holds their addresses: another tensor in the place of one would not be seen
+    cache = filled(vc, 1, 16, 2, 64)
+    for name in ("k_codes", "k_scales", "v_codes", "v_scales", "B", "Hkv", "capacity", "d"):
+        with pytest.raises(AttributeError):
+            setattr(cache, name, getattr(cache, name))
