@@ -800,11 +800,12 @@ def _expect(t, name: str, shape, dtype, device: int) -> None:
         raise ValueError(f"{name} must be contiguous")
 
 
-def _size(n: int, name: str) -> int:
-    """A size or a row's number as the C calls take them, in 32 bits (ctypes would drop the others)."""
-    if not -0x80000000 <= n <= 0x7FFFFFFF:
-        raise ValueError(f"{name} is {n}, past 32 bits")
-    return n
+# the sizes and row numbers that the C calls take, in 32 bits (ctypes would drop the others)
+_LEAST, _MOST = -0x80000000, 0x7FFFFFFF
+
+
+def _past(n: int, name: str):
+    raise ValueError(f"{name} is {n}, past 32 bits")
 
 
 def _here(t, name: str) -> int:
@@ -829,7 +830,8 @@ def _rows_of(t, name: str):
     if len(shape) != 2 or t.dtype not in _BF16:
         raise ValueError(f"{name} must be a bf16 matrix")
     M, K = shape
-    _size(max(M, K), name)
+    if M > _MOST or K > _MOST:
+        _past(max(M, K), name)
     if K > 1 and strides[1] != 1:
         raise ValueError(f"{name} must have contiguous rows")
     return M, K, strides[0] if M > 1 else K
@@ -856,7 +858,8 @@ def vitcop_mx4_dequantize(codes, scales, out=None):
     if codes.dim() != 2:
         raise ValueError("codes must be [M,K/2]")
     M, K = codes.shape[0], codes.shape[1] * 2
-    _size(max(M, K), "codes")
+    if M > _MOST or K > _MOST:
+        _past(max(M, K), "codes")
     _expect(codes, "codes", (M, K // 2), torch.uint8, dev)
     _expect(scales, "scales", (M, K // MX4_GROUP), torch.uint8, dev)
     stride = K
@@ -880,7 +883,8 @@ class CacheMx4:
         if k_codes.dim() != 4:
             raise ValueError("k_codes must be [B,Hkv,capacity,d/2]")
         B, Hkv, capacity, half = k_codes.shape
-        _size(max(B, Hkv, capacity, 2 * half), "k_codes")
+        if max(B, Hkv, capacity, 2 * half) > _MOST:
+            _past(max(B, Hkv, capacity, 2 * half), "k_codes")
         for t, name, width in ((k_codes, "k_codes", half), (k_scales, "k_scales", half * 2 // MX4_GROUP),
                                (v_codes, "v_codes", half), (v_scales, "v_scales", half * 2 // MX4_GROUP)):
             _expect(t, name, (B, Hkv, capacity, width), torch.uint8, device)
@@ -909,7 +913,9 @@ def _cache_rows(cache: CacheMx4, t, name: str):
     shape = t.shape
     if t.get_device() != cache.device or t.dtype not in _BF16 or len(shape) != 4:
         raise ValueError(f"{name} must be a bf16 [B,T,Hkv,d] tensor on cuda:{cache.device}")
-    T = _size(shape[1], name)
+    T = shape[1]
+    if T > _MOST:
+        _past(T, name)
     if shape != (cache.B, T, cache.Hkv, cache.d):
         raise ValueError(f"{name} must be {(cache.B, T, cache.Hkv, cache.d)}, not {tuple(shape)}")
     sb, st, sh, sd = t.stride()
@@ -924,7 +930,8 @@ def vitcop_cache_mx4_write(cache: CacheMx4, k, v, start: int = 0, start_samples=
     with n_samples (int32 [B]) the first n_samples[b] rows of sample b only.  A token's heads lie side by side; tokens and
     samples may be strided (views of fused QKV rows)."""
     dev = _here(cache.k_codes, "the cache")
-    _size(start, "start")
+    if not _LEAST <= start <= _MOST:
+        _past(start, "start")
     k_rows = _cache_rows(cache, k, "k") if k is not None else None
     v_rows = _cache_rows(cache, v, "v") if v is not None else k_rows
     if k_rows is not None and k_rows != v_rows:
@@ -948,8 +955,8 @@ def vitcop_cache_mx4_read(cache: CacheMx4, T: int, start: int = 0, start_samples
     """Rows [start, start + T) of every sample, or T rows from start_samples[b] (int32 [B]) on, as (k, v) [B,T,Hkv,d]
     bf16; ``out`` = (k, v) reuses buffers, of which one may be None."""
     dev = _here(cache.k_codes, "the cache")
-    _size(start, "start")
-    _size(T, "T")
+    if not _LEAST <= start <= _MOST or T > _MOST:
+        _past(max(start, T, key=abs), "start or T")
     shape = (cache.B, T, cache.Hkv, cache.d)
     if out is None:
         if T < 0:
@@ -971,8 +978,9 @@ def vitcop_decode_attn_mx4(q, cache: CacheMx4, N: int, n_samples=None, scale: fl
     dev = _here(q, "q")
     if q.dim() != 3:
         raise ValueError("q must be [B,Hq,d]")
-    Hq = _size(q.shape[1], "q")
-    _size(N, "N")
+    Hq = q.shape[1]
+    if not _LEAST <= N <= _MOST:
+        _past(N, "N")
     _expect(q, "q", (cache.B, Hq, cache.d), None, cache.device)
     if out is None:
         o = torch.empty_like(q)
@@ -999,7 +1007,9 @@ def vitcop_project_mx4(x, codes, scales, residual=None, out=None, ws=None):
     workspace (one that is too small for slices of K is not used)."""
     dev = _here(x, "x")
     M, K, x_stride = _rows_of(x, "x")
-    N = _size(codes.shape[0], "codes") if codes.dim() == 2 else 0
+    N = codes.shape[0] if codes.dim() == 2 else 0
+    if N > _MOST:
+        _past(N, "codes")
     _expect(codes, "codes", (N, K // 2), torch.uint8, dev)
     _expect(scales, "scales", (N, K // MX4_GROUP), torch.uint8, dev)
     y_stride = res_stride = N
