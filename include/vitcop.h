@@ -504,10 +504,10 @@ int vitcop_decode_attn(const uint16_t* q, const uint16_t* k, const uint16_t* v, 
  * sign is bit 3), two codes to a byte, the lower index in the lower half.  4.25 bits a value; every value is
  * a bf16, and the products below are those of vitcop_decode_attn and vitcop_project on these values.
  * To 4 bits: s - 127 is the least exponent in [-125,125] for which no magnitude of the group is above
- * 7 * 2^(s-127), or 125 where one is above that too; the code is the nearest value, ties going to the even code, what is above 6 to 6, and a zero
- * keeps its sign.  A group that holds an infinity or a NaN gets s = 255 and reads back as NaN (here inputs
- * need not be finite).  s = 253 and 254, which these calls never write, may stand for infinities, and an
- * attention over such rows may give NaN.
+ * 7 * 2^(s-127), or 125 where one is above that too; the code is the nearest value, ties going to the even code,
+ * what is above 6 to 6, and a zero keeps its sign.  A group that holds an infinity or a NaN gets s = 255 and reads
+ * back as NaN (here inputs need not be finite).  s = 253 and 254, which these calls never write, may stand for
+ * infinities, and an attention over such rows may give NaN.
  */
 #define VITCOP_MX4_GROUP 32
 
