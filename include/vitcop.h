@@ -573,6 +573,113 @@ int vitcop_project_mx4(const uint16_t* x, int64_t x_row_stride, const uint8_t* w
                        uint16_t* y, int64_t y_row_stride, const uint16_t* residual, int64_t res_row_stride,
                        int M, int N, int K, void* ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Prompts, tokens and drafts over a bf16 cache: rotary positions of several axes, attention of any number of tokens at
+ * a cache's end (all of it, or a window and the first rows), attention of a tree of drafted tokens, and rows written to
+ * the caches of all layers.  The cache is the one that vitcop_decoder_layer_prefill leaves and
+ * vitcop_decoder_decode_step reads: k, v [B,capacity,Hkv,d], dense.  The descriptor is host memory read during the call.
+ *
+ * Arguments that these calls share.  Each is optional (NULL), a DEVICE array, and read by the kernels, so that a captured
+ * graph goes by what it holds at the replay:
+ *   start_samples int32 [B]: rows that sample b's cache holds before the call (NULL: `start` of them)
+ *   n_samples     int32 [B]: sample b has min(max(n_samples[b], 0), T) tokens, the first ones of its T (NULL: T).  What
+ *                 belongs to its other tokens is neither read nor written: outputs there stay as they were.
+ * Strides are in elements and multiples of 8; a token's heads lie side by side, so that q, k and v may be views of fused
+ * QKV rows.  A row stride is not looked at where T is 1.
+ */
+typedef struct {
+    int B, capacity, Hkv, d;
+    uint16_t* k;
+    uint16_t* v;
+} vitcop_cache_t;
+
+/* Rotary embedding with a position for each of several axes (time, height and width of an image or video; the text has
+ * the same in all): channel i < d/2 pairs with i + d/2 and turns by the angle position * theta^(-2i/d), as in vitcop_rope,
+ * the position being that of the axis which pair i belongs to.  sections[a] pairs belong to axis a: section after section,
+ * or with `interleaved` one pair to each axis in turn, an axis that has no pair left being passed over.  Angles are formed
+ * in whole revolutions of 64 bits: far positions lose nothing.
+ *   q [B,T,Hq,d], k, v [B,T,Hkv,d]; q or k may be NULL, and v
+ *   positions int32 [n_axes,B,T], any values
+ *   q_out: q (in place, its strides), or dense [B,T,Hq,d]
+ *   k_out: k (in place, its strides; then v and v_out are NULL, start 0 and start_samples NULL), or the rows of a cache
+ *          [B,capacity,Hkv,d]: token t of sample b goes to row start + t, or start_samples[b] + t.  start + T <= capacity
+ *          is checked; of start_samples, rows outside [0,capacity) are skipped.
+ *   v_out: like k_out's cache, the rows of v as they are (v and v_out may both be NULL)
+ * Outputs overlap no input apart from those in place.
+ * 1 <= n_axes <= VITCOP_MAX_AXES, the sections' sum is d/2, d % 16 == 0, d <= 256, theta > 1, Hq + 2 Hkv <= 65535;
+ * B*T*(Hq + 2 Hkv)*d/16 < 2^31. */
+#define VITCOP_MAX_AXES 4
+typedef struct {
+    int B, T, Hq, Hkv, d;
+    int n_axes, interleaved;
+    int sections[VITCOP_MAX_AXES];
+    float theta;
+    int capacity, start;
+    const int32_t* positions;
+    const uint16_t *q, *k, *v;
+    int64_t q_row_stride, q_batch_stride, k_row_stride, k_batch_stride, v_row_stride, v_batch_stride;
+    uint16_t *q_out, *k_out, *v_out;
+    const int32_t* start_samples;
+    const int32_t* n_samples;
+} vitcop_rope_axes_t;
+int vitcop_rope_axes(const vitcop_rope_axes_t* R, void* stream);
+
+/* Attention of T tokens whose keys and values are the last rows of a cache: token t of sample b is row p = start_b + t
+ * (start_b: start, or start_samples[b] clamped to [0, start]) and sees the rows j <= p with j > p - window or j < sinks;
+ * window 0: all of j <= p.  A token's step (T = 1), a further question (T tokens behind a long conversation) and a
+ * right-padded prompt (start 0, n_samples) are the same call.  Rows of the cache that no token of the call sees may
+ * hold anything.
+ *   q [B,T,Hq,d] bf16;  out [B,T,Hq,d] bf16 dense;  lse_out [B,Hq,T] fp32 natural-log-sum-exp, may be NULL
+ *   scale 0 selects 1/sqrt(d);  query head h reads KV head h / (Hq/Hkv)
+ *   ws: device scratch of ws_bytes >= vitcop_window_attn_workspace_bytes, NULL where that is 0 (it is 0 too where the
+ *   sizes are refused)
+ * d in {64,128}; Hq % Hkv == 0; 0 <= start, start + T <= capacity; window, sinks >= 0; B, Hkv <= 65535;
+ * B*T*Hq < 2^28. */
+size_t vitcop_window_attn_workspace_bytes(int B, int T, int start, int Hq, int Hkv, int d, int window, int sinks);
+int vitcop_window_attn(const uint16_t* q, int64_t q_row_stride, int64_t q_batch_stride, const vitcop_cache_t* C,
+                       uint16_t* out, float* lse_out, int T, int start, const int32_t* start_samples,
+                       const int32_t* n_samples, int Hq, int window, int sinks, float scale, void* ws, size_t ws_bytes,
+                       void* stream);
+
+/* Attention of T <= VITCOP_MAX_DRAFTS drafted tokens, before it is known which of them stay: token t of sample b sees the
+ * start_b rows of its cache (start, or start_samples[b] clamped to [0, start]) and those drafts j of the sample for which
+ * bit j of tree[b*tree_batch_stride + t] is set (its ancestors in a tree, and itself).  A token that sees nothing gets zeros
+ * and an lse of -inf.  The drafts' keys and values lie beside the cache, which is not written; vitcop_cache_append takes
+ * the accepted ones over.  Rows of the cache from start_b on and drafts that no token sees may hold anything.
+ *   q [B,T,Hq,d], k, v [B,T,Hkv,d] bf16;  tree [B,T] uint64, or one [T] for all samples (tree_batch_stride 0)
+ *   C: k and v may be NULL where start is 0
+ *   out, lse_out, scale, ws and limits as vitcop_window_attn's; 0 <= start <= capacity; row strides of k and v at least
+ *   Hkv*d and below 2^25 (T > 1). */
+#define VITCOP_MAX_DRAFTS 64
+size_t vitcop_tree_attn_workspace_bytes(int B, int T, int start, int Hq, int Hkv, int d);
+int vitcop_tree_attn(const uint16_t* q, int64_t q_row_stride, int64_t q_batch_stride, const vitcop_cache_t* C,
+                     const uint16_t* k, int64_t k_row_stride, int64_t k_batch_stride, const uint16_t* v,
+                     int64_t v_row_stride, int64_t v_batch_stride, const uint64_t* tree, int64_t tree_batch_stride,
+                     uint16_t* out, float* lse_out, int T, int start, const int32_t* start_samples,
+                     const int32_t* n_samples, int Hq, float scale, void* ws, size_t ws_bytes, void* stream);
+
+/* Rows to the caches of all layers in one launch for 64 of them: row i < n_b of sample b, which is row idx[b,i] of k and v
+ * (i, without idx), goes to row start + i of its cache in layer l: start[l], or start_samples[l*B + b] (caches of a pruned
+ * prefill have lengths of their own in each layer).  n_b: `rows`, or n_samples[b] clamped to [0, rows].  Sources outside
+ * [0,T) and targets outside [0,capacity) are skipped on the device; all other rows stay as they were.
+ *   k_cache, v_cache: host arrays of n_layers device pointers, each [B,capacity,Hkv,d]; start: host [n_layers], not looked
+ *   at with start_samples.  start[l] + rows <= capacity is checked; without idx, rows <= T.
+ *   k, v [n_layers,B,T,Hkv,d] with strides (the row stride is not looked at where T is 1); one of the two may be NULL,
+ *   and its caches too.  They overlap no cache.
+ * Hkv*d % 8 == 0; B <= 65535; rows*Hkv*d < 2^31. */
+typedef struct {
+    int n_layers, B, capacity, Hkv, d, T, rows;
+    uint16_t* const* k_cache;
+    uint16_t* const* v_cache;
+    const uint16_t *k, *v;
+    int64_t k_layer_stride, k_batch_stride, k_row_stride, v_layer_stride, v_batch_stride, v_row_stride;
+    const int* start;
+    const int32_t* start_samples;
+    const int32_t* idx;
+    const int32_t* n_samples;
+} vitcop_cache_append_t;
+int vitcop_cache_append(const vitcop_cache_append_t* A, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

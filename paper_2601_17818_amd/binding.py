@@ -46,6 +46,8 @@ EXPORTS = (
     "vitcop_mx4_quantize", "vitcop_mx4_dequantize", "vitcop_cache_mx4_write", "vitcop_cache_mx4_read",
     "vitcop_decode_attn_mx4_workspace_bytes", "vitcop_decode_attn_mx4",
     "vitcop_project_mx4_workspace_bytes", "vitcop_project_mx4",
+    "vitcop_rope_axes", "vitcop_window_attn_workspace_bytes", "vitcop_window_attn",
+    "vitcop_tree_attn_workspace_bytes", "vitcop_tree_attn", "vitcop_cache_append",
 )
 
 
@@ -117,6 +119,32 @@ class FullScheduleT(C.Structure):
 class CacheMx4T(C.Structure):
     _fields_ = ([(n, C.c_int) for n in ("B", "capacity", "Hkv", "d")] +
                 [(n, C.c_void_p) for n in ("k_codes", "k_scales", "v_codes", "v_scales")])
+
+
+class CacheT(C.Structure):
+    _fields_ = ([(n, C.c_int) for n in ("B", "capacity", "Hkv", "d")] + [("k", C.c_void_p), ("v", C.c_void_p)])
+
+
+VITCOP_MAX_AXES = 4
+VITCOP_MAX_DRAFTS = 64
+_Sections = C.c_int * VITCOP_MAX_AXES
+
+
+class RopeAxesT(C.Structure):
+    _fields_ = ([(n, C.c_int) for n in ("B", "T", "Hq", "Hkv", "d", "n_axes", "interleaved")] +
+                [("sections", _Sections), ("theta", C.c_float), ("capacity", C.c_int), ("start", C.c_int)] +
+                [(n, C.c_void_p) for n in ("positions", "q", "k", "v")] +
+                [(n, C.c_int64) for n in ("q_row_stride", "q_batch_stride", "k_row_stride", "k_batch_stride",
+                                           "v_row_stride", "v_batch_stride")] +
+                [(n, C.c_void_p) for n in ("q_out", "k_out", "v_out", "start_samples", "n_samples")])
+
+
+class CacheAppendT(C.Structure):
+    _fields_ = ([(n, C.c_int) for n in ("n_layers", "B", "capacity", "Hkv", "d", "T", "rows")] +
+                [("k_cache", C.POINTER(C.c_void_p)), ("v_cache", C.POINTER(C.c_void_p)), ("k", C.c_void_p), ("v", C.c_void_p)] +
+                [(n, C.c_int64) for n in ("k_layer_stride", "k_batch_stride", "k_row_stride",
+                                           "v_layer_stride", "v_batch_stride", "v_row_stride")] +
+                [("start", C.POINTER(C.c_int))] + [(n, C.c_void_p) for n in ("start_samples", "idx", "n_samples")])
 
 
 class ScheduleT(C.Structure):
@@ -224,6 +252,19 @@ def _load() -> C.CDLL:
     lib.vitcop_project_mx4_workspace_bytes.argtypes = [i32, i32, i32]
     lib.vitcop_project_mx4.restype = i32
     lib.vitcop_project_mx4.argtypes = [vp, i64, vp, vp, vp, i64, vp, i64, i32, i32, i32, vp, sz, vp]
+    lib.vitcop_rope_axes.restype = i32
+    lib.vitcop_rope_axes.argtypes = [C.POINTER(RopeAxesT), vp]
+    lib.vitcop_window_attn_workspace_bytes.restype = sz
+    lib.vitcop_window_attn_workspace_bytes.argtypes = [i32] * 8
+    lib.vitcop_window_attn.restype = i32
+    lib.vitcop_window_attn.argtypes = [vp, i64, i64, C.POINTER(CacheT), vp, vp, i32, i32, vp, vp, i32, i32, i32, f32, vp, sz, vp]
+    lib.vitcop_tree_attn_workspace_bytes.restype = sz
+    lib.vitcop_tree_attn_workspace_bytes.argtypes = [i32] * 6
+    lib.vitcop_tree_attn.restype = i32
+    lib.vitcop_tree_attn.argtypes = [vp, i64, i64, C.POINTER(CacheT), vp, i64, i64, vp, i64, i64, vp, i64, vp, vp, i32, i32, vp,
+                                     vp, i32, f32, vp, sz, vp]
+    lib.vitcop_cache_append.restype = i32
+    lib.vitcop_cache_append.argtypes = [C.POINTER(CacheAppendT), vp]
     return lib
 
 
@@ -1032,3 +1073,263 @@ def vitcop_project_mx4(x, codes, scales, residual=None, out=None, ws=None):
                                   _ptr(residual), res_stride, M, N, K, _ptr(ws), ws.numel() if ws is not None else 0,
                                   _stream_of(dev)))
     return out
+
+
+# ----------------------------------------------------------------- prompts, tokens and drafts over a bf16 cache
+
+
+class Cache:
+    """One layer's KV cache in bf16, as the prefills leave it: k, v [B,capacity,Hkv,d], contiguous; an object keeps the tensors
+    that it was made of."""
+
+    def __init__(self, k, v):
+        device = _here(k, "k")
+        if k.dim() != 4:
+            raise ValueError("k must be [B,capacity,Hkv,d]")
+        B, capacity, Hkv, d = shape = k.shape
+        if max(shape) > _MOST:
+            _past(max(shape), "k")
+        _expect(k, "k", shape, None, device)
+        _expect(v, "v", shape, None, device)
+        self.__dict__.update(device=device, B=B, capacity=capacity, Hkv=Hkv, d=d, k=k, v=v,
+                             desc=CacheT(B, capacity, Hkv, d, k.data_ptr(), v.data_ptr()))
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"{name}: the descriptor holds the tensors' addresses; make another Cache")
+
+
+def _token_rows(t, name: str, device: int, shape):
+    """(row stride, batch stride) of bf16 rows [B,T,heads,d] whose heads lie side by side."""
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, not on cuda:{device}")
+    if t.shape != shape or t.dtype not in _BF16:
+        raise ValueError(f"{name} must be bf16 {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
+    B, T, heads, d = shape
+    sb, st, sh, sd = t.stride()
+    if sd != 1 or (heads > 1 and sh != d):
+        raise ValueError(f"{name}: a token's heads must lie side by side")
+    row = st if T > 1 else heads * d
+    return row, sb if B > 1 else T * row
+
+
+def _counts(t, name: str, shape, device: int):
+    if t is None:
+        return None
+    _expect(t, name, shape, torch.int32, device)
+    return t.data_ptr()
+
+
+def _whole(n: int, name: str) -> None:
+    if not _LEAST <= n <= _MOST:
+        _past(n, name)
+
+
+def vitcop_rope_axes(q, k, positions, sections, theta: float = 10000.0, v=None, interleaved: bool = False, cache: Cache = None,
+                     start: int = 0, start_samples=None, n_samples=None, out=None, k_out=None):
+    """q [B,T,Hq,d] and k [B,T,Hkv,d] (either may be None; views of fused QKV rows may be given) turned by positions
+    [n_axes,B,T] int32, of whose axes ``sections`` names the pairs -> (q turned, k turned).  With a cache, k and v go to its
+    rows start + t, or start_samples[b] + t (int32 [B]), and the second result is None; without one, v must be None.
+    n_samples int32 [B]: the first ones of a sample's tokens only, others' rows stay as they were.  ``out`` and ``k_out`` reuse
+    buffers, or are q and k themselves (in place)."""
+    like = q if q is not None else (k if k is not None else v)
+    if like is None:
+        raise ValueError("q, k and v are all None")
+    dev = _here(like, "the tokens")
+    if like.dim() != 4:
+        raise ValueError("the tokens must be [B,T,heads,d]")
+    B, T, _, d = like.shape
+    n_axes = len(sections)
+    if not 1 <= n_axes <= VITCOP_MAX_AXES:
+        raise ValueError(f"{n_axes} sections (1 to {VITCOP_MAX_AXES})")
+    for n in (*sections, *like.shape, start):
+        _whole(n, "a size, section or start")
+    _expect(positions, "positions", (n_axes, B, T), torch.int32, dev)
+    Hq = Hkv = capacity = 0
+    q_rows = k_rows = v_rows = (0, 0)
+    k_to = v_to = None
+    if q is not None:
+        Hq = q.shape[2] if q.dim() == 4 else 0
+        q_rows = _token_rows(q, "q", dev, (B, T, Hq, d))
+        if out is None:
+            out = torch.empty((B, T, Hq, d), dtype=q.dtype, device=q.device)
+        elif out is not q and out.data_ptr() != q.data_ptr():
+            _expect(out, "out", (B, T, Hq, d), None, dev)
+        elif _token_rows(out, "out", dev, (B, T, Hq, d)) != q_rows:
+            raise ValueError("out begins where q does, with other strides")
+    elif out is not None:
+        raise ValueError("out without q")
+    if k is not None or v is not None:
+        Hkv = (k if k is not None else v).shape[2] if (k if k is not None else v).dim() == 4 else 0
+    if k is not None:
+        k_rows = _token_rows(k, "k", dev, (B, T, Hkv, d))
+    if v is not None:
+        v_rows = _token_rows(v, "v", dev, (B, T, Hkv, d))
+    if cache is not None:
+        if k is None and v is None:
+            raise ValueError("a cache without k and v")
+        if k_out is not None:
+            raise ValueError("k_out beside a cache")
+        if cache.device != dev or cache.B != B or (cache.Hkv, cache.d) != (Hkv, d):
+            raise ValueError(f"the cache is for {cache.B} samples and {cache.Hkv} heads of {cache.d} on cuda:{cache.device}")
+        capacity = cache.capacity
+        k_to, v_to = _ptr(cache.k if k is not None else None), _ptr(cache.v if v is not None else None)
+    elif v is not None or start or start_samples is not None:
+        raise ValueError("v and a start need a cache")
+    elif k is not None:
+        capacity = T
+        if k_out is None:
+            k_out = torch.empty((B, T, Hkv, d), dtype=k.dtype, device=k.device)
+        elif k_out is not k and k_out.data_ptr() != k.data_ptr():
+            _expect(k_out, "k_out", (B, T, Hkv, d), None, dev)
+        elif _token_rows(k_out, "k_out", dev, (B, T, Hkv, d)) != k_rows:
+            raise ValueError("k_out begins where k does, with other strides")
+        k_to = k_out.data_ptr()
+    elif k_out is not None:
+        raise ValueError("k_out without k")
+    desc = RopeAxesT(B, T, Hq, Hkv, d, n_axes, 1 if interleaved else 0, _Sections(*sections), theta, capacity, start,
+                     positions.data_ptr(), _ptr(q), _ptr(k), _ptr(v), *q_rows, *k_rows, *v_rows, _ptr(out), k_to, v_to,
+                     _counts(start_samples, "start_samples", (B,), dev), _counts(n_samples, "n_samples", (B,), dev))
+    _check(lib.vitcop_rope_axes(desc, _stream_of(dev)))
+    return out, k_out
+
+
+def _attention_buffers(q, cache: Cache, out, want_lse: bool, nbytes: int, ws):
+    """(out, lse, ws) of an attention of q [B,T,Hq,d] over a cache, made or checked."""
+    B, T, Hq, d = q.shape
+    if out is None:
+        o = torch.empty((B, T, Hq, d), dtype=q.dtype, device=q.device)
+        lse = torch.empty((B, Hq, T), dtype=torch.float32, device=q.device) if want_lse else None
+    else:
+        o, lse = out
+        _expect(o, "out", q.shape, None, cache.device)
+        if lse is not None:
+            _expect(lse, "lse", (B, Hq, T), torch.float32, cache.device)
+    if ws is None:
+        ws = _ws(nbytes, q) if nbytes else None
+    elif ws.get_device() != cache.device or ws.dtype is not torch.uint8 or not ws.is_contiguous():
+        raise ValueError(f"ws must be a contiguous uint8 tensor on cuda:{cache.device}")
+    return o, lse, ws
+
+
+def _query_rows(q, cache: Cache):
+    """(T, Hq, row stride, batch stride) of q [B,T,Hq,d] beside a cache."""
+    dev = _here(q, "q")
+    if q.dim() != 4:
+        raise ValueError("q must be [B,T,Hq,d]")
+    T, Hq = q.shape[1], q.shape[2]
+    if T > _MOST or Hq > _MOST:
+        _past(max(T, Hq), "q")
+    if cache.device != dev:
+        raise ValueError(f"the cache is on cuda:{cache.device}, q on cuda:{dev}")
+    return (T, Hq, *_token_rows(q, "q", dev, (cache.B, T, Hq, cache.d)))
+
+
+def vitcop_window_attn(q, cache: Cache, start: int, window: int = 0, sinks: int = 0, start_samples=None, n_samples=None,
+                       scale: float = 0.0, want_lse: bool = True, out=None, ws=None):
+    """q [B,T,Hq,d], token t of sample b being row start + t of the cache (start_samples[b] + t, int32 [B], each at most
+    start), over the rows j up to its own with j > row - window or j < sinks (window 0: all) -> (out [B,T,Hq,d],
+    lse [B,Hq,T] or None).  n_samples int32 [B]: the first ones of a sample's tokens only, others' results stay as they were.
+    ``out`` = (out, lse) reuses buffers, ``ws`` a uint8 workspace."""
+    T, Hq, row, batch = _query_rows(q, cache)
+    for n, name in ((start, "start"), (window, "window"), (sinks, "sinks")):
+        _whole(n, name)
+    dev, B = cache.device, cache.B
+    need = 0 if ws is not None else lib.vitcop_window_attn_workspace_bytes(B, T, start, Hq, cache.Hkv, cache.d, window, sinks)
+    o, lse, ws = _attention_buffers(q, cache, out, want_lse, need, ws)
+    _check(lib.vitcop_window_attn(q.data_ptr(), row, batch, cache.desc, o.data_ptr(), _ptr(lse), T, start,
+                                  _counts(start_samples, "start_samples", (B,), dev),
+                                  _counts(n_samples, "n_samples", (B,), dev), Hq, window, sinks, scale, _ptr(ws),
+                                  ws.numel() if ws is not None else 0, _stream_of(dev)))
+    return o, lse
+
+
+def vitcop_tree_attn(q, k, v, tree, cache: Cache, start: int, start_samples=None, n_samples=None, scale: float = 0.0,
+                     want_lse: bool = True, out=None, ws=None):
+    """q [B,T,Hq,d], k, v [B,T,Hkv,d] of T <= 64 drafted tokens (views of fused QKV rows may be given): each over the first
+    start rows of the cache (start_samples[b], int32 [B], each at most start) and the drafts j whose bit j is set in
+    tree[b,t] (int64 or uint64 [B,T], or [T] for all samples) -> (out [B,T,Hq,d], lse [B,Hq,T] or None).  n_samples, ``out``
+    and ``ws`` as vitcop_window_attn's."""
+    T, Hq, row, batch = _query_rows(q, cache)
+    _whole(start, "start")
+    dev, B = cache.device, cache.B
+    shape = (B, T, cache.Hkv, cache.d)
+    k_rows, v_rows = _token_rows(k, "k", dev, shape), _token_rows(v, "v", dev, shape)
+    if tree.dtype not in (torch.int64, torch.uint64):
+        raise ValueError(f"tree must be int64 or uint64, not {tree.dtype}")
+    _expect(tree, "tree", (T,) if tree.dim() == 1 else (B, T), tree.dtype, dev)
+    need = 0 if ws is not None else lib.vitcop_tree_attn_workspace_bytes(B, T, start, Hq, cache.Hkv, cache.d)
+    o, lse, ws = _attention_buffers(q, cache, out, want_lse, need, ws)
+    _check(lib.vitcop_tree_attn(q.data_ptr(), row, batch, cache.desc, k.data_ptr(), *k_rows, v.data_ptr(), *v_rows,
+                                tree.data_ptr(), 0 if tree.dim() == 1 else T, o.data_ptr(), _ptr(lse), T, start,
+                                _counts(start_samples, "start_samples", (B,), dev),
+                                _counts(n_samples, "n_samples", (B,), dev), Hq, scale, _ptr(ws),
+                                ws.numel() if ws is not None else 0, _stream_of(dev)))
+    return o, lse
+
+
+def _layer_caches(caches, name: str, device: int):
+    """(host array of the layers' addresses, shape of one) of a list of caches [B,capacity,Hkv,d] or of one tensor of them."""
+    if isinstance(caches, torch.Tensor):
+        if caches.dim() != 5:
+            raise ValueError(f"{name} must be [n_layers,B,capacity,Hkv,d]")
+        _expect(caches, name, caches.shape, None, device)
+        L, first, step = caches.shape[0], caches.data_ptr(), caches.stride(0) * 2
+        return (C.c_void_p * L)(*range(first, first + L * step, step)) if step else (C.c_void_p * L)(), caches.shape[1:]
+    if not caches or caches[0].dim() != 4:
+        raise ValueError(f"{name}: no caches, or not [B,capacity,Hkv,d]")
+    shape = caches[0].shape
+    for t in caches:
+        _expect(t, name, shape, None, device)
+    return (C.c_void_p * len(caches))(*[t.data_ptr() for t in caches]), shape
+
+
+def vitcop_cache_append(k_caches, v_caches, k, v, start=None, start_samples=None, idx=None, n_samples=None) -> None:
+    """Rows of k, v [n_layers,B,T,Hkv,d] (either may be None; strided layers, samples and tokens) to the caches of all layers,
+    lists of [B,capacity,Hkv,d] or one tensor [n_layers,B,capacity,Hkv,d] each: row idx[b,i] (int32 [B,rows]; i itself without
+    idx) of sample b to row start + i of layer l's, start being one number or one for each layer, or start_samples[l,b] (int32
+    [n_layers,B]).  n_samples int32 [B]: the first ones of a sample's rows only."""
+    sides = [(c, t, name) for c, t, name in ((k_caches, k, "k"), (v_caches, v, "v")) if t is not None]
+    if not sides:
+        raise ValueError("k and v are both None")
+    dev = _here(sides[0][1], sides[0][2])
+    tables, strides, shape, cache_shape = [None, None], [(0, 0, 0), (0, 0, 0)], sides[0][1].shape, None
+    if len(shape) != 5:
+        raise ValueError("k and v must be [n_layers,B,T,Hkv,d]")
+    L, B, T, Hkv, d = shape
+    for caches, t, name in sides:
+        if caches is None:
+            raise ValueError(f"{name} without its caches")
+        table, of_one = _layer_caches(caches, f"{name}_caches", dev)
+        if t.shape != shape or len(table) != L or (of_one[0], of_one[2], of_one[3]) != (B, Hkv, d):
+            raise ValueError(f"{name} {tuple(t.shape)} does not fit {len(table)} caches of {tuple(of_one)}")
+        if cache_shape is not None and cache_shape != of_one:
+            raise ValueError("the caches of k and of v differ in their shape")
+        cache_shape = of_one
+        sl, sb, st, sh, sd = t.stride()
+        if t.get_device() != dev or t.dtype not in _BF16 or sd != 1 or (Hkv > 1 and sh != d):
+            raise ValueError(f"{name} must be bf16 on cuda:{dev}, a token's heads side by side")
+        side = 0 if name == "k" else 1
+        tables[side], strides[side] = table, (sl if L > 1 else 0, sb if B > 1 else 0, st if T > 1 else 0)
+    capacity = cache_shape[1]
+    rows = T
+    if idx is not None:
+        if idx.dim() != 2:
+            raise ValueError("idx must be [B,rows]")
+        rows = idx.shape[1]
+    for n in (*shape, capacity, rows):
+        _whole(n, "a size")
+    idx_ptr = _counts(idx, "idx", (B, rows), dev)
+    starts = None
+    if start_samples is None:
+        starts = [start] * L if isinstance(start, int) else list(start) if start is not None else None
+        if starts is None or len(starts) != L:
+            raise ValueError("start must be a number, one for each layer, or start_samples be given")
+        for n in starts:
+            _whole(n, "start")
+        starts = (C.c_int * L)(*starts)
+    elif start is not None:
+        raise ValueError("start beside start_samples")
+    desc = CacheAppendT(L, B, capacity, Hkv, d, T, rows, tables[0], tables[1], _ptr(k), _ptr(v), *strides[0], *strides[1], starts,
+                        _counts(start_samples, "start_samples", (L, B), dev), idx_ptr,
+                        _counts(n_samples, "n_samples", (B,), dev))
+    _check(lib.vitcop_cache_append(desc, _stream_of(dev)))

@@ -20,7 +20,7 @@ OUT = os.path.join(PKG, "libvitcop.so")
 BUILD = os.path.join(ROOT, "_build")
 
 SOURCES = ["api.hip", "knorm_select.hip", "compact.hip", "filter.hip", "attn.hip", "gemm.hip", "gemm_skinny.hip", "gemv.hip", "vic.hip", "collab.hip", "decoder.hip", "decode.hip",
-           "mx4.hip", "mx4_attn.hip", "mx4_project.hip"]
+           "mx4.hip", "mx4_attn.hip", "mx4_project.hip", "rope_axes.hip", "span_attn.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",

@@ -1460,5 +1460,201 @@ int vitcop_project_mx4(const uint16_t* x, int64_t x_row_stride, const uint8_t* w
                               ws ? ws_bytes : 0, static_cast<hipStream_t>(stream));
 }
 
+/* ------------------------------------------- prompts, tokens and drafts over a bf16 cache */
+
+static int check_cache(const char* what, const vitcop_cache_t* C, bool read) {
+    REQUIRE(C, VITCOP_EINVAL, "%s: the cache's descriptor is null", what);
+    REQUIRE(C->B >= 0 && C->capacity >= 0 && C->Hkv >= 1, VITCOP_EINVAL, "%s: B=%d capacity=%d Hkv=%d", what, C->B,
+            C->capacity, C->Hkv);
+    REQUIRE(C->d == 64 || C->d == 128, VITCOP_EUNSUPPORTED, "%s: d=%d (64 or 128)", what, C->d);
+    REQUIRE(C->B <= 65535 && C->Hkv <= 65535, VITCOP_EUNSUPPORTED, "%s: Hkv or B above 65535", what);
+    REQUIRE(C->capacity <= (1 << 30), VITCOP_EUNSUPPORTED, "%s: capacity above 2^30", what);
+    if (C->B == 0 || !read) return VITCOP_OK;
+    REQUIRE(C->k && C->v, VITCOP_EINVAL, "%s: the cache has a null pointer", what);
+    REQUIRE(aligned16(C->k) && aligned16(C->v), VITCOP_EINVAL, "%s: the cache's pointers must be 16-byte aligned", what);
+    return VITCOP_OK;
+}
+
+// Strides of rows [B,T,heads,d] (a batch stride matters with B > 1, a row stride with T > 1), such that offsets fit 64 bits.
+static int check_strides(const char* what, const char* name, int B, int T, int64_t row, int64_t batch) {
+    if (T <= 1) row = 0;
+    if (B <= 1) batch = 0;
+    REQUIRE(row >= 0 && batch >= 0 && row % 8 == 0 && batch % 8 == 0, VITCOP_EINVAL, "%s: strides of %s (%lld, %lld)", what,
+            name, (long long)row, (long long)batch);
+    REQUIRE(row < ((int64_t)1 << 31) && batch < ((int64_t)1 << 46), VITCOP_EUNSUPPORTED,
+            "%s: strides of %s (%lld, %lld) past 2^31 and 2^46", what, name, (long long)row, (long long)batch);
+    return VITCOP_OK;
+}
+
+// Rows that are written through strides: no two of them share an element.
+static bool rows_apart(int B, int T, int64_t width, int64_t row, int64_t batch) {
+    if (T > 1 && row < width) return false;
+    if (B <= 1) return true;
+    if (T <= 1) return batch >= width;
+    return batch >= (T - 1) * row + width || (batch >= width && row >= (B - 1) * batch + width);
+}
+
+int vitcop_rope_axes(const vitcop_rope_axes_t* R, void* stream) {
+    REQUIRE(R, VITCOP_EINVAL, "rope_axes: descriptor is null");
+    REQUIRE(R->B >= 0 && R->T >= 0 && R->d >= 16 && (!R->q || R->Hq >= 0) && ((!R->k && !R->v) || R->Hkv >= 0), VITCOP_EINVAL,
+            "rope_axes: B=%d T=%d Hq=%d Hkv=%d d=%d", R->B, R->T, R->Hq, R->Hkv, R->d);
+    REQUIRE(R->d % 16 == 0 && R->d <= 256, VITCOP_EUNSUPPORTED, "rope_axes: d=%d not a multiple of 16 up to 256", R->d);
+    REQUIRE(std::isfinite(R->theta) && R->theta > 1.f, VITCOP_EINVAL, "rope_axes: theta must exceed 1");
+    REQUIRE(R->n_axes >= 1 && R->n_axes <= VITCOP_MAX_AXES, VITCOP_EINVAL, "rope_axes: n_axes=%d outside [1,%d]", R->n_axes,
+            VITCOP_MAX_AXES);
+    int64_t pairs = 0;
+    for (int a = 0; a < R->n_axes; ++a) {
+        REQUIRE(R->sections[a] >= 0, VITCOP_EINVAL, "rope_axes: section %d has %d pairs", a, R->sections[a]);
+        pairs += R->sections[a];
+    }
+    REQUIRE(pairs == R->d / 2, VITCOP_EINVAL, "rope_axes: sections of %lld pairs together, not d/2 = %d", (long long)pairs,
+            R->d / 2);
+    const int64_t heads = (R->q ? (int64_t)R->Hq : 0) + (R->k ? (int64_t)R->Hkv : 0) + (R->v ? (int64_t)R->Hkv : 0);
+    REQUIRE(heads <= 65535, VITCOP_EUNSUPPORTED, "rope_axes: %lld heads a token, above 65535", (long long)heads);
+    REQUIRE(at_most(R->B, R->T, INT32_MAX) && (heads == 0 || (int64_t)R->B * R->T <= INT32_MAX / (heads * (R->d / 16))),
+            VITCOP_EUNSUPPORTED, "rope_axes: B*T*(heads a token)*d/16 of 2^31 and more");
+    const bool k_in_place = R->k && R->k_out == R->k;
+    const bool to_cache = (R->k && !k_in_place) || R->v;
+    if (to_cache) {
+        REQUIRE(R->capacity >= 0, VITCOP_EINVAL, "rope_axes: capacity=%d", R->capacity);
+        REQUIRE(R->start_samples || (R->start >= 0 && (int64_t)R->start + R->T <= R->capacity), VITCOP_EINVAL,
+                "rope_axes: rows [%d,%lld) outside [0,%d)", R->start, (long long)R->start + R->T, R->capacity);
+    }
+    if (R->B == 0 || R->T == 0 || heads == 0) return VITCOP_OK;
+    REQUIRE(R->positions, VITCOP_EINVAL, "rope_axes: null positions");
+    REQUIRE(!R->q || R->q_out, VITCOP_EINVAL, "rope_axes: null q_out");
+    REQUIRE(!R->k || R->k_out, VITCOP_EINVAL, "rope_axes: null k_out");
+    REQUIRE(!R->v || R->v_out, VITCOP_EINVAL, "rope_axes: null v_out");
+    REQUIRE(!R->v || R->v_out != R->v, VITCOP_EINVAL, "rope_axes: v_out is v");
+    REQUIRE(!k_in_place || (!R->v && R->start == 0 && !R->start_samples), VITCOP_EINVAL,
+            "rope_axes: k in place takes neither v nor a start");
+    REQUIRE(aligned16(R->q) && aligned16(R->k) && aligned16(R->v) && aligned16(R->q_out) && aligned16(R->k_out) &&
+                aligned16(R->v_out),
+            VITCOP_EINVAL, "rope_axes: pointers must be 16-byte aligned");
+    int rc = R->q ? check_strides("rope_axes", "q", R->B, R->T, R->q_row_stride, R->q_batch_stride) : VITCOP_OK;
+    if (!rc && R->k) rc = check_strides("rope_axes", "k", R->B, R->T, R->k_row_stride, R->k_batch_stride);
+    if (!rc && R->v) rc = check_strides("rope_axes", "v", R->B, R->T, R->v_row_stride, R->v_batch_stride);
+    if (rc) return rc;
+    REQUIRE((!R->q || R->q_out != R->q || rows_apart(R->B, R->T, (int64_t)R->Hq * R->d, R->q_row_stride, R->q_batch_stride)) &&
+                (!k_in_place || rows_apart(R->B, R->T, (int64_t)R->Hkv * R->d, R->k_row_stride, R->k_batch_stride)),
+            VITCOP_EINVAL, "rope_axes: rows turned in place overlap");
+    return launch_rope_axes(*R, static_cast<hipStream_t>(stream));
+}
+
+static int check_span(const char* what, int64_t B, int64_t T, int64_t start, int64_t Hq, int64_t Hkv, int d) {
+    REQUIRE(B >= 0 && T >= 0 && start >= 0 && Hq >= 1 && Hkv >= 1, VITCOP_EINVAL, "%s: B=%lld T=%lld start=%lld Hq=%lld Hkv=%lld",
+            what, (long long)B, (long long)T, (long long)start, (long long)Hq, (long long)Hkv);
+    REQUIRE(Hq % Hkv == 0, VITCOP_EINVAL, "%s: Hq=%lld not a multiple of Hkv=%lld", what, (long long)Hq, (long long)Hkv);
+    REQUIRE(d == 64 || d == 128, VITCOP_EUNSUPPORTED, "%s: d=%d (64 or 128)", what, d);
+    REQUIRE(B <= 65535 && Hkv <= 65535 && B * Hkv < (1 << 23), VITCOP_EUNSUPPORTED,
+            "%s: B or Hkv above 65535, or B*Hkv of 2^23 and more", what);
+    REQUIRE(start + T <= (1 << 30), VITCOP_EUNSUPPORTED, "%s: start + T above 2^30", what);
+    REQUIRE(at_most(B * T, Hq, (1 << 28) - 1), VITCOP_EUNSUPPORTED, "%s: B*T*Hq of 2^28 and more", what);
+    return VITCOP_OK;
+}
+
+// What the two attentions check alike, once their caches, sizes and strides have been; fills the default scale in.
+static int check_span_call(const char* what, SpanCall& c, int d, const void* ws, size_t ws_bytes, size_t need) {
+    REQUIRE(c.q && c.out, VITCOP_EINVAL, "%s: null pointer", what);
+    REQUIRE(aligned16(c.q) && aligned16(c.k) && aligned16(c.v) && aligned16(c.out) && aligned16(ws), VITCOP_EINVAL,
+            "%s: pointers must be 16-byte aligned", what);
+    REQUIRE(need == 0 || (ws && ws_bytes >= need), VITCOP_EWORKSPACE, "%s: workspace %zu < %zu", what, ws_bytes, need);
+    if (c.scale == 0.f) c.scale = 1.0f / std::sqrt((float)d);
+    return VITCOP_OK;
+}
+
+size_t vitcop_window_attn_workspace_bytes(int B, int T, int start, int Hq, int Hkv, int d, int window, int sinks) {
+    if (check_span("window_attn", B, T, start, Hq, Hkv, d) != VITCOP_OK || window < 0 || sinks < 0 || B == 0 || T == 0) return 0;
+    return span_workspace_bytes(B, T, start, Hq, Hkv, d, window, sinks);
+}
+
+int vitcop_window_attn(const uint16_t* q, int64_t q_row_stride, int64_t q_batch_stride, const vitcop_cache_t* C,
+                       uint16_t* out, float* lse_out, int T, int start, const int32_t* start_samples,
+                       const int32_t* n_samples, int Hq, int window, int sinks, float scale, void* ws, size_t ws_bytes,
+                       void* stream) {
+    int rc = check_cache("window_attn", C, T > 0);
+    if (!rc) rc = check_span("window_attn", C->B, T, start, Hq, C->Hkv, C->d);
+    if (!rc) rc = check_strides("window_attn", "q", C->B, T, q_row_stride, q_batch_stride);
+    if (rc) return rc;
+    REQUIRE((int64_t)start + T <= C->capacity, VITCOP_EINVAL, "window_attn: rows [%d,%lld) outside [0,%d)", start,
+            (long long)start + T, C->capacity);
+    REQUIRE(window >= 0 && sinks >= 0, VITCOP_EINVAL, "window_attn: window=%d sinks=%d", window, sinks);
+    REQUIRE(std::isfinite(scale) && scale >= 0.f, VITCOP_EINVAL, "window_attn: scale");
+    if (C->B == 0 || T == 0) return VITCOP_OK;
+    SpanCall c{q, q_row_stride, q_batch_stride, nullptr, nullptr, 0, 0, 0, 0, nullptr, 0, start_samples, n_samples, T, start,
+               window, sinks, scale, out, lse_out};
+    rc = check_span_call("window_attn", c, C->d, ws, ws_bytes,
+                         span_workspace_bytes(C->B, T, start, Hq, C->Hkv, C->d, window, sinks));
+    return rc ? rc : launch_span_attn(c, *C, Hq, ws, static_cast<hipStream_t>(stream));
+}
+
+size_t vitcop_tree_attn_workspace_bytes(int B, int T, int start, int Hq, int Hkv, int d) {
+    if (check_span("tree_attn", B, T, start, Hq, Hkv, d) != VITCOP_OK || T > VITCOP_MAX_DRAFTS || B == 0 || T == 0) return 0;
+    return span_workspace_bytes(B, T, start, Hq, Hkv, d, 0, 0);
+}
+
+int vitcop_tree_attn(const uint16_t* q, int64_t q_row_stride, int64_t q_batch_stride, const vitcop_cache_t* C,
+                     const uint16_t* k, int64_t k_row_stride, int64_t k_batch_stride, const uint16_t* v,
+                     int64_t v_row_stride, int64_t v_batch_stride, const uint64_t* tree, int64_t tree_batch_stride,
+                     uint16_t* out, float* lse_out, int T, int start, const int32_t* start_samples,
+                     const int32_t* n_samples, int Hq, float scale, void* ws, size_t ws_bytes, void* stream) {
+    int rc = check_cache("tree_attn", C, T > 0 && start > 0);
+    if (!rc) rc = check_span("tree_attn", C->B, T, start, Hq, C->Hkv, C->d);
+    REQUIRE(rc || T <= VITCOP_MAX_DRAFTS, VITCOP_EUNSUPPORTED, "tree_attn: T=%d above %d", T, VITCOP_MAX_DRAFTS);
+    if (!rc) rc = check_strides("tree_attn", "q", C->B, T, q_row_stride, q_batch_stride);
+    if (!rc) rc = check_strides("tree_attn", "k", C->B, T, k_row_stride, k_batch_stride);
+    if (!rc) rc = check_strides("tree_attn", "v", C->B, T, v_row_stride, v_batch_stride);
+    if (rc) return rc;
+    const int64_t width = (int64_t)C->Hkv * C->d;
+    if (T <= 1) k_row_stride = v_row_stride = width;
+    REQUIRE(k_row_stride >= width && v_row_stride >= width, VITCOP_EINVAL, "tree_attn: row strides of k and v (%lld, %lld)",
+            (long long)k_row_stride, (long long)v_row_stride);
+    REQUIRE(k_row_stride < (1 << 25) && v_row_stride < (1 << 25), VITCOP_EUNSUPPORTED,
+            "tree_attn: row strides of k and v (%lld, %lld) of 2^25 and more", (long long)k_row_stride, (long long)v_row_stride);
+    REQUIRE(tree_batch_stride == 0 || tree_batch_stride >= T, VITCOP_EINVAL, "tree_attn: batch stride of the tree %lld",
+            (long long)tree_batch_stride);
+    REQUIRE(tree_batch_stride < ((int64_t)1 << 31), VITCOP_EUNSUPPORTED, "tree_attn: batch stride of the tree past 2^31");
+    REQUIRE(start <= C->capacity, VITCOP_EINVAL, "tree_attn: start=%d above the capacity %d", start, C->capacity);
+    REQUIRE(std::isfinite(scale) && scale >= 0.f, VITCOP_EINVAL, "tree_attn: scale");
+    if (C->B == 0 || T == 0) return VITCOP_OK;
+    REQUIRE(k && v && tree, VITCOP_EINVAL, "tree_attn: null pointer");
+    REQUIRE((reinterpret_cast<uintptr_t>(tree) & 7u) == 0, VITCOP_EINVAL, "tree_attn: the tree must be 8-byte aligned");
+    SpanCall c{q, q_row_stride, q_batch_stride, k, v, k_row_stride, k_batch_stride, v_row_stride, v_batch_stride, tree,
+               tree_batch_stride, start_samples, n_samples, T, start, 0, 0, scale, out, lse_out};
+    rc = check_span_call("tree_attn", c, C->d, ws, ws_bytes, span_workspace_bytes(C->B, T, start, Hq, C->Hkv, C->d, 0, 0));
+    return rc ? rc : launch_span_attn(c, *C, Hq, ws, static_cast<hipStream_t>(stream));
+}
+
+int vitcop_cache_append(const vitcop_cache_append_t* A, void* stream) {
+    REQUIRE(A, VITCOP_EINVAL, "cache_append: descriptor is null");
+    REQUIRE(A->n_layers >= 0 && A->B >= 0 && A->capacity >= 0 && A->Hkv >= 1 && A->d >= 1 && A->T >= 0 && A->rows >= 0,
+            VITCOP_EINVAL, "cache_append: n_layers=%d B=%d capacity=%d Hkv=%d d=%d T=%d rows=%d", A->n_layers, A->B, A->capacity,
+            A->Hkv, A->d, A->T, A->rows);
+    REQUIRE((int64_t)A->Hkv * A->d % 8 == 0, VITCOP_EUNSUPPORTED, "cache_append: Hkv*d not a multiple of 8");
+    REQUIRE(A->B <= 65535 && (int64_t)A->Hkv * A->d <= INT32_MAX && at_most(A->rows, (int64_t)A->Hkv * A->d, INT32_MAX),
+            VITCOP_EUNSUPPORTED, "cache_append: B above 65535, or rows*Hkv*d of 2^31 and more");
+    REQUIRE(A->idx || A->rows <= A->T, VITCOP_EINVAL, "cache_append: %d rows of %d", A->rows, A->T);
+    if (A->n_layers == 0 || A->B == 0 || A->rows == 0) return VITCOP_OK;
+    REQUIRE(A->k || A->v, VITCOP_EINVAL, "cache_append: k and v are both null");
+    REQUIRE(aligned16(A->k) && aligned16(A->v), VITCOP_EINVAL, "cache_append: k and v must be 16-byte aligned");
+    REQUIRE((!A->k || A->k_cache) && (!A->v || A->v_cache) && (A->start || A->start_samples), VITCOP_EINVAL,
+            "cache_append: null pointer");
+    int rc = A->k ? check_strides("cache_append", "k", A->B, A->T, A->k_row_stride, A->k_batch_stride) : VITCOP_OK;
+    if (!rc && A->v) rc = check_strides("cache_append", "v", A->B, A->T, A->v_row_stride, A->v_batch_stride);
+    if (rc) return rc;
+    if (A->n_layers > 1)
+        for (const int64_t stride : {A->k ? A->k_layer_stride : 0, A->v ? A->v_layer_stride : 0})
+            REQUIRE(stride >= 0 && stride % 8 == 0 && at_most(A->n_layers, stride, (int64_t)1 << 61), VITCOP_EINVAL,
+                    "cache_append: layer stride %lld", (long long)stride);
+    for (int l = 0; l < A->n_layers; ++l) {
+        REQUIRE((!A->k || (A->k_cache[l] && aligned16(A->k_cache[l]))) && (!A->v || (A->v_cache[l] && aligned16(A->v_cache[l]))),
+                VITCOP_EINVAL, "cache_append: a cache of layer %d is null or not 16-byte aligned", l);
+        REQUIRE(A->start_samples || (A->start[l] >= 0 && (int64_t)A->start[l] + A->rows <= A->capacity), VITCOP_EINVAL,
+                "cache_append: rows [%d,%lld) of layer %d outside [0,%d)", A->start[l], (long long)A->start[l] + A->rows, l,
+                A->capacity);
+    }
+    return launch_cache_append(*A, static_cast<hipStream_t>(stream));
+}
+
 #pragma GCC visibility pop
 }  // extern "C"

@@ -49,6 +49,26 @@ int launch_attn(const uint16_t* q, const uint16_t* k, const uint16_t* v, uint16_
                 float* lse, int B, int N, int Hq, int Hkv, int d, float scale, int causal,
                 hipStream_t s, int64_t kv_batch = 0);
 
+// ---- tokens and drafts over a cache (span_attn.hip, rope_axes.hip) ---------
+// What vitcop_window_attn and vitcop_tree_attn (with `tree`, and the drafts' k and v) are given, checked.
+struct SpanCall {
+    const uint16_t* q;
+    int64_t q_row, q_batch;
+    const uint16_t *k, *v;
+    int64_t k_row, k_batch, v_row, v_batch;
+    const uint64_t* tree;
+    int64_t tree_batch;
+    const int32_t *start_samples, *n_samples;
+    int T, start, window, sinks;
+    float scale;
+    uint16_t* out;
+    float* lse;
+};
+size_t span_workspace_bytes(int B, int T, int start, int Hq, int Hkv, int d, int window, int sinks);
+int launch_span_attn(const SpanCall& c, const vitcop_cache_t& C, int Hq, void* ws, hipStream_t s);
+int launch_rope_axes(const vitcop_rope_axes_t& R, hipStream_t s);
+int launch_cache_append(const vitcop_cache_append_t& A, hipStream_t s);
+
 // ---- projection GEMM (gemm.hip) -------------------------------------------
 int gemm_sumsq_parts(int N);
 int launch_gemm(const uint16_t* x, int64_t x_stride, const uint16_t* w, uint16_t* y,
