@@ -1563,8 +1563,15 @@ static int check_span_call(const char* what, SpanCall& c, int d, const void* ws,
     return VITCOP_OK;
 }
 
+// A window of all rows is none, and there are no more sinks than rows.
+static void clamp_window(int rows, int& window, int& sinks) {
+    if (window >= rows) window = 0;
+    sinks = window == 0 ? 0 : std::min(sinks, rows);
+}
+
 size_t vitcop_window_attn_workspace_bytes(int B, int T, int start, int Hq, int Hkv, int d, int window, int sinks) {
     if (check_span("window_attn", B, T, start, Hq, Hkv, d) != VITCOP_OK || window < 0 || sinks < 0 || B == 0 || T == 0) return 0;
+    clamp_window(start + T, window, sinks);
     return span_workspace_bytes(B, T, start, Hq, Hkv, d, window, sinks);
 }
 
@@ -1581,6 +1588,7 @@ int vitcop_window_attn(const uint16_t* q, int64_t q_row_stride, int64_t q_batch_
     REQUIRE(window >= 0 && sinks >= 0, VITCOP_EINVAL, "window_attn: window=%d sinks=%d", window, sinks);
     REQUIRE(std::isfinite(scale) && scale >= 0.f, VITCOP_EINVAL, "window_attn: scale");
     if (C->B == 0 || T == 0) return VITCOP_OK;
+    clamp_window(start + T, window, sinks);
     SpanCall c{q, q_row_stride, q_batch_stride, nullptr, nullptr, 0, 0, 0, 0, nullptr, 0, start_samples, n_samples, T, start,
                window, sinks, scale, out, lse_out};
     rc = check_span_call("window_attn", c, C->d, ws, ws_bytes,

@@ -359,13 +359,32 @@ constexpr SmTable make_sm_table(bool masked, int U, int slots) {
 template <int D, int U, bool MASKED>
 constexpr SmTable SM_TABLE_OF = make_sm_table(MASKED, U, D / 8 * U);
 
-template <int D, bool CAUSAL, int U, bool REST = false>
+// WIN: AttnWhole, the keys are the queries' own rows, all of one length; or two spans of keys of a cache's tokens (see
+// span_attn.hip, which takes the calls with few query rows): AttnWindow (vitcop_window_attn), the sinks and the window;
+// AttnTree (vitcop_tree_attn), the cache and the drafts.  The queries are then the query rows of a KV head, row t * G + g being
+// head g of token t: a workgroup's rows are of few tokens, so that their windows all but coincide, and heads that share K and V
+// share the tiles.  Its keys are one of `slices` of its tiles: span a's, and then span b's, which begins with the first row that
+// one of its queries sees.  Rows past a span's end are past its descriptor and read as zeros.  The tiles that all queries of a
+// wavefront see whole run as in the other calls; the last tile of span a, the window's far edge and the diagonal, and the drafts
+// are masked.  Probabilities go into the product with V as bf16, as in the other calls of this kernel: their rounding is as
+// large as that of the output.
+struct AttnWhole {};
+struct AttnWindow {
+    SpanArgs a;
+};
+struct AttnTree {
+    SpanArgs a;
+};
+
+template <int D, bool CAUSAL, int U, bool REST = false, typename WIN = AttnWhole>
 __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
     const uint16_t* __restrict__ q, const uint16_t* __restrict__ k,
     const uint16_t* __restrict__ v, uint16_t* __restrict__ out, float* __restrict__ lse,
-    int N, int Hq, int Hkv, float scale_log2e, int n_qb, int n_heads, int group, int64_t kv_batch) {
+    int N, int Hq, int Hkv, float scale_log2e, int n_qb, int n_heads, int group, int64_t kv_batch, WIN win) {
     extern __shared__ __attribute__((aligned(1024))) char aw_lds[];
     static_assert(U == 1 || (U == 2 && D == 128), "query blocks per wavefront");
+    constexpr bool SPANS = !std::is_same<WIN, AttnWhole>::value, TREE = std::is_same<WIN, AttnTree>::value;
+    static_assert(!SPANS || (CAUSAL && !REST), "spans end with the queries' own rows");
     constexpr int BM = 128 * U, QW = 32 * U;       // queries per workgroup and per wavefront
     constexpr int DC = D / 16, DB = D / 32;        // 16-channel steps of the scores, 32-channel blocks of the output
     constexpr int ROWB = 2 * D;                    // bytes of a K or V row
@@ -396,19 +415,45 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
         hb = first + ((gsz & 7) == 0 ? (j & 7) * (gsz >> 3) + (j >> 3) : j);
         qb = CAUSAL ? n_qb - 1 - r : r;
     }
-    const int h = __builtin_amdgcn_readfirstlane(hb % Hq), b = __builtin_amdgcn_readfirstlane(hb / Hq);
-    const int hk = __builtin_amdgcn_readfirstlane(h / (Hq / Hkv));
+    const int heads = SPANS ? Hkv : Hq;
+    const int h = __builtin_amdgcn_readfirstlane(hb % heads);
+    int b = __builtin_amdgcn_readfirstlane(hb / heads), slice = 0;
+    if constexpr (SPANS) {
+        slice = b % win.a.slices;
+        b /= win.a.slices;
+    }
+    const int hk = SPANS ? h : __builtin_amdgcn_readfirstlane(h / (Hq / Hkv));
     // Query blocks are aligned to the END of the sequence: a ragged block is then the first one,
     // which has the fewest keys to waste wavefronts on (query indices below 0 do not exist).
-    const int q0 = N - (n_qb - qb) * BM, wq0 = q0 + QW * wv;
+    int n_rows = N, n_blocks = n_qb, n_tok = 0, start = 0;        // of the sample: rows (blocks of them), tokens, rows before
+    if constexpr (SPANS) {
+        n_tok = win.a.counts ? __builtin_amdgcn_readfirstlane(min(max(win.a.counts[b], 0), win.a.T)) : win.a.T;
+        start = win.a.starts ? __builtin_amdgcn_readfirstlane(min(max(win.a.starts[b], 0), win.a.start)) : win.a.start;
+        n_rows = n_tok * win.a.G;
+        n_blocks = (n_rows + BM - 1) / BM;
+        if (qb >= n_blocks) return;
+    }
+    const int q0 = n_rows - (n_blocks - qb) * BM, wq0 = q0 + QW * wv;
     const int64_t q_rs = (int64_t)Hq * D, kv_rs = (int64_t)Hkv * D;
 
     // Q^T fragments of the query blocks
     bf16x8 qf[U][DC];
+    int at[U] = {};                  // SPANS: the token of the lane's query, as a row of the cache,
+    uint32_t bits[U][2] = {};        // or of a tree the drafts that it sees
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int query = max(wq0 + 32 * u + l32, 0);
         const uint16_t* qp = q + ((int64_t)b * N + query) * q_rs + h * D + 8 * g;
+        if constexpr (SPANS) {
+            const int G = win.a.G, tok = query / G;
+            qp = q + b * win.a.q_batch + tok * win.a.q_row + (hk * G + query - tok * G) * D + 8 * g;
+            at[u] = start + tok;
+            if constexpr (TREE) {
+                const uint64_t w = win.a.tree[b * win.a.tree_batch + tok] & (~0ull >> (64 - n_tok));
+                bits[u][0] = (uint32_t)w >> (4 * g);
+                bits[u][1] = (uint32_t)(w >> 32) >> (4 * g);
+            }
+        }
 #pragma unroll
         for (int dc = 0; dc < DC; ++dc) qf[u][dc] = *reinterpret_cast<const bf16x8*>(qp + 16 * dc);
     }
@@ -435,7 +480,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
     float m_ref[U], thr[U], l_run[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        m_ref[u] = -INFINITY;
+        m_ref[u] = SPANS ? -3.0e38f : -INFINITY;      // (a tile may hide all its keys from a query)
         thr[u] = -3.0e38f;
         l_run[u] = 0.f;
     }
@@ -448,9 +493,31 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
     static_assert(!REST || (!CAUSAL && U == 1), "without the mask, one query block");
     const int rest = REST ? N % AW_BN : 0;
     const int kend = CAUSAL ? min(N, q0 + BM) : N - rest;
-    const int ntiles = (kend + AW_BN - 1) / AW_BN;                 // tiles the workgroup streams
+    int ntiles = (kend + AW_BN - 1) / AW_BN;                       // tiles the workgroup streams
     const int wave_kend = CAUSAL ? wq0 + QW : N - rest;            // keys this wavefront needs
-    const int my_tiles = wq0 + QW > 0 ? (wave_kend + AW_BN - 1) / AW_BN : 0;
+    int my_tiles = wq0 + QW > 0 ? (wave_kend + AW_BN - 1) / AW_BN : 0;
+    // SPANS: the cache row that span b begins with, the lengths of both; the tiles of this slice are numbered from 0, `skip`
+    // being those before it, and span a has those below a_tiles; the cache rows of this wavefront's tokens
+    int lo = 0, len_a = 0, len_b = 0, a_tiles = 0, skip = 0, row_first = 0, row_last = 0;
+    if constexpr (SPANS) {
+        const int G = win.a.G;
+        row_first = start + max(wq0, 0) / G;
+        row_last = start + max(wq0 + QW - 1, 0) / G;
+        if constexpr (TREE) {
+            len_a = start;
+            len_b = n_tok;
+        } else {
+            if (win.a.window) lo = max(0, start + max(q0, 0) / G - win.a.window + 1);
+            len_a = min(win.a.sinks, lo);
+            len_b = start + (q0 + BM - 1) / G + 1 - lo;
+        }
+        const int all_a = (len_a + AW_BN - 1) / AW_BN, all = all_a + (len_b + AW_BN - 1) / AW_BN;
+        const int per = all / win.a.slices, more = all - per * win.a.slices;
+        skip = slice * per + min(slice, more);
+        ntiles = per + (slice < more ? 1 : 0);
+        a_tiles = all_a - skip;
+        my_tiles = wq0 + QW <= 0 ? 0 : (TREE ? ntiles : min(ntiles, max(0, a_tiles + (row_last - lo) / AW_BN + 1)));
+    }
     // tiles whose 64 keys are visible to all 64 queries and lie inside the sequence: no masking
     const int full_tiles = min(CAUSAL ? max(wq0, 0) / AW_BN : N / AW_BN, min(N / AW_BN, my_tiles));
     const char* kbase = reinterpret_cast<const char*>(k + b * kv_batch + hk * D);
@@ -468,7 +535,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
         (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)aw_lds);
     const unsigned row_bytes = (unsigned)(kv_rs * 2);
     const unsigned tile_stride = AW_BN * row_bytes;
-    const unsigned n_rec = (unsigned)(N - 1) * row_bytes + D * 2;      // through the last row of THIS head
+    const unsigned n_rec = (unsigned)((SPANS ? len_a : N) - 1) * row_bytes + D * 2;      // through the last row of THIS head
     auto make_desc = [&](const char* base) __attribute__((always_inline)) {
         const uint64_t a = reinterpret_cast<uint64_t>(base);
         u32x4 d;                          // raw buffer: base address, no stride, byte range, 32-bit data format
@@ -480,11 +547,52 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
     };
     const u32x4 k_desc = make_desc(kbase), v_desc = make_desc(vbase);
     const unsigned lane_off = (unsigned)(GPW * wv + GROUPS * (lane / LPR)) * row_bytes + ((unsigned)(lane % LPR) << 4);
+    u32x4 k_desc_b = k_desc, v_desc_b = v_desc;                        // SPANS: of span b
+    unsigned k_row_b = row_bytes, v_row_b = row_bytes, k_off_b = lane_off, v_off_b = lane_off;
+    uint64_t seen = 0;                                                 // TREE: the drafts that a token of the sample sees
+    if constexpr (TREE) {
+        const uint64_t w = lane < n_tok ? win.a.tree[b * win.a.tree_batch + lane] : 0;
+        uint32_t w0 = (uint32_t)w, w1 = (uint32_t)(w >> 32);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            w0 |= __shfl_xor(w0, o, 64);
+            w1 |= __shfl_xor(w1, o, 64);
+        }
+        seen = (uint64_t)__builtin_amdgcn_readfirstlane(w1) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane(w0);
+        k_row_b = (unsigned)win.a.k2_row * 2;
+        v_row_b = (unsigned)win.a.v2_row * 2;
+        k_desc_b = make_desc(reinterpret_cast<const char*>(win.a.k2 + b * win.a.k2_batch + hk * D));
+        v_desc_b = make_desc(reinterpret_cast<const char*>(win.a.v2 + b * win.a.v2_batch + hk * D));
+        k_off_b = (unsigned)(GPW * wv + GROUPS * (lane / LPR)) * k_row_b + ((unsigned)(lane % LPR) << 4);
+        v_off_b = (unsigned)(GPW * wv + GROUPS * (lane / LPR)) * v_row_b + ((unsigned)(lane % LPR) << 4);
+    } else if constexpr (SPANS) {
+        k_desc_b = make_desc(kbase + lo * kv_rs * 2);
+        v_desc_b = make_desc(vbase + lo * kv_rs * 2);
+    }
+    if constexpr (SPANS) {
+        k_desc_b.z = (unsigned)(len_b - 1) * k_row_b + D * 2;
+        v_desc_b.z = (unsigned)(len_b - 1) * v_row_b + D * 2;
+    }
     // load j of tile t: row group GPW*wv + j/2 of K (j even) or V (j odd)
     auto issue_one = [&](int t, int j) __attribute__((always_inline)) {
         const int i = j >> 1;
         const unsigned stage = lds_base0 + (t % ST) * AW_STAGE<D>;
         const unsigned dst = (j & 1) ? stage + AW_KTILE<D> + (GPW * wv + i) * AW_VGRP : stage + (GPW * wv + i) * AW_KGRP;
+        if constexpr (SPANS) {
+            const bool in_b = t >= a_tiles;
+            const unsigned row = (unsigned)(in_b ? t - a_tiles : t + skip) * AW_BN + i, of_b = (j & 1) ? v_row_b : k_row_b;
+            const u32x4 desc = (j & 1) ? (in_b ? v_desc_b : v_desc) : (in_b ? k_desc_b : k_desc);
+            unsigned lane_at = lane_off;
+            if constexpr (TREE) {
+                if (in_b) {                          // (there is one such tile; drafts that no token sees: past the range)
+                    const int r = GPW * wv + GROUPS * (lane / LPR) + i;
+                    lane_at = !(seen >> r & 1) ? 0xFFFFF000u : ((j & 1) ? v_off_b : k_off_b);
+                }
+            }
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                         :: "s"(dst), "v"(lane_at), "s"(desc), "s"(row * (in_b ? of_b : row_bytes)) : "memory");
+            return;
+        }
         const unsigned off = (unsigned)t * tile_stride + (unsigned)i * row_bytes;
         if (j & 1)
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
@@ -565,7 +673,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
     auto stage_block = [&](int par, int t, auto masked_c, bool has_prev) __attribute__((always_inline)) {
         constexpr bool MASKED = decltype(masked_c)::value;
         constexpr int SLOTS = (DC + 2 * DB) * U;
-        const int key0 = t * AW_BN + 32 * par;
+        int key0 = t * AW_BN + 32 * par;
         // The fragments requested a whole block ago have long arrived; saying so here (a wait on
         // the LDS counter alone) spares the block partial waits: with its own 24 requests queued
         // behind them the 4-bit counter could not express "only the older ones".
@@ -577,12 +685,20 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
         // diagonal and ragged tiles: key key0 + 4g + 8(r/4) + r%4 of register r is visible to
         // the lane's query iff it is <= min(query, N-1), i.e. iff 8(r/4) + r%4 <= lim
         int lim[U] = {};
+        int far[U] = {}, sink = 0;       // of a window also iff it is > far, or < sink
+        uint32_t word[U] = {};           // TREE: a bit for each of the keys from key0 + 4 g on
+        if constexpr (SPANS) key0 = t < a_tiles ? (t + skip) * AW_BN + 32 * par : lo + (t - a_tiles) * AW_BN + 32 * par;
         if constexpr (MASKED) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int query = max(wq0 + 32 * u + l32, 0);      // rows below 0 are never stored
                 lim[u] = (CAUSAL ? min(query, N - 1) : N - 1) - key0 - 4 * g;
+                if constexpr (SPANS) lim[u] = (t < a_tiles ? len_a - 1 : at[u]) - key0 - 4 * g;
+                if constexpr (TREE)
+                    word[u] = t >= a_tiles ? bits[u][par] : (lim[u] < 0 ? 0u : (lim[u] >= 31 ? ~0u : (2u << lim[u]) - 1u));
+                if constexpr (SPANS && !TREE) far[u] = win.a.window == 0 ? -INT32_MAX : at[u] - win.a.window - key0 - 4 * g;
             }
+            if constexpr (SPANS && !TREE) sink = win.a.sinks - key0 - 4 * g;
         }
         // state of the vector work (see SmKind)
         float m5[U][5], m3[U][3], alpha[U];
@@ -595,7 +711,12 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
             constexpr int kind = kc.value, u = uc.value, i = ic.value;
             const f32x16& sv = s[par][u];
             if constexpr (kind == SM_MASK) {
-                if (8 * (i >> 2) + (i & 3) > lim[u]) s[par][u][i] = -INFINITY;
+                constexpr int n = 8 * (i >> 2) + (i & 3);
+                if constexpr (TREE) {
+                    if (!(word[u] >> n & 1)) s[par][u][i] = -INFINITY;
+                } else {
+                    if (n > lim[u] || (SPANS && n <= far[u] && n >= sink)) s[par][u][i] = -INFINITY;
+                }
             } else if constexpr (kind == SM_MAX5) {
                 // (the empty asm pins the instruction to its run: nothing else needs the maxima before
                 // the check, so the compiler would otherwise gather them all right in front of it)
@@ -755,7 +876,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
                 rest_v[db][j / 2] = (4 * g + j < rest ? a : 0u) | (4 * g + j + 1 < rest ? c << 16 : 0u);
             }
     }
-    issue_tile(0);
+    if (!SPANS || ntiles > 0) issue_tile(0);
     if (ntiles > 1) issue_tile(1);
     if (ST == 4 && ntiles > 2) issue_tile(2);
     if constexpr (REST) {
@@ -790,10 +911,44 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
                                                                o[0][db], 0, 0, 0);
         }
     }
-    tile_sync(0);                    // also covers the Q fragments, which were requested first
+    if (!SPANS || ntiles > 0) tile_sync(0);              // also covers the Q fragments, which were requested first
 
     int t = 1;
-    if (my_tiles > 0) {
+    if constexpr (SPANS) {
+        if (my_tiles > 0) {
+            // (the first block's product with V, of a stage that there is not, adds zeros: no branch in any block)
+            scores_only(0, 0, 0);
+            load_k_frags(0, 0, 1);
+#pragma unroll
+            for (int i = 0; i < 2 * DB; ++i) vlo[0][i] = vhi[0][i] = s16x4{0, 0, 0, 0};
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int tt = 0; tt < 2; ++tt) pf[1][u][tt] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
+            // tiles [whole, edge): all queries of this wavefront see all their keys.  (Those of a window's sinks are masked.)
+            int whole = 0, edge = len_a / AW_BN - skip;
+            if constexpr (!TREE) {
+                whole = a_tiles;
+                if (win.a.window) whole += (max(0, row_last + 1 - win.a.window - lo) + AW_BN - 1) / AW_BN;
+                edge = a_tiles + (row_first + 1 - lo) / AW_BN;
+            }
+            whole = min(max(whole, 0), my_tiles);
+            edge = min(edge, my_tiles);
+            for (t = 0; t < whole; ++t) {
+                if (t > 0) tile_sync(t);
+                tile_body(t, std::true_type{}, false);
+            }
+            for (; t < edge; ++t) {
+                if (t > 0) tile_sync(t);
+                tile_body(t, std::false_type{}, false);
+            }
+            for (; t < my_tiles; ++t) {
+                if (t > 0) tile_sync(t);
+                tile_body(t, std::true_type{}, false);
+            }
+            values_only(1, 0);
+        }
+    } else if (my_tiles > 0) {
         scores_only(0, 0, 0);
         load_k_frags(0, 0, 1);                                          // for S(1) in the first block
         t = 0;
@@ -817,9 +972,32 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
     for (int u = 0; u < U; ++u) {
         const int query = wq0 + 32 * u + l32;                          // < N by construction
         const float l_tot = l_run[u] + __shfl_xor(l_run[u], 32, 64);
+        if constexpr (SPANS) {
+            if (query >= 0 && win.a.slices > 1) {        // for span_merge_kernel
+                const int64_t slot = (((int64_t)b * Hkv + hk) * N + query) * win.a.slices + slice;
+                float* op = win.a.part_o + slot * D;
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int r4 = 0; r4 < 4; ++r4)
+                        *reinterpret_cast<f32x4*>(op + db * 32 + 8 * r4 + 4 * g) =
+                            f32x4{o[u][db][4 * r4], o[u][db][4 * r4 + 1], o[u][db][4 * r4 + 2], o[u][db][4 * r4 + 3]};
+                if (g == 0) {
+                    win.a.part_ml[slot * 2] = l_tot == 0.f ? -INFINITY : m_ref[u];
+                    win.a.part_ml[slot * 2 + 1] = l_tot;
+                }
+                continue;
+            }
+        }
         if (query >= 0) {
-            const float inv = 1.0f / l_tot;
+            const float inv = SPANS && l_tot == 0.f ? 0.f : 1.0f / l_tot;
             uint16_t* op = out + ((int64_t)b * N + query) * q_rs + h * D;
+            float* lp = lse + ((int64_t)b * Hq + h) * N + query;
+            if constexpr (SPANS) {
+                const int tok = query / win.a.G, head = hk * win.a.G + query - tok * win.a.G;
+                op = out + ((int64_t)b * win.a.T + tok) * q_rs + head * D;
+                lp = lse + ((int64_t)b * Hq + head) * win.a.T + tok;
+            }
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -830,8 +1008,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
                     *reinterpret_cast<uint2*>(op + db * 32 + 8 * r4 + 4 * g) = pk;
                 }
             if (lse && g == 0)
-                lse[((int64_t)b * Hq + h) * N + query] =
-                    (m_ref[u] + __builtin_amdgcn_logf(l_tot)) * 0.6931471805599453f;
+                *lp = SPANS && l_tot == 0.f ? -INFINITY : (m_ref[u] + __builtin_amdgcn_logf(l_tot)) * 0.6931471805599453f;
         }
     }
 }
@@ -844,13 +1021,13 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
 constexpr int AW_U2_MIN_N = 512;   // a wavefront takes two query blocks from this length on,
 constexpr int AW_U2_MIN_WGS = 256;  // if that still leaves more workgroups than this
 
-template <int D, bool CAUSAL, int U, bool REST = false>
+template <int D, bool CAUSAL, int U, bool REST = false, typename WIN = AttnWhole>
 static int launch_attn_wide(const uint16_t* q, const uint16_t* k, const uint16_t* v, uint16_t* out, float* lse,
-                            int B, int N, int Hq, int Hkv, float sl2, int64_t kv_batch, hipStream_t s) {
+                            int B, int N, int Hq, int Hkv, float sl2, int64_t kv_batch, hipStream_t s, const WIN& win = WIN{}) {
     static std::atomic<bool> attr_set{false};   // set once; a second thread repeating the call is harmless
     constexpr int lds = AW_STAGES<D> * AW_STAGE<D>;
     if (!attr_set.load(std::memory_order_acquire)) {
-        const int rc = hip_status(hipFuncSetAttribute((const void*)attn_wide_kernel<D, CAUSAL, U, REST>,
+        const int rc = hip_status(hipFuncSetAttribute((const void*)attn_wide_kernel<D, CAUSAL, U, REST, WIN>,
                                                       hipFuncAttributeMaxDynamicSharedMemorySize, lds),
                                   "hipFuncSetAttribute(attn_wide)");
         if (rc) return rc;
@@ -858,12 +1035,13 @@ static int launch_attn_wide(const uint16_t* q, const uint16_t* k, const uint16_t
     }
     constexpr int BM = 128 * U;
     const int n_qb = (N + BM - 1) / BM;
-    const long n_heads = (long)Hq * B;
+    long n_heads = (long)Hq * B;
+    if constexpr (!std::is_same<WIN, AttnWhole>::value) n_heads = (long)Hkv * B * win.a.slices;
     // (sample, head) pairs in flight together: few, so that their query blocks share K/V
     // in L2, but enough to fill the 256 CUs twice over (measured: 32 from N = 2048 up)
     const int group = std::max(32, (512 / n_qb + 7) / 8 * 8);
-    hipLaunchKernelGGL((attn_wide_kernel<D, CAUSAL, U, REST>), dim3((unsigned)(n_heads * n_qb)), dim3(256), lds, s, q, k, v,
-                       out, lse, N, Hq, Hkv, sl2, n_qb, (int)n_heads, group, kv_batch);
+    hipLaunchKernelGGL((attn_wide_kernel<D, CAUSAL, U, REST, WIN>), dim3((unsigned)(n_heads * n_qb)), dim3(256), lds, s, q, k, v,
+                       out, lse, N, Hq, Hkv, sl2, n_qb, (int)n_heads, group, kv_batch, win);
     return launch_status("attn_wide");
 }
 
@@ -903,6 +1081,20 @@ int launch_attn(const uint16_t* q, const uint16_t* k, const uint16_t* v, uint16_
                       : launch_attn_wide<128, false, 2>(q, k, v, out, lse, B, N, Hq, Hkv, sl2, kv_batch, s);
     return causal ? launch_attn_wide<128, true, 1>(q, k, v, out, lse, B, N, Hq, Hkv, sl2, kv_batch, s)
                   : launch_attn_wide<128, false, 1>(q, k, v, out, lse, B, N, Hq, Hkv, sl2, kv_batch, s);
+}
+
+// Tokens over two spans of keys, T G query rows of each (sample, KV head), in A.slices slices: see SpanArgs.
+template <typename WIN>
+static int launch_spans(const SpanArgs& A, int d, int blocks, hipStream_t s) {
+    const int R = A.T * A.G, Hq = A.Hkv * A.G;
+    auto go = [&](auto launch) {
+        return launch(A.q, A.k, A.v, A.out, A.lse, A.B, R, Hq, A.Hkv, A.scale_log2e, A.kv_batch, s, WIN{A});
+    };
+    if (d == 64) return go(launch_attn_wide<64, true, 1, false, WIN>);
+    return blocks == 2 ? go(launch_attn_wide<128, true, 2, false, WIN>) : go(launch_attn_wide<128, true, 1, false, WIN>);
+}
+int launch_attn_spans(const SpanArgs& A, int d, int blocks, hipStream_t s) {
+    return A.tree ? launch_spans<AttnTree>(A, d, blocks, s) : launch_spans<AttnWindow>(A, d, blocks, s);
 }
 
 }  // namespace vitcop

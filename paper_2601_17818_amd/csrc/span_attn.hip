@@ -19,28 +19,11 @@
 #include "span_plan.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace vitcop {
 
 constexpr float SP_SLACK = 8.f;              // log2
-
-struct SpanArgs {
-    const uint16_t* q;
-    int64_t q_row, q_batch;
-    const uint16_t *k, *v;                   // the cache
-    int64_t kv_batch;
-    const uint16_t *k2, *v2;                 // the drafts
-    int64_t k2_row, k2_batch, v2_row, v2_batch;
-    const uint64_t* tree;
-    int64_t tree_batch;
-    const int32_t *starts, *counts;
-    int B, T, G, Hkv, start, window, sinks;
-    float scale_log2e;
-    int row_blocks, slices;
-    float *part_o, *part_ml;
-    uint16_t* out;
-    float* lse;
-};
 
 __device__ __forceinline__ float span_quotient(float o, float l) { return l == 0.f ? 0.f : o / l; }
 __device__ __forceinline__ float span_lse(float m, float l) {
@@ -355,29 +338,39 @@ __global__ __launch_bounds__(SM_THREADS) void span_merge_kernel(const SpanArgs A
     if (A.lse && c == 0) A.lse[((int64_t)b * Hq + h) * A.T + t] = span_lse(mn, l);
 }
 
-static int64_t span_keys(int T, int start, int window, int sinks) {
-    const int64_t all = (int64_t)start + T;
-    return window == 0 ? all : std::min<int64_t>(all, (int64_t)window + T - 1 + sinks);
+// The rows that a block of query rows looks at, at most (of a tree those of the cache), and the launches for them.
+static SpanPlan plan_of(int B, int T, int start, int Hq, int Hkv, int d, int window, int sinks) {
+    const int64_t all = (int64_t)start + T, keys = window == 0 ? all : std::min<int64_t>(all, (int64_t)window + T + sinks);
+    return span_plan(B, Hkv, (int64_t)T * (Hq / Hkv), keys, d, (keys + 256) * Hkv * d * 2 < ((int64_t)1 << 32));
 }
 
 size_t span_workspace_bytes(int B, int T, int start, int Hq, int Hkv, int d, int window, int sinks) {
-    const size_t s = span_plan(B, Hkv, (int64_t)T * (Hq / Hkv), span_keys(T, start, window, sinks), d).slices;
+    const size_t s = plan_of(B, T, start, Hq, Hkv, d, window, sinks).slices;
     return s == 1 ? 0 : up256((size_t)B * T * Hq * s * d * 4) + up256((size_t)B * T * Hq * s * 2 * 4);
 }
 
-template <int D, bool TREE>
+template <int D>
 static int launch_span_d(SpanArgs A, int Hq, void* ws, hipStream_t s) {
-    const SpanPlan p = span_plan(A.B, A.Hkv, (int64_t)A.T * A.G, span_keys(A.T, A.start, A.window, A.sinks), D);
+    const SpanPlan p = plan_of(A.B, A.T, A.start, Hq, A.Hkv, D, A.window, A.sinks);
     A.row_blocks = p.row_blocks;
     A.slices = p.slices;
     A.part_o = static_cast<float*>(ws);
     A.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + up256((size_t)A.B * A.T * Hq * p.slices * D * 4));
-    const int64_t units = (int64_t)A.B * A.Hkv * p.slices, wgs = (units + 7) / 8 * 8 * p.row_blocks;
-    if (wgs >= (int64_t)1 << 24) return fail(VITCOP_EUNSUPPORTED, "attention over a cache: 2^24 workgroups and more");
-    auto* kernel = p.blocks == 1 ? span_attn_kernel<D, 1, TREE>
+    int rc;
+    if (p.wide) {
+        rc = launch_attn_spans(A, D, p.blocks, s);
+    } else {
+        const int64_t units = (int64_t)A.B * A.Hkv * p.slices, wgs = (units + 7) / 8 * 8 * p.row_blocks;
+        if (wgs >= (int64_t)1 << 24) return fail(VITCOP_EUNSUPPORTED, "attention over a cache: 2^24 workgroups and more");
+        auto kernel = [&](auto tree) {
+            constexpr bool TREE = decltype(tree)::value;
+            return p.blocks == 1 ? span_attn_kernel<D, 1, TREE>
                                  : (p.blocks == 2 ? span_attn_kernel<D, 2, TREE> : span_attn_kernel<D, 4, TREE>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(64 * SP_WAVES), 0, s, A);
-    const int rc = launch_status("span_attn");
+        };
+        hipLaunchKernelGGL(A.tree ? kernel(std::true_type{}) : kernel(std::false_type{}), dim3((unsigned)wgs), dim3(64 * SP_WAVES),
+                           0, s, A);
+        rc = launch_status("span_attn");
+    }
     if (rc || p.slices == 1) return rc;
     hipLaunchKernelGGL((span_merge_kernel<D>), dim3((unsigned)((int64_t)A.B * A.T * Hq)), dim3(SM_THREADS), 0, s, A);
     return launch_status("span_merge");
@@ -411,8 +404,7 @@ int launch_span_attn(const SpanCall& c, const vitcop_cache_t& C, int Hq, void* w
     A.scale_log2e = c.scale * 1.4426950408889634f;
     A.out = c.out;
     A.lse = c.lse;
-    if (c.tree) return C.d == 64 ? launch_span_d<64, true>(A, Hq, ws, s) : launch_span_d<128, true>(A, Hq, ws, s);
-    return C.d == 64 ? launch_span_d<64, false>(A, Hq, ws, s) : launch_span_d<128, false>(A, Hq, ws, s);
+    return C.d == 64 ? launch_span_d<64>(A, Hq, ws, s) : launch_span_d<128>(A, Hq, ws, s);
 }
 
 }  // namespace vitcop

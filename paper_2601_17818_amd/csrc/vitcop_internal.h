@@ -49,7 +49,28 @@ int launch_attn(const uint16_t* q, const uint16_t* k, const uint16_t* v, uint16_
                 float* lse, int B, int N, int Hq, int Hkv, int d, float scale, int causal,
                 hipStream_t s, int64_t kv_batch = 0);
 
-// ---- tokens and drafts over a cache (span_attn.hip, rope_axes.hip) ---------
+// ---- tokens and drafts over a cache (span_attn.hip, attn.hip, rope_axes.hip) ---------
+// What the kernels of vitcop_window_attn and vitcop_tree_attn are given: T tokens of G query heads to each of Hkv KV heads.
+struct SpanArgs {
+    const uint16_t* q;
+    int64_t q_row, q_batch;
+    const uint16_t *k, *v;                   // the cache
+    int64_t kv_batch;
+    const uint16_t *k2, *v2;                 // the drafts
+    int64_t k2_row, k2_batch, v2_row, v2_batch;
+    const uint64_t* tree;
+    int64_t tree_batch;
+    const int32_t *starts, *counts;
+    int B, T, G, Hkv, start, window, sinks;  // (window and sinks: below start + T, so that sums with them fit 32 bits)
+    float scale_log2e;
+    int row_blocks, slices;                  // part_o, part_ml: [B,Hkv,T*G,slices] rows of d outputs, of (reference, sum)
+    float *part_o, *part_ml;
+    uint16_t* out;
+    float* lse;
+};
+// In tiles of 64 keys, 128 or 256 query rows a workgroup (blocks 1 or 2); of more than one slice the partials are left in
+// part_o and part_ml.  Spans of less than 2^32 - 2^26 bytes.
+int launch_attn_spans(const SpanArgs& A, int d, int blocks, hipStream_t s);
 // What vitcop_window_attn and vitcop_tree_attn (with `tree`, and the drafts' k and v) are given, checked.
 struct SpanCall {
     const uint16_t* q;

@@ -2,8 +2,8 @@
 
 Bounds. A score's fp32 sum of d products and its scaling are off by at most e = (d + 4) 2^-24 of the sum of |q k| scale; a
 probability then by e twice over (its own and its sum's) and by 2^-21 of the exponential and its argument; the sums over n keys
-by n 2^-24. A probability goes into the product with V in 16 bits (half a step of the second eight: 2^-16), in calls of many
-tokens in eight (2^-8). The output is rounded to bf16: 2^-8 of it. lse: e, the sum's n 2^-24, 2^-21 and 2^-22 of its own size.
+by n 2^-24. A probability goes into the product with V in 16 bits (half a step of the second eight: 2^-16), in calls of more than
+64 query rows to a KV head in eight (2^-8). The output is rounded to bf16: 2^-8 of it. lse: e, the sum's n 2^-24, 2^-21 and 2^-22 of its own size.
 """
 import math
 
@@ -18,7 +18,7 @@ from oracle import vitcop_oracle as O
 
 pytestmark = pytest.mark.gpu
 
-FEW = 64                       # tokens of a call whose probabilities are 16 bits at any size
+FEW = 64                       # query rows to a KV head whose probabilities are 16 bits
 
 
 @pytest.fixture(scope="module")
@@ -31,12 +31,12 @@ def bits(rng, shape, std=1.0):
     return I.f32_to_bf16_bits((rng.standard_normal(shape) * std).astype(np.float32))
 
 
-def check(got, lse, want, T, where):
+def check(got, lse, want, rows, where):
     """got [n,Hq,d], lse [Hq,n] of one sample's tokens."""
     d = got.shape[-1]
     keys = want["keys"]
     e = (d + 4) * 2.0 ** -24 * want["reach"]
-    p = 2.0 ** -16 if T <= FEW else 2.0 ** -8
+    p = 2.0 ** -16 if rows <= FEW else 2.0 ** -8
     bound = 2.0 ** -8 * np.abs(want["out"]) + (p + 2 * e[..., None] + 2.0 ** -21 + keys * 2.0 ** -24) * want["mass"] * 1.01
     err = np.abs(got - want["out"])
     assert (err <= bound).all(), f"{where}: {np.max(err - bound)} over the bound {bound.flat[np.argmax(err - bound)]}"
@@ -94,7 +94,7 @@ class Case:
                 k, v, sees, scale = sample(b, n)
                 want = S.attend(self.q[b, :n], k, v, sees, scale)
                 want["keys"] = sees.shape[1]
-                check(got[b, :n], glse[b, :, :n], want, self.T, f"sample {b}")
+                check(got[b, :n], glse[b, :, :n], want, self.T * self.Hq // self.Hkv, f"sample {b}")
 
     def window(self, window, sinks, scale=0.0, **kw):
         rows = [self.held(b) + self.n(b) for b in range(self.B)]
@@ -203,7 +203,8 @@ def test_windows_and_sinks_past_the_cache(vc):
         Case(vc, 6, 1, 300, 0, 2, 2, 128).window(window, sinks)
 
 
-TREES = [
+TREES = [                                                # (of more than 64 query rows, too)
+    (1, 9, 200, 8, 1, 128), (2, 20, 63, 14, 2, 64), (1, 64, 1000, 4, 2, 128), (2, 33, 0, 4, 1, 128), (1, 40, 2100, 28, 4, 64),
     # B, T, start, Hq, Hkv, d
     (1, 1, 0, 1, 1, 128), (1, 1, 33, 4, 4, 64), (2, 8, 384, 4, 4, 128), (1, 16, 31, 28, 4, 128), (1, 17, 32, 16, 4, 64),
     (2, 25, 500, 3, 3, 128), (1, 31, 2000, 2, 2, 128), (1, 32, 64, 4, 1, 128), (1, 33, 1000, 8, 1, 64), (1, 63, 5, 2, 1, 128),
@@ -217,8 +218,9 @@ def test_tree(vc, B, T, start, Hq, Hkv, d):
 
 def test_trees_of_their_own_lengths(vc):
     for d in (64, 128):
-        c = Case(vc, 8, 5, 40, 130, 6, 2, d, starts=[130, 0, 77, 1, 129], counts=[40, 39, 0, 1, 33])
-        c.tree(trees(np.random.default_rng(9), 5, 40), fused=True)
+        for Hq in (2, 6, 16):
+            c = Case(vc, 8, 5, 40, 130, Hq, 2, d, starts=[130, 0, 77, 1, 129], counts=[40, 39, 0, 1, 33])
+            c.tree(trees(np.random.default_rng(9), 5, 40), fused=True)
 
 
 def test_any_masks(vc):
@@ -229,6 +231,8 @@ def test_any_masks(vc):
     some[0][:3], some[1][47] = [0, 1 << 47, 0], 0                    # nothing, one later draft alone
     Case(vc, 9, 2, 48, 0, 2, 1, 128).tree(some)
     Case(vc, 9, 2, 48, 37, 2, 1, 64).tree(some)
+    Case(vc, 9, 2, 48, 1500, 4, 1, 128).tree(some)
+    Case(vc, 9, 1, 64, 0, 2, 2, 64).tree([0] * 63 + [1 << 63])
     Case(vc, 9, 2, 64, 0, 4, 2, 64).tree([0] * 63 + [1 << 63])       # all but one see nothing
 
 
