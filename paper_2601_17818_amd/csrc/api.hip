@@ -1572,7 +1572,7 @@ static void clamp_window(int rows, int& window, int& sinks) {
 size_t vitcop_window_attn_workspace_bytes(int B, int T, int start, int Hq, int Hkv, int d, int window, int sinks) {
     if (check_span("window_attn", B, T, start, Hq, Hkv, d) != VITCOP_OK || window < 0 || sinks < 0 || B == 0 || T == 0) return 0;
     clamp_window(start + T, window, sinks);
-    return span_workspace_bytes(B, T, start, Hq, Hkv, d, window, sinks);
+    return span_workspace_bytes(B, T, start, Hq, Hkv, d, window, sinks, false);
 }
 
 int vitcop_window_attn(const uint16_t* q, int64_t q_row_stride, int64_t q_batch_stride, const vitcop_cache_t* C,
@@ -1592,13 +1592,13 @@ int vitcop_window_attn(const uint16_t* q, int64_t q_row_stride, int64_t q_batch_
     SpanCall c{q, q_row_stride, q_batch_stride, nullptr, nullptr, 0, 0, 0, 0, nullptr, 0, start_samples, n_samples, T, start,
                window, sinks, scale, out, lse_out};
     rc = check_span_call("window_attn", c, C->d, ws, ws_bytes,
-                         span_workspace_bytes(C->B, T, start, Hq, C->Hkv, C->d, window, sinks));
+                         span_workspace_bytes(C->B, T, start, Hq, C->Hkv, C->d, window, sinks, false));
     return rc ? rc : launch_span_attn(c, *C, Hq, ws, static_cast<hipStream_t>(stream));
 }
 
 size_t vitcop_tree_attn_workspace_bytes(int B, int T, int start, int Hq, int Hkv, int d) {
     if (check_span("tree_attn", B, T, start, Hq, Hkv, d) != VITCOP_OK || T > VITCOP_MAX_DRAFTS || B == 0 || T == 0) return 0;
-    return span_workspace_bytes(B, T, start, Hq, Hkv, d, 0, 0);
+    return span_workspace_bytes(B, T, start, Hq, Hkv, d, 0, 0, true);
 }
 
 int vitcop_tree_attn(const uint16_t* q, int64_t q_row_stride, int64_t q_batch_stride, const vitcop_cache_t* C,
@@ -1629,7 +1629,7 @@ int vitcop_tree_attn(const uint16_t* q, int64_t q_row_stride, int64_t q_batch_st
     REQUIRE((reinterpret_cast<uintptr_t>(tree) & 7u) == 0, VITCOP_EINVAL, "tree_attn: the tree must be 8-byte aligned");
     SpanCall c{q, q_row_stride, q_batch_stride, k, v, k_row_stride, k_batch_stride, v_row_stride, v_batch_stride, tree,
                tree_batch_stride, start_samples, n_samples, T, start, 0, 0, scale, out, lse_out};
-    rc = check_span_call("tree_attn", c, C->d, ws, ws_bytes, span_workspace_bytes(C->B, T, start, Hq, C->Hkv, C->d, 0, 0));
+    rc = check_span_call("tree_attn", c, C->d, ws, ws_bytes, span_workspace_bytes(C->B, T, start, Hq, C->Hkv, C->d, 0, 0, true));
     return rc ? rc : launch_span_attn(c, *C, Hq, ws, static_cast<hipStream_t>(stream));
 }
 

@@ -414,6 +414,9 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
         const int r = rem / gsz, j = rem - r * gsz;
         hb = first + ((gsz & 7) == 0 ? (j & 7) * (gsz >> 3) + (j >> 3) : j);
         qb = CAUSAL ? n_qb - 1 - r : r;
+        // samples of their own lengths: every 16 query blocks the heads move on by an XCD, or those of a long sample would keep
+        // theirs busy when the others have long been done
+        if (SPANS && (gsz & 7) == 0) hb = first + (hb - first + (r >> 4) * (gsz >> 3)) % gsz;
     }
     const int heads = SPANS ? Hkv : Hq;
     const int h = __builtin_amdgcn_readfirstlane(hb % heads);
@@ -1091,7 +1094,9 @@ static int launch_spans(const SpanArgs& A, int d, int blocks, hipStream_t s) {
         return launch(A.q, A.k, A.v, A.out, A.lse, A.B, R, Hq, A.Hkv, A.scale_log2e, A.kv_batch, s, WIN{A});
     };
     if (d == 64) return go(launch_attn_wide<64, true, 1, false, WIN>);
-    return blocks == 2 ? go(launch_attn_wide<128, true, 2, false, WIN>) : go(launch_attn_wide<128, true, 1, false, WIN>);
+    if constexpr (std::is_same<WIN, AttnWindow>::value)
+        if (blocks == 2) return go(launch_attn_wide<128, true, 2, false, WIN>);
+    return go(launch_attn_wide<128, true, 1, false, WIN>);
 }
 int launch_attn_spans(const SpanArgs& A, int d, int blocks, hipStream_t s) {
     return A.tree ? launch_spans<AttnTree>(A, d, blocks, s) : launch_spans<AttnWindow>(A, d, blocks, s);

@@ -31,7 +31,7 @@ __device__ __forceinline__ float span_lse(float m, float l) {
 }
 
 template <int D, int NB, bool TREE>
-__global__ __launch_bounds__(64 * SP_WAVES, NB == 4 ? 1 : (NB == 2 ? 2 : 3)) void span_attn_kernel(const SpanArgs A) {
+__global__ __launch_bounds__(64 * SP_WAVES, NB == 2 ? 2 : 3) void span_attn_kernel(const SpanArgs A) {
     constexpr int STEPS = D / 32, BLOCKS = D / 16, ROWS = 16 * NB;
     constexpr int VROW = 2 * D + 32;                                 // bytes of a V row in LDS: the pad keeps eight rows apart
     constexpr int LPR = D / 8, RPL = 64 / LPR, VL = SP_KEYS / RPL;   // V: lanes a row, rows a load, loads a tile
@@ -39,12 +39,7 @@ __global__ __launch_bounds__(64 * SP_WAVES, NB == 4 ? 1 : (NB == 2 ? 2 : 3)) voi
     __shared__ __attribute__((aligned(16))) char vt[SP_WAVES][SP_KEYS * VROW];
     __shared__ float sm[SP_WAVES][ROWS][2];
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, g4 = lane >> 4;
-    // Units (sample, slice, KV head) are dealt out over the XCDs, heads side by side (their rows are neighbours in memory); the
-    // row blocks of a unit stay on its XCD, whose L2 holds the keys for them.
-    const unsigned units = (unsigned)A.B * A.slices * A.Hkv;
-    const unsigned id8 = blockIdx.x >> 3, rb = id8 % (unsigned)A.row_blocks, unit = id8 / (unsigned)A.row_blocks * 8 + (blockIdx.x & 7);
-    if (unit >= units) return;
-    const int hk = unit % (unsigned)A.Hkv, bs = unit / (unsigned)A.Hkv, slice = bs % A.slices, b = bs / A.slices;
+    const int hk = blockIdx.x, b = blockIdx.z, rb = blockIdx.y / (unsigned)A.slices, slice = blockIdx.y - rb * A.slices;
     const int G = A.G, Hq = A.Hkv * G;
     const int n_tok = A.counts ? min(max(A.counts[b], 0), A.T) : A.T;
     const int start = A.starts ? min(max(A.starts[b], 0), A.start) : A.start;
@@ -280,28 +275,33 @@ __global__ __launch_bounds__(64 * SP_WAVES, NB == 4 ? 1 : (NB == 2 ? 2 : 3)) voi
     }
 }
 
-// The slices of a query row combined: a thread takes four channels of every SM_GROUPSth slice; the groups' sums meet in LDS in
-// a fixed order.
-constexpr int SM_THREADS = 256;
-template <int D>
+// The slices of a query row combined, by threads (slices, four channels) whose loads go out before the weights are known.
+// GROUPS = 1: up to SM_FEW slices, all of a thread's, a workgroup taking as many rows as it has room for.  GROUPS = 8 (d = 64: 16):
+// a thread takes every GROUPSth slice of one row, and the groups' sums meet in LDS in a fixed order.  (14336 rows of two slices
+// 5.5 us, 8876 of seven 7.5; with a workgroup to each row 14336 of four took 17.4.)
+constexpr int SM_THREADS = 256, SM_FEW = 8;
+template <int D, int GROUPS>
 __global__ __launch_bounds__(SM_THREADS) void span_merge_kernel(const SpanArgs A) {
-    constexpr int QUADS = D / 4, SM_GROUPS = SM_THREADS / QUADS, AHEAD = 4;
-    __shared__ f32x4 sums[SM_GROUPS][QUADS];
-    __shared__ float total[SM_GROUPS];
+    constexpr int QUADS = D / 4, ROWS = SM_THREADS / (QUADS * GROUPS), AHEAD = GROUPS == 1 ? SM_FEW : 4;
+    __shared__ f32x4 sums[GROUPS][QUADS];
+    __shared__ float total[GROUPS];
     const int rows = A.T * A.G, G = A.G, Hq = A.Hkv * G;
-    const unsigned pair = blockIdx.x / (unsigned)rows, r = blockIdx.x - pair * (unsigned)rows;
+    const int c = threadIdx.x % QUADS, grp = GROUPS == 1 ? 0 : threadIdx.x / QUADS;
+    const unsigned id = ROWS == 1 ? blockIdx.x : blockIdx.x * ROWS + threadIdx.x / QUADS;
+    const unsigned pair = id / (unsigned)rows, r = id - pair * (unsigned)rows;
     const int b = pair / (unsigned)A.Hkv, hk = pair - b * A.Hkv;
     const int t = (int)r / G, h = hk * G + (int)r - t * G;
-    if (t >= (A.counts ? A.counts[b] : A.T)) return;
-    const int c = threadIdx.x % QUADS, grp = threadIdx.x / QUADS;
-    const float* po = A.part_o + (int64_t)blockIdx.x * A.slices * D + 4 * c;
-    const float2* ml = reinterpret_cast<const float2*>(A.part_ml) + (int64_t)blockIdx.x * A.slices;
+    if (b >= A.B || t >= (A.counts ? A.counts[b] : A.T)) return;         // (one row: for all of its threads)
+    const float* po = A.part_o + (int64_t)id * A.slices * D + 4 * c;
+    const float2* ml = reinterpret_cast<const float2*>(A.part_ml) + (int64_t)id * A.slices;
     f32x4 x[AHEAD];
     float2 w[AHEAD];
     auto request = [&](int s0) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            const int s = s0 + i * SM_GROUPS;
+            const int s = s0 + i * GROUPS;
+            w[i] = float2{-INFINITY, 0.f};
+            x[i] = f32x4{0.f, 0.f, 0.f, 0.f};
             if (s < A.slices) {
                 x[i] = *reinterpret_cast<const f32x4*>(po + (int64_t)s * D);
                 w[i] = ml[s];
@@ -310,48 +310,66 @@ __global__ __launch_bounds__(SM_THREADS) void span_merge_kernel(const SpanArgs A
     };
     request(grp);
     float mn = -INFINITY;
-    for (int s = threadIdx.x & 63; s < A.slices; s += 64) mn = fmaxf(mn, ml[s].x);
-    mn = wave_max(mn);
+    if constexpr (GROUPS == 1) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) mn = fmaxf(mn, w[i].x);
+    } else {
+        for (int s = threadIdx.x & 63; s < A.slices; s += 64) mn = fmaxf(mn, ml[s].x);
+        mn = wave_max(mn);
+    }
     f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
     float l = 0.f;
-    for (int s0 = grp; s0 < A.slices; s0 += AHEAD * SM_GROUPS) {
+    for (int s0 = grp; s0 < A.slices; s0 += AHEAD * GROUPS) {
         if (s0 != grp) request(s0);
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i)
-            if (s0 + i * SM_GROUPS < A.slices) {
-                const float a = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(w[i].x - mn);
-                v += x[i] * a;
-                l += w[i].y * a;
-            }
+        for (int i = 0; i < AHEAD; ++i) {
+            const float a = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(w[i].x - mn);
+            v += x[i] * a;
+            l += w[i].y * a;
+        }
     }
-    sums[grp][c] = v;
-    if (c == 0) total[grp] = l;
-    __syncthreads();
-    if (grp != 0) return;
+    if constexpr (GROUPS > 1) {
+        sums[grp][c] = v;
+        if (c == 0) total[grp] = l;
+        __syncthreads();
+        if (grp != 0) return;
 #pragma unroll
-    for (int i = 1; i < SM_GROUPS; ++i) {
-        v += sums[i][c];
-        l += total[i];
+        for (int i = 1; i < GROUPS; ++i) {
+            v += sums[i][c];
+            l += total[i];
+        }
     }
     *reinterpret_cast<uint2*>(A.out + (((int64_t)b * A.T + t) * Hq + h) * D + 4 * c) =
         make_uint2(pack_bf16(span_quotient(v.x, l), span_quotient(v.y, l)), pack_bf16(span_quotient(v.z, l), span_quotient(v.w, l)));
     if (A.lse && c == 0) A.lse[((int64_t)b * Hq + h) * A.T + t] = span_lse(mn, l);
 }
 
-// The rows that a block of query rows looks at, at most (of a tree those of the cache), and the launches for them.
-static SpanPlan plan_of(int B, int T, int start, int Hq, int Hkv, int d, int window, int sinks) {
-    const int64_t all = (int64_t)start + T, keys = window == 0 ? all : std::min<int64_t>(all, (int64_t)window + T + sinks);
-    return span_plan(B, Hkv, (int64_t)T * (Hq / Hkv), keys, d, (keys + 256) * Hkv * d * 2 < ((int64_t)1 << 32));
+template <int D>
+static int launch_span_merge(const SpanArgs& A, hipStream_t s) {
+    const int64_t rows = (int64_t)A.B * A.T * A.G * A.Hkv;
+    constexpr int GROUPS = SM_THREADS / (D / 4);
+    if (A.slices <= SM_FEW)
+        hipLaunchKernelGGL((span_merge_kernel<D, 1>), dim3((unsigned)((rows + GROUPS - 1) / GROUPS)), dim3(SM_THREADS), 0, s, A);
+    else
+        hipLaunchKernelGGL((span_merge_kernel<D, GROUPS>), dim3((unsigned)rows), dim3(SM_THREADS), 0, s, A);
+    return launch_status("span_merge");
 }
 
-size_t span_workspace_bytes(int B, int T, int start, int Hq, int Hkv, int d, int window, int sinks) {
-    const size_t s = plan_of(B, T, start, Hq, Hkv, d, window, sinks).slices;
+static SpanPlan plan_of(int B, int T, int start, int Hq, int Hkv, int d, int window, int sinks, bool tree) {
+    // the wide kernel addresses a span with 32 bits of bytes
+    const int64_t all = (int64_t)start + T, keys = window == 0 ? all : std::min<int64_t>(all, (int64_t)window + T);
+    return span_plan(SpanSizes{B, Hkv, T, Hq / Hkv, start, window, sinks, d, tree},
+                     (std::max<int64_t>(keys, sinks) + 256) * Hkv * d * 2 < ((int64_t)1 << 32));
+}
+
+size_t span_workspace_bytes(int B, int T, int start, int Hq, int Hkv, int d, int window, int sinks, bool tree) {
+    const size_t s = plan_of(B, T, start, Hq, Hkv, d, window, sinks, tree).slices;
     return s == 1 ? 0 : up256((size_t)B * T * Hq * s * d * 4) + up256((size_t)B * T * Hq * s * 2 * 4);
 }
 
 template <int D>
 static int launch_span_d(SpanArgs A, int Hq, void* ws, hipStream_t s) {
-    const SpanPlan p = plan_of(A.B, A.T, A.start, Hq, A.Hkv, D, A.window, A.sinks);
+    const SpanPlan p = plan_of(A.B, A.T, A.start, Hq, A.Hkv, D, A.window, A.sinks, A.tree != nullptr);
     A.row_blocks = p.row_blocks;
     A.slices = p.slices;
     A.part_o = static_cast<float*>(ws);
@@ -360,20 +378,16 @@ static int launch_span_d(SpanArgs A, int Hq, void* ws, hipStream_t s) {
     if (p.wide) {
         rc = launch_attn_spans(A, D, p.blocks, s);
     } else {
-        const int64_t units = (int64_t)A.B * A.Hkv * p.slices, wgs = (units + 7) / 8 * 8 * p.row_blocks;
-        if (wgs >= (int64_t)1 << 24) return fail(VITCOP_EUNSUPPORTED, "attention over a cache: 2^24 workgroups and more");
+        if ((int64_t)p.slices * p.row_blocks > 65535) return fail(VITCOP_EUNSUPPORTED, "attention over a cache: too many query rows");
         auto kernel = [&](auto tree) {
             constexpr bool TREE = decltype(tree)::value;
-            return p.blocks == 1 ? span_attn_kernel<D, 1, TREE>
-                                 : (p.blocks == 2 ? span_attn_kernel<D, 2, TREE> : span_attn_kernel<D, 4, TREE>);
+            return p.blocks == 1 ? span_attn_kernel<D, 1, TREE> : span_attn_kernel<D, 2, TREE>;
         };
-        hipLaunchKernelGGL(A.tree ? kernel(std::true_type{}) : kernel(std::false_type{}), dim3((unsigned)wgs), dim3(64 * SP_WAVES),
-                           0, s, A);
+        hipLaunchKernelGGL(A.tree ? kernel(std::true_type{}) : kernel(std::false_type{}),
+                           dim3(A.Hkv, p.slices * p.row_blocks, A.B), dim3(64 * SP_WAVES), 0, s, A);
         rc = launch_status("span_attn");
     }
-    if (rc || p.slices == 1) return rc;
-    hipLaunchKernelGGL((span_merge_kernel<D>), dim3((unsigned)((int64_t)A.B * A.T * Hq)), dim3(SM_THREADS), 0, s, A);
-    return launch_status("span_merge");
+    return rc || p.slices == 1 ? rc : launch_span_merge<D>(A, s);
 }
 
 int launch_span_attn(const SpanCall& c, const vitcop_cache_t& C, int Hq, void* ws, hipStream_t s) {

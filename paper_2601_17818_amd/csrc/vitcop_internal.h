@@ -85,7 +85,7 @@ struct SpanCall {
     uint16_t* out;
     float* lse;
 };
-size_t span_workspace_bytes(int B, int T, int start, int Hq, int Hkv, int d, int window, int sinks);
+size_t span_workspace_bytes(int B, int T, int start, int Hq, int Hkv, int d, int window, int sinks, bool tree);
 int launch_span_attn(const SpanCall& c, const vitcop_cache_t& C, int Hq, void* ws, hipStream_t s);
 int launch_rope_axes(const vitcop_rope_axes_t& R, hipStream_t s);
 int launch_cache_append(const vitcop_cache_append_t& A, hipStream_t s);

@@ -3,7 +3,7 @@
 Bounds. A score's fp32 sum of d products and its scaling are off by at most e = (d + 4) 2^-24 of the sum of |q k| scale; a
 probability then by e twice over (its own and its sum's) and by 2^-21 of the exponential and its argument; the sums over n keys
 by n 2^-24. A probability goes into the product with V in 16 bits (half a step of the second eight: 2^-16), in calls of more than
-64 query rows to a KV head in eight (2^-8). The output is rounded to bf16: 2^-8 of it. lse: e, the sum's n 2^-24, 2^-21 and 2^-22 of its own size.
+32 query rows to a KV head in eight (2^-8). The output is rounded to bf16: 2^-8 of it. lse: e, the sum's n 2^-24, 2^-21 and 2^-22 of its own size.
 """
 import math
 
@@ -18,7 +18,7 @@ from oracle import vitcop_oracle as O
 
 pytestmark = pytest.mark.gpu
 
-FEW = 64                       # query rows to a KV head whose probabilities are 16 bits
+FEW = 32                       # query rows to a KV head whose probabilities are 16 bits
 
 
 @pytest.fixture(scope="module")
