@@ -658,12 +658,13 @@ int vitcop_tree_attn(const uint16_t* q, int64_t q_row_stride, int64_t q_batch_st
                      uint16_t* out, float* lse_out, int T, int start, const int32_t* start_samples,
                      const int32_t* n_samples, int Hq, float scale, void* ws, size_t ws_bytes, void* stream);
 
-/* Rows to the caches of all layers in one launch for 64 of them: row i < n_b of sample b, which is row idx[b,i] of k and v
+/* Rows to the caches of all layers in one launch (for 64 of them, where they are given one by one): row i < n_b of sample b, which is row idx[b,i] of k and v
  * (i, without idx), goes to row start + i of its cache in layer l: start[l], or start_samples[l*B + b] (caches of a pruned
  * prefill have lengths of their own in each layer).  n_b: `rows`, or n_samples[b] clamped to [0, rows].  Sources outside
  * [0,T) and targets outside [0,capacity) are skipped on the device; all other rows stay as they were.
- *   k_cache, v_cache: host arrays of n_layers device pointers, each [B,capacity,Hkv,d]; start: host [n_layers], not looked
- *   at with start_samples.  start[l] + rows <= capacity is checked; without idx, rows <= T.
+ *   k_cache, v_cache: host arrays of n_layers device pointers, each [B,capacity,Hkv,d]; with a cache_layer_stride other than
+ *   0, arrays of one, the first layer's, behind which the others lie that many elements apart
+ *   start: host [n_layers], not looked at with start_samples.  start[l] + rows <= capacity is checked; without idx, rows <= T.
  *   k, v [n_layers,B,T,Hkv,d] with strides (the row stride is not looked at where T is 1); one of the two may be NULL,
  *   and its caches too.  They overlap no cache.
  * Hkv*d % 8 == 0; B <= 65535; rows*Hkv*d < 2^31. */
@@ -671,6 +672,7 @@ typedef struct {
     int n_layers, B, capacity, Hkv, d, T, rows;
     uint16_t* const* k_cache;
     uint16_t* const* v_cache;
+    int64_t cache_layer_stride;
     const uint16_t *k, *v;
     int64_t k_layer_stride, k_batch_stride, k_row_stride, v_layer_stride, v_batch_stride, v_row_stride;
     const int* start;

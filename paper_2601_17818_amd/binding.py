@@ -128,6 +128,7 @@ class CacheT(C.Structure):
 VITCOP_MAX_AXES = 4
 VITCOP_MAX_DRAFTS = 64
 _Sections = C.c_int * VITCOP_MAX_AXES
+_OneCache = C.c_void_p * 1
 
 
 class RopeAxesT(C.Structure):
@@ -141,7 +142,8 @@ class RopeAxesT(C.Structure):
 
 class CacheAppendT(C.Structure):
     _fields_ = ([(n, C.c_int) for n in ("n_layers", "B", "capacity", "Hkv", "d", "T", "rows")] +
-                [("k_cache", C.POINTER(C.c_void_p)), ("v_cache", C.POINTER(C.c_void_p)), ("k", C.c_void_p), ("v", C.c_void_p)] +
+                [("k_cache", C.POINTER(C.c_void_p)), ("v_cache", C.POINTER(C.c_void_p)), ("cache_layer_stride", C.c_int64),
+                 ("k", C.c_void_p), ("v", C.c_void_p)] +
                 [(n, C.c_int64) for n in ("k_layer_stride", "k_batch_stride", "k_row_stride",
                                            "v_layer_stride", "v_batch_stride", "v_row_stride")] +
                 [("start", C.POINTER(C.c_int))] + [(n, C.c_void_p) for n in ("start_samples", "idx", "n_samples")])
@@ -1084,15 +1086,17 @@ class Cache:
 
     def __init__(self, k, v):
         device = _here(k, "k")
-        if k.dim() != 4:
+        shape = k.shape
+        if len(shape) != 4:
             raise ValueError("k must be [B,capacity,Hkv,d]")
-        B, capacity, Hkv, d = shape = k.shape
-        if max(shape) > _MOST:
+        B, capacity, Hkv, d = shape
+        if B > _MOST or capacity > _MOST or Hkv > _MOST or d > _MOST:
             _past(max(shape), "k")
         _expect(k, "k", shape, None, device)
         _expect(v, "v", shape, None, device)
-        self.__dict__.update(device=device, B=B, capacity=capacity, Hkv=Hkv, d=d, k=k, v=v,
-                             desc=CacheT(B, capacity, Hkv, d, k.data_ptr(), v.data_ptr()))
+        own = self.__dict__
+        own["device"], own["B"], own["capacity"], own["Hkv"], own["d"], own["k"], own["v"] = device, B, capacity, Hkv, d, k, v
+        own["desc"] = CacheT(B, capacity, Hkv, d, k.data_ptr(), v.data_ptr())
 
     def __setattr__(self, name, value):
         raise AttributeError(f"{name}: the descriptor holds the tensors' addresses; make another Cache")
@@ -1100,16 +1104,17 @@ class Cache:
 
 def _token_rows(t, name: str, device: int, shape):
     """(row stride, batch stride) of bf16 rows [B,T,heads,d] whose heads lie side by side."""
-    if t.get_device() != device:
-        raise ValueError(f"{name} is on {t.device}, not on cuda:{device}")
-    if t.shape != shape or t.dtype not in _BF16:
+    if t.shape != shape or t.dtype not in _BF16 or t.get_device() != device:
+        if t.get_device() != device:
+            raise ValueError(f"{name} is on {t.device}, not on cuda:{device}")
         raise ValueError(f"{name} must be bf16 {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
     B, T, heads, d = shape
     sb, st, sh, sd = t.stride()
-    if sd != 1 or (heads > 1 and sh != d):
+    if sd != 1 or (sh != d and heads > 1):
         raise ValueError(f"{name}: a token's heads must lie side by side")
-    row = st if T > 1 else heads * d
-    return row, sb if B > 1 else T * row
+    if T <= 1:
+        st = heads * d
+    return st, sb if B > 1 else T * st
 
 
 def _counts(t, name: str, shape, device: int):
@@ -1135,93 +1140,103 @@ def vitcop_rope_axes(q, k, positions, sections, theta: float = 10000.0, v=None, 
     if like is None:
         raise ValueError("q, k and v are all None")
     dev = _here(like, "the tokens")
-    if like.dim() != 4:
+    shape = like.shape
+    if len(shape) != 4:
         raise ValueError("the tokens must be [B,T,heads,d]")
-    B, T, _, d = like.shape
+    B, T, _, d = shape
     n_axes = len(sections)
     if not 1 <= n_axes <= VITCOP_MAX_AXES:
         raise ValueError(f"{n_axes} sections (1 to {VITCOP_MAX_AXES})")
-    for n in (*sections, *like.shape, start):
-        _whole(n, "a size, section or start")
+    if max(*sections, *shape, start) > _MOST or min(*sections, start) < _LEAST:
+        _past(max(*sections, *shape, start, key=abs), "a size, section or start")
     _expect(positions, "positions", (n_axes, B, T), torch.int32, dev)
-    Hq = Hkv = capacity = 0
-    q_rows = k_rows = v_rows = (0, 0)
-    k_to = v_to = None
+    Hq = Hkv = capacity = q_row = q_batch = k_row = k_batch = v_row = v_batch = 0
+    q_at = q_to = k_at = k_to = v_at = v_to = None
     if q is not None:
-        Hq = q.shape[2] if q.dim() == 4 else 0
-        q_rows = _token_rows(q, "q", dev, (B, T, Hq, d))
+        Hq, q_at = q.shape[2], q.data_ptr()
+        q_row, q_batch = _token_rows(q, "q", dev, (B, T, Hq, d))
         if out is None:
             out = torch.empty((B, T, Hq, d), dtype=q.dtype, device=q.device)
-        elif out is not q and out.data_ptr() != q.data_ptr():
+        q_to = out.data_ptr()
+        if q_to != q_at:
             _expect(out, "out", (B, T, Hq, d), None, dev)
-        elif _token_rows(out, "out", dev, (B, T, Hq, d)) != q_rows:
+        elif out is not q and _token_rows(out, "out", dev, (B, T, Hq, d)) != (q_row, q_batch):
             raise ValueError("out begins where q does, with other strides")
     elif out is not None:
         raise ValueError("out without q")
-    if k is not None or v is not None:
-        Hkv = (k if k is not None else v).shape[2] if (k if k is not None else v).dim() == 4 else 0
     if k is not None:
-        k_rows = _token_rows(k, "k", dev, (B, T, Hkv, d))
+        k_shape = k.shape
+        Hkv, k_at = k_shape[2] if len(k_shape) == 4 else 0, k.data_ptr()
+        k_row, k_batch = _token_rows(k, "k", dev, (B, T, Hkv, d))
     if v is not None:
-        v_rows = _token_rows(v, "v", dev, (B, T, Hkv, d))
+        v_shape = v.shape
+        Hkv, v_at = Hkv if k is not None else (v_shape[2] if len(v_shape) == 4 else 0), v.data_ptr()
+        v_row, v_batch = _token_rows(v, "v", dev, (B, T, Hkv, d))
+    if Hkv > _MOST:
+        _past(Hkv, "k and v")
     if cache is not None:
         if k is None and v is None:
             raise ValueError("a cache without k and v")
         if k_out is not None:
             raise ValueError("k_out beside a cache")
-        if cache.device != dev or cache.B != B or (cache.Hkv, cache.d) != (Hkv, d):
+        desc = cache.desc
+        if cache.device != dev or desc.B != B or desc.Hkv != Hkv or desc.d != d:
             raise ValueError(f"the cache is for {cache.B} samples and {cache.Hkv} heads of {cache.d} on cuda:{cache.device}")
-        capacity = cache.capacity
-        k_to, v_to = _ptr(cache.k if k is not None else None), _ptr(cache.v if v is not None else None)
+        capacity, k_to, v_to = desc.capacity, desc.k if k is not None else None, desc.v if v is not None else None
     elif v is not None or start or start_samples is not None:
         raise ValueError("v and a start need a cache")
     elif k is not None:
         capacity = T
         if k_out is None:
             k_out = torch.empty((B, T, Hkv, d), dtype=k.dtype, device=k.device)
-        elif k_out is not k and k_out.data_ptr() != k.data_ptr():
-            _expect(k_out, "k_out", (B, T, Hkv, d), None, dev)
-        elif _token_rows(k_out, "k_out", dev, (B, T, Hkv, d)) != k_rows:
-            raise ValueError("k_out begins where k does, with other strides")
         k_to = k_out.data_ptr()
+        if k_to != k_at:
+            _expect(k_out, "k_out", (B, T, Hkv, d), None, dev)
+        elif k_out is not k and _token_rows(k_out, "k_out", dev, (B, T, Hkv, d)) != (k_row, k_batch):
+            raise ValueError("k_out begins where k does, with other strides")
     elif k_out is not None:
         raise ValueError("k_out without k")
-    desc = RopeAxesT(B, T, Hq, Hkv, d, n_axes, 1 if interleaved else 0, _Sections(*sections), theta, capacity, start,
-                     positions.data_ptr(), _ptr(q), _ptr(k), _ptr(v), *q_rows, *k_rows, *v_rows, _ptr(out), k_to, v_to,
-                     _counts(start_samples, "start_samples", (B,), dev), _counts(n_samples, "n_samples", (B,), dev))
-    _check(lib.vitcop_rope_axes(desc, _stream_of(dev)))
+    _check(lib.vitcop_rope_axes(
+        RopeAxesT(B, T, Hq, Hkv, d, n_axes, 1 if interleaved else 0, _Sections(*sections), theta, capacity, start,
+                  positions.data_ptr(), q_at, k_at, v_at, q_row, q_batch, k_row, k_batch, v_row, v_batch, q_to, k_to, v_to,
+                  _counts(start_samples, "start_samples", (B,), dev) if start_samples is not None else None,
+                  _counts(n_samples, "n_samples", (B,), dev) if n_samples is not None else None), _stream_of(dev)))
     return out, k_out
 
 
-def _attention_buffers(q, cache: Cache, out, want_lse: bool, nbytes: int, ws):
-    """(out, lse, ws) of an attention of q [B,T,Hq,d] over a cache, made or checked."""
-    B, T, Hq, d = q.shape
+def _attention_buffers(q, shape, cache: Cache, out, want_lse: bool, nbytes: int, ws):
+    """(out, its address, lse, its address, ws's address and bytes, ws) of an attention of q [B,T,Hq,d] over a cache, made or
+    checked."""
+    B, T, Hq, d = shape
     if out is None:
-        o = torch.empty((B, T, Hq, d), dtype=q.dtype, device=q.device)
+        o = torch.empty(shape, dtype=q.dtype, device=q.device)
         lse = torch.empty((B, Hq, T), dtype=torch.float32, device=q.device) if want_lse else None
     else:
         o, lse = out
-        _expect(o, "out", q.shape, None, cache.device)
+        _expect(o, "out", shape, None, cache.device)
         if lse is not None:
             _expect(lse, "lse", (B, Hq, T), torch.float32, cache.device)
     if ws is None:
-        ws = _ws(nbytes, q) if nbytes else None
-    elif ws.get_device() != cache.device or ws.dtype is not torch.uint8 or not ws.is_contiguous():
+        if nbytes:
+            ws = q.new_empty((nbytes,), dtype=torch.uint8)
+            return o, o.data_ptr(), lse, None if lse is None else lse.data_ptr(), ws.data_ptr(), nbytes, ws
+        return o, o.data_ptr(), lse, None if lse is None else lse.data_ptr(), None, 0, None
+    if ws.get_device() != cache.device or ws.dtype is not torch.uint8 or not ws.is_contiguous():
         raise ValueError(f"ws must be a contiguous uint8 tensor on cuda:{cache.device}")
-    return o, lse, ws
+    return o, o.data_ptr(), lse, None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.numel(), ws
 
 
 def _query_rows(q, cache: Cache):
-    """(T, Hq, row stride, batch stride) of q [B,T,Hq,d] beside a cache."""
+    """(shape, row stride, batch stride) of q [B,T,Hq,d] beside a cache."""
     dev = _here(q, "q")
-    if q.dim() != 4:
-        raise ValueError("q must be [B,T,Hq,d]")
-    T, Hq = q.shape[1], q.shape[2]
-    if T > _MOST or Hq > _MOST:
-        _past(max(T, Hq), "q")
+    shape = q.shape
+    if len(shape) != 4 or shape[0] != cache.B or shape[3] != cache.d:
+        raise ValueError(f"q must be [{cache.B},T,Hq,{cache.d}], not {tuple(shape)}")
     if cache.device != dev:
         raise ValueError(f"the cache is on cuda:{cache.device}, q on cuda:{dev}")
-    return (T, Hq, *_token_rows(q, "q", dev, (cache.B, T, Hq, cache.d)))
+    if shape[1] > _MOST or shape[2] > _MOST:
+        _past(max(shape[1], shape[2]), "q")
+    return (shape, *_token_rows(q, "q", dev, shape))
 
 
 def vitcop_window_attn(q, cache: Cache, start: int, window: int = 0, sinks: int = 0, start_samples=None, n_samples=None,
@@ -1230,16 +1245,17 @@ def vitcop_window_attn(q, cache: Cache, start: int, window: int = 0, sinks: int 
     start), over the rows j up to its own with j > row - window or j < sinks (window 0: all) -> (out [B,T,Hq,d],
     lse [B,Hq,T] or None).  n_samples int32 [B]: the first ones of a sample's tokens only, others' results stay as they were.
     ``out`` = (out, lse) reuses buffers, ``ws`` a uint8 workspace."""
-    T, Hq, row, batch = _query_rows(q, cache)
-    for n, name in ((start, "start"), (window, "window"), (sinks, "sinks")):
-        _whole(n, name)
-    dev, B = cache.device, cache.B
-    need = 0 if ws is not None else lib.vitcop_window_attn_workspace_bytes(B, T, start, Hq, cache.Hkv, cache.d, window, sinks)
-    o, lse, ws = _attention_buffers(q, cache, out, want_lse, need, ws)
-    _check(lib.vitcop_window_attn(q.data_ptr(), row, batch, cache.desc, o.data_ptr(), _ptr(lse), T, start,
-                                  _counts(start_samples, "start_samples", (B,), dev),
-                                  _counts(n_samples, "n_samples", (B,), dev), Hq, window, sinks, scale, _ptr(ws),
-                                  ws.numel() if ws is not None else 0, _stream_of(dev)))
+    shape, row, batch = _query_rows(q, cache)
+    B, T, Hq, d = shape
+    if max(start, window, sinks) > _MOST or min(start, window, sinks) < _LEAST:
+        _past(max(start, window, sinks, key=abs), "start, window or sinks")
+    dev = cache.device
+    need = 0 if ws is not None else lib.vitcop_window_attn_workspace_bytes(B, T, start, Hq, cache.Hkv, d, window, sinks)
+    o, o_at, lse, lse_at, ws_at, ws_bytes, ws = _attention_buffers(q, shape, cache, out, want_lse, need, ws)
+    _check(lib.vitcop_window_attn(q.data_ptr(), row, batch, cache.desc, o_at, lse_at, T, start,
+                                  _counts(start_samples, "start_samples", (B,), dev) if start_samples is not None else None,
+                                  _counts(n_samples, "n_samples", (B,), dev) if n_samples is not None else None, Hq, window,
+                                  sinks, scale, ws_at, ws_bytes, _stream_of(dev)))
     return o, lse
 
 
@@ -1249,38 +1265,41 @@ def vitcop_tree_attn(q, k, v, tree, cache: Cache, start: int, start_samples=None
     start rows of the cache (start_samples[b], int32 [B], each at most start) and the drafts j whose bit j is set in
     tree[b,t] (int64 or uint64 [B,T], or [T] for all samples) -> (out [B,T,Hq,d], lse [B,Hq,T] or None).  n_samples, ``out``
     and ``ws`` as vitcop_window_attn's."""
-    T, Hq, row, batch = _query_rows(q, cache)
+    shape, row, batch = _query_rows(q, cache)
+    B, T, Hq, d = shape
     _whole(start, "start")
-    dev, B = cache.device, cache.B
-    shape = (B, T, cache.Hkv, cache.d)
-    k_rows, v_rows = _token_rows(k, "k", dev, shape), _token_rows(v, "v", dev, shape)
+    dev, Hkv = cache.device, cache.Hkv
+    k_row, k_batch = _token_rows(k, "k", dev, (B, T, Hkv, d))
+    v_row, v_batch = _token_rows(v, "v", dev, (B, T, Hkv, d))
     if tree.dtype not in (torch.int64, torch.uint64):
         raise ValueError(f"tree must be int64 or uint64, not {tree.dtype}")
-    _expect(tree, "tree", (T,) if tree.dim() == 1 else (B, T), tree.dtype, dev)
-    need = 0 if ws is not None else lib.vitcop_tree_attn_workspace_bytes(B, T, start, Hq, cache.Hkv, cache.d)
-    o, lse, ws = _attention_buffers(q, cache, out, want_lse, need, ws)
-    _check(lib.vitcop_tree_attn(q.data_ptr(), row, batch, cache.desc, k.data_ptr(), *k_rows, v.data_ptr(), *v_rows,
-                                tree.data_ptr(), 0 if tree.dim() == 1 else T, o.data_ptr(), _ptr(lse), T, start,
-                                _counts(start_samples, "start_samples", (B,), dev),
-                                _counts(n_samples, "n_samples", (B,), dev), Hq, scale, _ptr(ws),
-                                ws.numel() if ws is not None else 0, _stream_of(dev)))
+    own = tree.dim() != 1
+    _expect(tree, "tree", (B, T) if own else (T,), tree.dtype, dev)
+    need = 0 if ws is not None else lib.vitcop_tree_attn_workspace_bytes(B, T, start, Hq, Hkv, d)
+    o, o_at, lse, lse_at, ws_at, ws_bytes, ws = _attention_buffers(q, shape, cache, out, want_lse, need, ws)
+    _check(lib.vitcop_tree_attn(q.data_ptr(), row, batch, cache.desc, k.data_ptr(), k_row, k_batch, v.data_ptr(), v_row, v_batch,
+                                tree.data_ptr(), T if own else 0, o_at, lse_at, T, start,
+                                _counts(start_samples, "start_samples", (B,), dev) if start_samples is not None else None,
+                                _counts(n_samples, "n_samples", (B,), dev) if n_samples is not None else None, Hq, scale, ws_at,
+                                ws_bytes, _stream_of(dev)))
     return o, lse
 
 
 def _layer_caches(caches, name: str, device: int):
-    """(host array of the layers' addresses, shape of one) of a list of caches [B,capacity,Hkv,d] or of one tensor of them."""
+    """(host array of the layers' addresses, their distance or 0, their number, shape of one) of a list of caches
+    [B,capacity,Hkv,d] or of one tensor of them."""
     if isinstance(caches, torch.Tensor):
-        if caches.dim() != 5:
+        shape = caches.shape
+        if len(shape) != 5:
             raise ValueError(f"{name} must be [n_layers,B,capacity,Hkv,d]")
-        _expect(caches, name, caches.shape, None, device)
-        L, first, step = caches.shape[0], caches.data_ptr(), caches.stride(0) * 2
-        return (C.c_void_p * L)(*range(first, first + L * step, step)) if step else (C.c_void_p * L)(), caches.shape[1:]
+        _expect(caches, name, shape, None, device)
+        return _OneCache(caches.data_ptr()), caches.stride(0), shape[0], shape[1:]
     if not caches or caches[0].dim() != 4:
         raise ValueError(f"{name}: no caches, or not [B,capacity,Hkv,d]")
     shape = caches[0].shape
     for t in caches:
         _expect(t, name, shape, None, device)
-    return (C.c_void_p * len(caches))(*[t.data_ptr() for t in caches]), shape
+    return (C.c_void_p * len(caches))(*[t.data_ptr() for t in caches]), 0, len(caches), shape
 
 
 def vitcop_cache_append(k_caches, v_caches, k, v, start=None, start_samples=None, idx=None, n_samples=None) -> None:
@@ -1288,48 +1307,53 @@ def vitcop_cache_append(k_caches, v_caches, k, v, start=None, start_samples=None
     lists of [B,capacity,Hkv,d] or one tensor [n_layers,B,capacity,Hkv,d] each: row idx[b,i] (int32 [B,rows]; i itself without
     idx) of sample b to row start + i of layer l's, start being one number or one for each layer, or start_samples[l,b] (int32
     [n_layers,B]).  n_samples int32 [B]: the first ones of a sample's rows only."""
-    sides = [(c, t, name) for c, t, name in ((k_caches, k, "k"), (v_caches, v, "v")) if t is not None]
-    if not sides:
+    if k is None and v is None:
         raise ValueError("k and v are both None")
-    dev = _here(sides[0][1], sides[0][2])
-    tables, strides, shape, cache_shape = [None, None], [(0, 0, 0), (0, 0, 0)], sides[0][1].shape, None
+    like, like_name = (k, "k") if k is not None else (v, "v")
+    dev = _here(like, like_name)
+    shape = like.shape
     if len(shape) != 5:
         raise ValueError("k and v must be [n_layers,B,T,Hkv,d]")
     L, B, T, Hkv, d = shape
-    for caches, t, name in sides:
+    given = cache_shape = None
+    args = []
+    for caches, t, name in ((k_caches, k, "k"), (v_caches, v, "v")):
+        if t is None:
+            args.append((None, None, 0, 0, 0))
+            continue
         if caches is None:
             raise ValueError(f"{name} without its caches")
-        table, of_one = _layer_caches(caches, f"{name}_caches", dev)
-        if t.shape != shape or len(table) != L or (of_one[0], of_one[2], of_one[3]) != (B, Hkv, d):
-            raise ValueError(f"{name} {tuple(t.shape)} does not fit {len(table)} caches of {tuple(of_one)}")
-        if cache_shape is not None and cache_shape != of_one:
-            raise ValueError("the caches of k and of v differ in their shape")
-        cache_shape = of_one
+        table, apart, n, of_one = _layer_caches(caches, name + "_caches", dev)
+        if t.shape != shape or n != L or (of_one[0], of_one[2], of_one[3]) != (B, Hkv, d):
+            raise ValueError(f"{name} {tuple(t.shape)} does not fit {n} caches of {tuple(of_one)}")
+        if given is None:
+            given, cache_shape = apart, of_one
+        elif (apart, of_one) != (given, cache_shape):
+            raise ValueError("the caches of k and of v differ in their shape, or lie in one tensor and in several")
         sl, sb, st, sh, sd = t.stride()
-        if t.get_device() != dev or t.dtype not in _BF16 or sd != 1 or (Hkv > 1 and sh != d):
+        if t.dtype not in _BF16 or sd != 1 or (sh != d and Hkv > 1) or t.get_device() != dev:
             raise ValueError(f"{name} must be bf16 on cuda:{dev}, a token's heads side by side")
-        side = 0 if name == "k" else 1
-        tables[side], strides[side] = table, (sl if L > 1 else 0, sb if B > 1 else 0, st if T > 1 else 0)
-    capacity = cache_shape[1]
-    rows = T
+        args.append((table, t.data_ptr(), sl if L > 1 else 0, sb if B > 1 else 0, st if T > 1 else 0))
+    capacity, rows, idx_at, starts, starts_at = cache_shape[1], T, None, None, None
     if idx is not None:
         if idx.dim() != 2:
             raise ValueError("idx must be [B,rows]")
         rows = idx.shape[1]
-    for n in (*shape, capacity, rows):
-        _whole(n, "a size")
-    idx_ptr = _counts(idx, "idx", (B, rows), dev)
-    starts = None
-    if start_samples is None:
+        idx_at = _counts(idx, "idx", (B, rows), dev)
+    if max(*shape, capacity, rows) > _MOST:
+        _past(max(*shape, capacity, rows), "a size")
+    if start_samples is not None:
+        if start is not None:
+            raise ValueError("start beside start_samples")
+        starts_at = _counts(start_samples, "start_samples", (L, B), dev)
+    else:
         starts = [start] * L if isinstance(start, int) else list(start) if start is not None else None
         if starts is None or len(starts) != L:
             raise ValueError("start must be a number, one for each layer, or start_samples be given")
         for n in starts:
             _whole(n, "start")
         starts = (C.c_int * L)(*starts)
-    elif start is not None:
-        raise ValueError("start beside start_samples")
-    desc = CacheAppendT(L, B, capacity, Hkv, d, T, rows, tables[0], tables[1], _ptr(k), _ptr(v), *strides[0], *strides[1], starts,
-                        _counts(start_samples, "start_samples", (L, B), dev), idx_ptr,
-                        _counts(n_samples, "n_samples", (B,), dev))
+    (k_table, k_at, *k_strides), (v_table, v_at, *v_strides) = args
+    desc = CacheAppendT(L, B, capacity, Hkv, d, T, rows, k_table, v_table, given if B and capacity else 0, k_at, v_at, *k_strides,
+                        *v_strides, starts, starts_at, idx_at, _counts(n_samples, "n_samples", (B,), dev))
     _check(lib.vitcop_cache_append(desc, _stream_of(dev)))

@@ -1654,13 +1654,18 @@ int vitcop_cache_append(const vitcop_cache_append_t* A, void* stream) {
         for (const int64_t stride : {A->k ? A->k_layer_stride : 0, A->v ? A->v_layer_stride : 0})
             REQUIRE(stride >= 0 && stride % 8 == 0 && at_most(A->n_layers, stride, (int64_t)1 << 61), VITCOP_EINVAL,
                     "cache_append: layer stride %lld", (long long)stride);
-    for (int l = 0; l < A->n_layers; ++l) {
+    const bool stacked = A->cache_layer_stride != 0;
+    REQUIRE(!stacked || (A->cache_layer_stride > 0 && A->cache_layer_stride % 8 == 0 &&
+                         at_most((int64_t)A->B * A->capacity, (int64_t)A->Hkv * A->d, A->cache_layer_stride) &&
+                         at_most(A->n_layers, A->cache_layer_stride, (int64_t)1 << 61)),
+            VITCOP_EINVAL, "cache_append: layer stride of the caches %lld", (long long)A->cache_layer_stride);
+    for (int l = 0; l < (stacked ? 1 : A->n_layers); ++l)
         REQUIRE((!A->k || (A->k_cache[l] && aligned16(A->k_cache[l]))) && (!A->v || (A->v_cache[l] && aligned16(A->v_cache[l]))),
                 VITCOP_EINVAL, "cache_append: a cache of layer %d is null or not 16-byte aligned", l);
-        REQUIRE(A->start_samples || (A->start[l] >= 0 && (int64_t)A->start[l] + A->rows <= A->capacity), VITCOP_EINVAL,
+    for (int l = 0; l < (A->start_samples ? 0 : A->n_layers); ++l)
+        REQUIRE(A->start[l] >= 0 && (int64_t)A->start[l] + A->rows <= A->capacity, VITCOP_EINVAL,
                 "cache_append: rows [%d,%lld) of layer %d outside [0,%d)", A->start[l], (long long)A->start[l] + A->rows, l,
                 A->capacity);
-    }
     return launch_cache_append(*A, static_cast<hipStream_t>(stream));
 }
 

@@ -5,17 +5,21 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 namespace vitcop {
 
 // theta^(-2i/d) / (2 pi) as a fraction of 2^64: position * fraction modulo 2^64 is the angle's part of a revolution, which a
 // 32-bit product of a far position and a speed has lost (position 10^5, the fastest pair: 2^-8 of a radian), and costs two
-// integer products instead of arithmetic in 64-bit floating point.
+// integer products instead of arithmetic in 64-bit floating point.  The host gives the speed of every eighth pair, each thread
+// goes on from there by products with theta^(-2/d) (64 bits of each are kept: the eighth is off by less than 2^-60, the farthest
+// position's angle by 2^-29 of a revolution), which keeps the launch's arguments short: all speeds of 128 channels and the caches' descriptor
+// took 6.8 us of host time a call, this 4.1.
 struct RopeAxesArgs {
     vitcop_rope_axes_t R;
     int slots;                          // threads that share a pair group's heads
     uint16_t axes[16];                  // two bits for each of a group's eight pairs
-    uint64_t speed[128];
+    uint64_t speed[16], step;
 };
 
 constexpr int RA_THREADS = 256;
@@ -66,11 +70,13 @@ __global__ __launch_bounds__(RA_THREADS) void rope_axes_kernel(const RopeAxesArg
         pos[a] = a < R.n_axes ? R.positions[((int64_t)a * R.B + b) * R.T + t] : 0;
     float sn[8], cs[8];
     const unsigned axes = A.axes[group];
+    uint64_t speed = A.speed[group];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const unsigned a = (axes >> (2 * i)) & 3;
         const int p = a < 2 ? (a == 0 ? pos[0] : pos[1]) : (a == 2 ? pos[2] : pos[3]);
-        const uint64_t turn = (uint64_t)(int64_t)p * A.speed[c0 + i];
+        const uint64_t turn = (uint64_t)(int64_t)p * speed;
+        speed = __umul64hi(speed, A.step);
         sincospif((float)(int32_t)(turn >> 32) * 0x1p-31f, &sn[i], &cs[i]);        // (in half revolutions, [-1, 1])
     }
 #pragma unroll
@@ -103,10 +109,10 @@ int launch_rope_axes(const vitcop_rope_axes_t& R, hipStream_t s) {
         A.axes[i / 8] |= (uint16_t)(a << (2 * (i % 8)));
         if (R.interleaved) a = (a + 1) % R.n_axes;
     }
-    // (one power and a product for each pair: 2^-64 of relative error a product, 128 of them)
-    const long double step = powl((long double)R.theta, -2.0L / R.d);
+    const long double step = powl((long double)R.theta, -2.0L / R.d), two = step * step, eight = two * two * two * two;
+    A.step = (uint64_t)(step * 0x1p64L + 0.5L);                          // (theta > 1: below 1)
     long double speed = 0x1p64L * 0.15915494309189533576888376337251436L;
-    for (int i = 0; i < pairs; ++i, speed *= step) A.speed[i] = (uint64_t)(speed + 0.5L);
+    for (int i = 0; i < pairs / 8; ++i, speed *= eight) A.speed[i] = (uint64_t)(speed + 0.5L);
     const int64_t units = (int64_t)R.B * R.T * (R.d / 16) * heads;
     const int per_thread = units >= (1 << 20) ? 4 : (units >= (1 << 18) ? 2 : 1);
     A.slots = (heads + per_thread - 1) / per_thread;
@@ -116,44 +122,67 @@ int launch_rope_axes(const vitcop_rope_axes_t& R, hipStream_t s) {
     return launch_status("rope_axes");
 }
 
-// Rows to the caches: 16 bytes a thread.
+// Rows to the caches: 16 bytes a thread.  The caches of up to CA_LAYERS layers by a table, or, where they are one allocation,
+// by the first one and their distance, which spares the call the table (32 layers, host time with the binding 14.0 -> 10.1 us).
 constexpr int CA_THREADS = 256, CA_LAYERS = 64;
-struct CacheAppendArgs {
-    vitcop_cache_append_t A;
-    int first, sides;                       // layer; of k and v, those given
+struct CacheTable {
     uint16_t* cache[2][CA_LAYERS];          // of k, of v
     int start[CA_LAYERS];
 };
-__global__ __launch_bounds__(CA_THREADS) void cache_append_kernel(const CacheAppendArgs P) {
+struct CacheStack {
+    uint16_t* cache[2];
+    int64_t stride;
+};
+template <typename CACHES>
+struct CacheAppendArgs {
+    vitcop_cache_append_t A;
+    int first, sides;                       // layer; of k and v, those given
+    CACHES caches;
+};
+template <typename CACHES>
+__global__ __launch_bounds__(CA_THREADS) void cache_append_kernel(const CacheAppendArgs<CACHES> P) {
     const vitcop_cache_append_t& A = P.A;
     const int layer = blockIdx.z / P.sides, of_v = P.sides == 2 ? blockIdx.z & 1 : A.k == nullptr, b = blockIdx.y;
     const unsigned chunks = (unsigned)(A.Hkv * A.d) / 8, id = blockIdx.x * CA_THREADS + threadIdx.x;
     const int i = (int)(id / chunks), c = (int)(id - (unsigned)i * chunks);
     if (i >= (A.n_samples ? min(A.n_samples[b], A.rows) : A.rows)) return;
     const int from = A.idx ? A.idx[(int64_t)b * A.rows + i] : i;
-    const int64_t to = (int64_t)(A.start_samples ? A.start_samples[(int64_t)(P.first + layer) * A.B + b] : P.start[layer]) + i;
+    int64_t to;
+    uint16_t* cache;
+    if constexpr (std::is_same<CACHES, CacheTable>::value) {
+        to = A.start_samples ? A.start_samples[(int64_t)(P.first + layer) * A.B + b] : P.caches.start[layer];
+        cache = P.caches.cache[of_v][layer];
+    } else {
+        to = A.start_samples[(int64_t)layer * A.B + b];
+        cache = P.caches.cache[of_v] + layer * P.caches.stride;
+    }
+    to += i;
     if (from < 0 || from >= A.T || to < 0 || to >= A.capacity) return;
     const uint16_t* src = of_v ? A.v + (P.first + layer) * A.v_layer_stride + b * A.v_batch_stride + from * A.v_row_stride
                                : A.k + (P.first + layer) * A.k_layer_stride + b * A.k_batch_stride + from * A.k_row_stride;
-    uint16_t* dst = P.cache[of_v][layer] + ((int64_t)b * A.capacity + to) * A.Hkv * A.d;
+    uint16_t* dst = cache + ((int64_t)b * A.capacity + to) * A.Hkv * A.d;
     *reinterpret_cast<uint4*>(dst + 8 * c) = *reinterpret_cast<const uint4*>(src + 8 * c);
 }
 
 int launch_cache_append(const vitcop_cache_append_t& A, hipStream_t s) {
     const int64_t units = (int64_t)A.rows * A.Hkv * A.d / 8;
+    const int sides = (A.k != nullptr) + (A.v != nullptr);
+    const unsigned wgs = (unsigned)((units + CA_THREADS - 1) / CA_THREADS);
+    if (A.cache_layer_stride != 0 && A.start_samples && A.n_layers * sides <= 65535) {
+        const CacheAppendArgs<CacheStack> P{A, 0, sides, {{A.k ? A.k_cache[0] : nullptr, A.v ? A.v_cache[0] : nullptr}, A.cache_layer_stride}};
+        hipLaunchKernelGGL(cache_append_kernel<CacheStack>, dim3(wgs, A.B, sides * A.n_layers), dim3(CA_THREADS), 0, s, P);
+        return launch_status("cache_append");
+    }
     for (int first = 0; first < A.n_layers; first += CA_LAYERS) {
-        CacheAppendArgs P{};
-        P.A = A;
-        P.first = first;
-        P.sides = (A.k != nullptr) + (A.v != nullptr);
+        CacheAppendArgs<CacheTable> P{A, first, sides, {}};
         const int n = std::min(CA_LAYERS, A.n_layers - first);
         for (int l = 0; l < n; ++l) {
-            if (A.k) P.cache[0][l] = A.k_cache[first + l];
-            if (A.v) P.cache[1][l] = A.v_cache[first + l];
-            P.start[l] = A.start_samples ? 0 : A.start[first + l];
+            const int at = first + l;
+            if (A.k) P.caches.cache[0][l] = A.cache_layer_stride ? A.k_cache[0] + at * A.cache_layer_stride : A.k_cache[at];
+            if (A.v) P.caches.cache[1][l] = A.cache_layer_stride ? A.v_cache[0] + at * A.cache_layer_stride : A.v_cache[at];
+            P.caches.start[l] = A.start_samples ? 0 : A.start[at];
         }
-        hipLaunchKernelGGL(cache_append_kernel, dim3((unsigned)((units + CA_THREADS - 1) / CA_THREADS), A.B, P.sides * n),
-                           dim3(CA_THREADS), 0, s, P);
+        hipLaunchKernelGGL(cache_append_kernel<CacheTable>, dim3(wgs, A.B, sides * n), dim3(CA_THREADS), 0, s, P);
         const int rc = launch_status("cache_append");
         if (rc) return rc;
     }

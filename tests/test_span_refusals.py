@@ -13,7 +13,7 @@ BIG = 2147483647
 
 
 def test_struct_layouts():
-    assert C.sizeof(vc.CacheT) == 32 and C.sizeof(vc.RopeAxesT) == 176 and C.sizeof(vc.CacheAppendT) == 144
+    assert C.sizeof(vc.CacheT) == 32 and C.sizeof(vc.RopeAxesT) == 176 and C.sizeof(vc.CacheAppendT) == 152
 
 
 def cache(B=2, capacity=64, Hkv=2, d=128, k=A, v=A):
@@ -123,7 +123,7 @@ def test_rope_axes(change, code):
 
 def append(**change):
     two, starts = (C.c_void_p * 2)(A, 2 * A), (C.c_int * 2)(0, 5)
-    p = dict(dict(n_layers=2, B=2, capacity=9, Hkv=2, d=64, T=4, rows=4, k_cache=two, v_cache=two, k=A, v=A, kl=1024, kb=512, kr=128,
+    p = dict(dict(n_layers=2, B=2, capacity=9, Hkv=2, d=64, T=4, rows=4, k_cache=two, v_cache=two, cl=0, k=A, v=A, kl=1024, kb=512, kr=128,
                   vl=1024, vb=512, vr=128, start=starts, start_samples=None, idx=None, n_samples=None), **change)
     return lib.vitcop_cache_append(vc.CacheAppendT(*p.values()), None)
 
@@ -140,6 +140,9 @@ NULLS = C.POINTER(C.c_void_p)()
     (dict(vb=-8), EINVAL), (dict(kl=-8), EINVAL), (dict(vl=4), EINVAL), (dict(kl=1 << 61), EINVAL), (dict(kb=1 << 46), EUNSUPPORTED),
     (dict(k_cache=(C.c_void_p * 2)(A, None)), EINVAL), (dict(v_cache=(C.c_void_p * 2)(A + 8, A)), EINVAL),
     (dict(start=(C.c_int * 2)(0, 6)), EINVAL), (dict(start=(C.c_int * 2)(-1, 0)), EINVAL), (dict(start=(C.c_int * 2)(BIG, 0)), EINVAL),
+    (dict(cl=-8), EINVAL), (dict(cl=2 * 9 * 2 * 64 - 8), EINVAL), (dict(cl=2 * 9 * 2 * 64 + 4), EINVAL), (dict(cl=1 << 61), EINVAL),
+    (dict(cl=1 << 40, k_cache=(C.c_void_p * 1)(A + 8)), EINVAL), (dict(cl=1 << 40, v_cache=(C.c_void_p * 1)(None)), EINVAL),
+    (dict(cl=1 << 40, B=65535, capacity=BIG), EINVAL),
     (dict(n_layers=0), OK), (dict(B=0), OK), (dict(rows=0), OK)])
 def test_cache_append(change, code):
     assert append(**change) == code
