@@ -21,6 +21,7 @@
 
 #include "vitcop_internal.h"
 #include "device_utils.h"
+#include "span_device.h"
 #include <algorithm>
 
 namespace vitcop {
@@ -404,8 +405,15 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
     // Consecutive workgroup ids go to different XCDs (each with its own L2): with a group size
     // that is a multiple of 8 a head keeps its XCD for all its query blocks, and the heads
     // of one XCD are consecutive, i.e. they share their K/V head under grouped-query attention.
-    int qb, hb;
-    {
+    int qb, hb, slice = 0;
+    if constexpr (SPANS) {
+        // sample after sample, the longest first; of a sample the last query block first, all heads and slices of each
+        const int id = blockIdx.x, units = Hkv * win.a.slices, row = id / units, unit = id - row * units, nth = row / n_qb;
+        const bool own = win.a.B > 1 && (win.a.starts || win.a.counts);
+        slice = unit / Hkv;
+        hb = (own ? span_sample(win.a, nth, 0) : nth) * Hkv + unit - slice * Hkv;
+        qb = n_qb - 1 - (row - nth * n_qb);
+    } else {
         const int id = blockIdx.x;
         const int grp = id / (n_qb * group);
         const int first = grp * group;
@@ -414,17 +422,9 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
         const int r = rem / gsz, j = rem - r * gsz;
         hb = first + ((gsz & 7) == 0 ? (j & 7) * (gsz >> 3) + (j >> 3) : j);
         qb = CAUSAL ? n_qb - 1 - r : r;
-        // samples of their own lengths: every 16 query blocks the heads move on by an XCD, or those of a long sample would keep
-        // theirs busy when the others have long been done
-        if (SPANS && (gsz & 7) == 0) hb = first + (hb - first + (r >> 4) * (gsz >> 3)) % gsz;
     }
     const int heads = SPANS ? Hkv : Hq;
-    const int h = __builtin_amdgcn_readfirstlane(hb % heads);
-    int b = __builtin_amdgcn_readfirstlane(hb / heads), slice = 0;
-    if constexpr (SPANS) {
-        slice = b % win.a.slices;
-        b /= win.a.slices;
-    }
+    const int h = __builtin_amdgcn_readfirstlane(hb % heads), b = __builtin_amdgcn_readfirstlane(hb / heads);
     const int hk = SPANS ? h : __builtin_amdgcn_readfirstlane(h / (Hq / Hkv));
     // Query blocks are aligned to the END of the sequence: a ragged block is then the first one,
     // which has the fewest keys to waste wavefronts on (query indices below 0 do not exist).
@@ -510,9 +510,11 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
             len_a = start;
             len_b = n_tok;
         } else {
+            const int end = start + (q0 + BM - 1) / G + 1;             // (sinks: 0 without a window)
             if (win.a.window) lo = max(0, start + max(q0, 0) / G - win.a.window + 1);
-            len_a = min(win.a.sinks, lo);
-            len_b = start + (q0 + BM - 1) / G + 1 - lo;
+            len_a = min(win.a.sinks, end);
+            lo = max(lo, len_a);
+            len_b = end - lo;
         }
         const int all_a = (len_a + AW_BN - 1) / AW_BN, all = all_a + (len_b + AW_BN - 1) / AW_BN;
         const int per = all / win.a.slices, more = all - per * win.a.slices;
@@ -688,7 +690,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
         // diagonal and ragged tiles: key key0 + 4g + 8(r/4) + r%4 of register r is visible to
         // the lane's query iff it is <= min(query, N-1), i.e. iff 8(r/4) + r%4 <= lim
         int lim[U] = {};
-        int far[U] = {}, sink = 0;       // of a window also iff it is > far, or < sink
+        int near[U] = {};                // SPANS: iff it is one of the lim + near from -near on
         uint32_t word[U] = {};           // TREE: a bit for each of the keys from key0 + 4 g on
         if constexpr (SPANS) key0 = t < a_tiles ? (t + skip) * AW_BN + 32 * par : lo + (t - a_tiles) * AW_BN + 32 * par;
         if constexpr (MASKED) {
@@ -696,12 +698,15 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
             for (int u = 0; u < U; ++u) {
                 const int query = max(wq0 + 32 * u + l32, 0);      // rows below 0 are never stored
                 lim[u] = (CAUSAL ? min(query, N - 1) : N - 1) - key0 - 4 * g;
-                if constexpr (SPANS) lim[u] = (t < a_tiles ? len_a - 1 : at[u]) - key0 - 4 * g;
+                if constexpr (SPANS) lim[u] = (t < a_tiles ? min(len_a - 1, at[u]) : at[u]) - key0 - 4 * g;
+                if constexpr (TREE) lim[u] = len_a - 1 - key0 - 4 * g;
                 if constexpr (TREE)
                     word[u] = t >= a_tiles ? bits[u][par] : (lim[u] < 0 ? 0u : (lim[u] >= 31 ? ~0u : (2u << lim[u]) - 1u));
-                if constexpr (SPANS && !TREE) far[u] = win.a.window == 0 ? -INT32_MAX : at[u] - win.a.window - key0 - 4 * g;
+                if constexpr (SPANS && !TREE) {
+                    near[u] = t < a_tiles || win.a.window == 0 ? key0 + 4 * g : win.a.window - 1 - at[u] + key0 + 4 * g;
+                    lim[u] = max(lim[u] + near[u] + 1, 0);
+                }
             }
-            if constexpr (SPANS && !TREE) sink = win.a.sinks - key0 - 4 * g;
         }
         // state of the vector work (see SmKind)
         float m5[U][5], m3[U][3], alpha[U];
@@ -718,7 +723,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
                 if constexpr (TREE) {
                     if (!(word[u] >> n & 1)) s[par][u][i] = -INFINITY;
                 } else {
-                    if (n > lim[u] || (SPANS && n <= far[u] && n >= sink)) s[par][u][i] = -INFINITY;
+                    if (SPANS ? (unsigned)(n + near[u]) >= (unsigned)lim[u] : n > lim[u]) s[par][u][i] = -INFINITY;
                 }
             } else if constexpr (kind == SM_MAX5) {
                 // (the empty asm pins the instruction to its run: nothing else needs the maxima before
@@ -919,34 +924,35 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
     int t = 1;
     if constexpr (SPANS) {
         if (my_tiles > 0) {
-            // (the first block's product with V, of a stage that there is not, adds zeros: no branch in any block)
             scores_only(0, 0, 0);
             load_k_frags(0, 0, 1);
+            // tiles [whole, edge): all queries of this wavefront see all their keys.  (The first tile and those of a window's
+            // sinks are masked in any case.)
+            int whole = 1, edge = len_a / AW_BN - skip;
+            if constexpr (!TREE) {
+                whole = a_tiles;
+                if (win.a.window) whole += (max(0, row_last + 1 - win.a.window - lo) + AW_BN - 1) / AW_BN;
+                edge = a_tiles + (row_first + 1 - lo) / AW_BN;
+            }
+            whole = min(max(whole, 1), my_tiles);
+            edge = min(edge, my_tiles);
+            // (the first block's product with V, of a stage that there is not, adds zeros: no branch in any block)
 #pragma unroll
             for (int i = 0; i < 2 * DB; ++i) vlo[0][i] = vhi[0][i] = s16x4{0, 0, 0, 0};
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int tt = 0; tt < 2; ++tt) pf[1][u][tt] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
-            // tiles [whole, edge): all queries of this wavefront see all their keys.  (Those of a window's sinks are masked.)
-            int whole = 0, edge = len_a / AW_BN - skip;
-            if constexpr (!TREE) {
-                whole = a_tiles;
-                if (win.a.window) whole += (max(0, row_last + 1 - win.a.window - lo) + AW_BN - 1) / AW_BN;
-                edge = a_tiles + (row_first + 1 - lo) / AW_BN;
-            }
-            whole = min(max(whole, 0), my_tiles);
-            edge = min(edge, my_tiles);
             for (t = 0; t < whole; ++t) {
                 if (t > 0) tile_sync(t);
                 tile_body(t, std::true_type{}, false);
             }
             for (; t < edge; ++t) {
-                if (t > 0) tile_sync(t);
+                tile_sync(t);
                 tile_body(t, std::false_type{}, false);
             }
             for (; t < my_tiles; ++t) {
-                if (t > 0) tile_sync(t);
+                tile_sync(t);
                 tile_body(t, std::true_type{}, false);
             }
             values_only(1, 0);

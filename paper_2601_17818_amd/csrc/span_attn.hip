@@ -16,6 +16,7 @@
 // span_merge_kernel combines the slices; a single slice is finished on the spot.
 #include "vitcop_internal.h"
 #include "device_utils.h"
+#include "span_device.h"
 #include "span_plan.h"
 
 #include <algorithm>
@@ -39,7 +40,9 @@ __global__ __launch_bounds__(64 * SP_WAVES, NB == 2 ? 2 : 3) void span_attn_kern
     __shared__ __attribute__((aligned(16))) char vt[SP_WAVES][SP_KEYS * VROW];
     __shared__ float sm[SP_WAVES][ROWS][2];
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, g4 = lane >> 4;
-    const int hk = blockIdx.x, b = blockIdx.z, rb = blockIdx.y / (unsigned)A.slices, slice = blockIdx.y - rb * A.slices;
+    const int hk = blockIdx.x, rb = blockIdx.y / (unsigned)A.slices, slice = blockIdx.y - rb * A.slices;
+    int b = blockIdx.z;
+    if (A.B > 1 && (A.starts || A.counts)) b = span_sample(A, b, 256 / (A.Hkv * A.slices * A.row_blocks));
     const int G = A.G, Hq = A.Hkv * G;
     const int n_tok = A.counts ? min(max(A.counts[b], 0), A.T) : A.T;
     const int start = A.starts ? min(max(A.starts[b], 0), A.start) : A.start;
