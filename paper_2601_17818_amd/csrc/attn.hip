@@ -409,9 +409,8 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
     if constexpr (SPANS) {
         // sample after sample, the longest first; of a sample the last query block first, all heads and slices of each
         const int id = blockIdx.x, units = Hkv * win.a.slices, row = id / units, unit = id - row * units, nth = row / n_qb;
-        const bool own = win.a.B > 1 && (win.a.starts || win.a.counts);
         slice = unit / Hkv;
-        hb = (own ? span_sample(win.a, nth, 0) : nth) * Hkv + unit - slice * Hkv;
+        hb = (win.a.ragged ? span_sample(win.a, nth, 0) : nth) * Hkv + unit - slice * Hkv;
         qb = n_qb - 1 - (row - nth * n_qb);
     } else {
         const int id = blockIdx.x;
@@ -553,7 +552,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
     const u32x4 k_desc = make_desc(kbase), v_desc = make_desc(vbase);
     const unsigned lane_off = (unsigned)(GPW * wv + GROUPS * (lane / LPR)) * row_bytes + ((unsigned)(lane % LPR) << 4);
     u32x4 k_desc_b = k_desc, v_desc_b = v_desc;                        // SPANS: of span b
-    unsigned k_row_b = row_bytes, v_row_b = row_bytes, k_off_b = lane_off, v_off_b = lane_off;
+    unsigned k_row_b = row_bytes, v_row_b = row_bytes;
     uint64_t seen = 0;                                                 // TREE: the drafts that a token of the sample sees
     if constexpr (TREE) {
         const uint64_t w = lane < n_tok ? win.a.tree[b * win.a.tree_batch + lane] : 0;
@@ -568,8 +567,6 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
         v_row_b = (unsigned)win.a.v2_row * 2;
         k_desc_b = make_desc(reinterpret_cast<const char*>(win.a.k2 + b * win.a.k2_batch + hk * D));
         v_desc_b = make_desc(reinterpret_cast<const char*>(win.a.v2 + b * win.a.v2_batch + hk * D));
-        k_off_b = (unsigned)(GPW * wv + GROUPS * (lane / LPR)) * k_row_b + ((unsigned)(lane % LPR) << 4);
-        v_off_b = (unsigned)(GPW * wv + GROUPS * (lane / LPR)) * v_row_b + ((unsigned)(lane % LPR) << 4);
     } else if constexpr (SPANS) {
         k_desc_b = make_desc(kbase + lo * kv_rs * 2);
         v_desc_b = make_desc(vbase + lo * kv_rs * 2);
@@ -591,7 +588,8 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
             if constexpr (TREE) {
                 if (in_b) {                          // (there is one such tile; drafts that no token sees: past the range)
                     const int r = GPW * wv + GROUPS * (lane / LPR) + i;
-                    lane_at = !(seen >> r & 1) ? 0xFFFFF000u : ((j & 1) ? v_off_b : k_off_b);
+                    const unsigned off_b = (unsigned)(GPW * wv + GROUPS * (lane / LPR)) * of_b + ((unsigned)(lane % LPR) << 4);
+                    lane_at = !(seen >> r & 1) ? 0xFFFFF000u : off_b;
                 }
             }
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"

@@ -25,7 +25,10 @@ struct RopeAxesArgs {
 constexpr int RA_THREADS = 256;
 
 // A thread turns eight pairs (16 bytes of a head's lower half and 16 of its upper one) of up to HEADS heads of a token: its
-// sines and cosines serve them all, and their loads go out together.  The heads of v pass through.
+// sines and cosines serve them all, and their loads go out together.  The heads of v pass through.  Stores are non-temporal: us
+// with ordinary and with these, inputs from memory, 2 x 6400 tokens of 28 + 2 x 4 heads 49.5, 45.5 (5.2 TB/s), 8 x 1500 of
+// 3 x 32 110, 103.5, 4 x up to 640 of them 13.8, 13.1, 64 x up to 700 of 16 + 2 x 4 of 64 38.2, 32.7; non-temporal loads as well
+// 43.4, 99.8, 13.5, 38.1 (what has just been projected is better left where it is).
 template <int HEADS>
 __global__ __launch_bounds__(RA_THREADS) void rope_axes_kernel(const RopeAxesArgs A) {
     const vitcop_rope_axes_t& R = A.R;
@@ -92,8 +95,8 @@ __global__ __launch_bounds__(RA_THREADS) void rope_axes_kernel(const RopeAxesArg
                 h[j] = pack_bf16(y0 * cs[2 * j] + x0 * sn[2 * j], y1 * cs[2 * j + 1] + x1 * sn[2 * j + 1]);
             }
         }
-        *reinterpret_cast<uint4*>(dst[i] + c0) = lo[i];
-        *reinterpret_cast<uint4*>(dst[i] + half + c0) = hi[i];
+        st_nt16(dst[i] + c0, lo[i]);
+        st_nt16(dst[i] + half + c0, hi[i]);
     }
 }
 
@@ -122,7 +125,8 @@ int launch_rope_axes(const vitcop_rope_axes_t& R, hipStream_t s) {
     return launch_status("rope_axes");
 }
 
-// Rows to the caches: 16 bytes a thread.  The caches of up to CA_LAYERS layers by a table, or, where they are one allocation,
+// Rows to the caches: 16 bytes a thread, with non-temporal stores (us with ordinary and with these, of 8 KB a row: 32 layers x 16
+// samples x up to 8 of 16 rows 26.3, 19.3, 4 x 16 x 64 19.5, 14.4).  The caches of up to CA_LAYERS layers by a table, or, where they are one allocation,
 // by the first one and their distance, which spares the call the table (32 layers, host time with the binding 14.0 -> 10.1 us).
 constexpr int CA_THREADS = 256, CA_LAYERS = 64;
 struct CacheTable {
@@ -161,7 +165,7 @@ __global__ __launch_bounds__(CA_THREADS) void cache_append_kernel(const CacheApp
     const uint16_t* src = of_v ? A.v + (P.first + layer) * A.v_layer_stride + b * A.v_batch_stride + from * A.v_row_stride
                                : A.k + (P.first + layer) * A.k_layer_stride + b * A.k_batch_stride + from * A.k_row_stride;
     uint16_t* dst = cache + ((int64_t)b * A.capacity + to) * A.Hkv * A.d;
-    *reinterpret_cast<uint4*>(dst + 8 * c) = *reinterpret_cast<const uint4*>(src + 8 * c);
+    st_nt16(dst + 8 * c, *reinterpret_cast<const uint4*>(src + 8 * c));
 }
 
 int launch_cache_append(const vitcop_cache_append_t& A, hipStream_t s) {

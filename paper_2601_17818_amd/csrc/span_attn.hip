@@ -42,7 +42,7 @@ __global__ __launch_bounds__(64 * SP_WAVES, NB == 2 ? 2 : 3) void span_attn_kern
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, g4 = lane >> 4;
     const int hk = blockIdx.x, rb = blockIdx.y / (unsigned)A.slices, slice = blockIdx.y - rb * A.slices;
     int b = blockIdx.z;
-    if (A.B > 1 && (A.starts || A.counts)) b = span_sample(A, b, 256 / (A.Hkv * A.slices * A.row_blocks));
+    if (A.ragged) b = span_sample(A, b, 256 / (A.Hkv * A.slices * A.row_blocks));
     const int G = A.G, Hq = A.Hkv * G;
     const int n_tok = A.counts ? min(max(A.counts[b], 0), A.T) : A.T;
     const int start = A.starts ? min(max(A.starts[b], 0), A.start) : A.start;
@@ -358,21 +358,26 @@ static int launch_span_merge(const SpanArgs& A, hipStream_t s) {
     return launch_status("span_merge");
 }
 
-static SpanPlan plan_of(int B, int T, int start, int Hq, int Hkv, int d, int window, int sinks, bool tree) {
+static SpanPlan plan_of(int B, int T, int start, int Hq, int Hkv, int d, int window, int sinks, bool tree, bool own,
+                        bool* ragged = nullptr) {
     // the wide kernel addresses a span with 32 bits of bytes
     const int64_t all = (int64_t)start + T, keys = window == 0 ? all : std::min<int64_t>(all, (int64_t)window + T);
-    return span_plan(SpanSizes{B, Hkv, T, Hq / Hkv, start, window, sinks, d, tree},
-                     (std::max<int64_t>(keys, sinks) + 256) * Hkv * d * 2 < ((int64_t)1 << 32));
+    const SpanSizes z{B, Hkv, T, Hq / Hkv, start, window, sinks, d, tree, own};
+    if (ragged) *ragged = z.ragged();
+    return span_plan(z, (std::max<int64_t>(keys, sinks) + 256) * Hkv * d * 2 < ((int64_t)1 << 32));
 }
 
 size_t span_workspace_bytes(int B, int T, int start, int Hq, int Hkv, int d, int window, int sinks, bool tree) {
-    const size_t s = plan_of(B, T, start, Hq, Hkv, d, window, sinks, tree).slices;
+    size_t s = 1;                                            // (a call may have samples of their own lengths or not)
+    for (const bool own : {false, true})
+        s = std::max<size_t>(s, plan_of(B, T, start, Hq, Hkv, d, window, sinks, tree, own).slices);
     return s == 1 ? 0 : up256((size_t)B * T * Hq * s * d * 4) + up256((size_t)B * T * Hq * s * 2 * 4);
 }
 
 template <int D>
 static int launch_span_d(SpanArgs A, int Hq, void* ws, hipStream_t s) {
-    const SpanPlan p = plan_of(A.B, A.T, A.start, Hq, A.Hkv, D, A.window, A.sinks, A.tree != nullptr);
+    const SpanPlan p = plan_of(A.B, A.T, A.start, Hq, A.Hkv, D, A.window, A.sinks, A.tree != nullptr, A.starts || A.counts,
+                               &A.ragged);
     A.row_blocks = p.row_blocks;
     A.slices = p.slices;
     A.part_o = static_cast<float*>(ws);

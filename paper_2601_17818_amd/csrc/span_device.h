@@ -8,7 +8,7 @@ namespace vitcop {
 // The sample that a workgroup takes as the `nth`, where samples have lengths of their own: the longest first, so that no long
 // one is left over at the end, and every other `layer` of samples (what one workgroup on each CU takes; 0: no layers) backwards,
 // so that a CU that starts with a long one goes on with a short one.  Sorted in groups of 64, by every wavefront for itself.
-// (16 conversations of up to 2000 rows x 32 heads, 25 drafts: 79 us in the order given, PLACEHOLDER so.)
+// (16 conversations of up to 2000 rows x 32 heads, 25 drafts: 79 us in the order given, 65 so.)
 __device__ __forceinline__ int span_sample(const SpanArgs& A, int nth, int layer) {
     const int lane = threadIdx.x & 63, first = nth & ~63, n = min(64, A.B - first);
     int at = nth - first;

@@ -21,7 +21,9 @@ struct SpanPlan {
 struct SpanSizes {
     int64_t B, Hkv, T, G, start, window, sinks;
     int d;
-    bool tree;
+    bool tree, own;                                  // own: samples have lengths of their own
+    // Their order and their slices go by those lengths, unless a window makes most of them alike.
+    bool ragged() const { return own && B > 1 && (window == 0 || start < 2 * window); }
 };
 
 // The kernels are priced in us and the cheapest kind, number of blocks and of slices is taken.  What a launch streams costs its
@@ -36,12 +38,15 @@ struct SpanSizes {
 // of 64: 4 x 600 1: 7.4, 4: 7.8; x 4000 1: 22.2, 32: 9.0; 64 x 300 1: 7.0, 2: 9.3; x 3000 1: 27.0, 4: 17.4.
 //
 // Many rows, in tiles of 64 keys: one block of 128 rows takes 0.88 us a tile where CUs are left over and 1.0 where not, and 7 to
-// begin and end; two blocks 1.9 and 8.5, so that one is better where a workgroup has few tiles or all fit at once, two where there
-// are rounds of workgroups.  (Drafts take one: with two the registers do not hold the masks, 2.0 us a tile even on an idle chip.)  Measured,
-// us: 317 tokens of 7 query heads x 4 KV heads behind 16384 rows one block 3: 97.3, 7: 97.9, two 3: 140, 5: 99.1, 7: 87.5, 14: 104;
-// 100 behind 8000 one 4: 38.4, 10: 29.0, two 7: 42.3, 21: 33.2; 2 x 8192 with a window of 2048 one 530, two 465; 2 x 2000 with one
-// of 500 65.8, 70.6; 640 tokens of 32 heads 17.5, 31.5; 8 x 64 drafts x 28 / 4 heads behind 4096 1: 63.4, 2: 49.6, 3: 65.4; of 64:
-// 4 x 64 x 16 / 4 behind 3000 1: 37.4, 4: 19.1, 8: 17.9, 16: 24.7.
+// begin and end; two blocks 1.6 to 1.8 and 8, so that one is better where a workgroup has few tiles or all fit at once, two where
+// there are rounds of workgroups.  (Drafts take one: with two the registers do not hold the masks, 2.0 us a tile even on an idle
+// chip.)  Measured, us: 317 tokens of 7 query heads x 4 KV heads behind 16384 rows one block 3: 91.0, 7: 93.5, two 3: 132, 5: 89.6,
+// 7: 81.9, 14: 98.4; 100 behind 8000 one 4: 38.8, 8: 29.0, 10: 30.4, two 7: 40.2, 21: 31.9; 2 x 8192 with a window of 2048 one 487,
+// two 421; 2 x 2000 with one of 500 54.6, 53.3; 640 tokens of 32 heads 15.9, 24.8; 8 x 64 drafts x 28 / 4 heads behind 4096
+// 1: 63.1, 2: 47.9, 3: 62.1; of 64: 4 x 64 x 16 / 4 behind 3000 1: 38.8, 4: 19.7, 8: 18.3, 16: 25.4.
+// Samples of their own lengths: 64 x up to 16000 keys x 28 / 4 1: 263, 2: 211, 8: 224; 12 x 8000 x 16 1: 127, 2: 98.6, 4: 86.7;
+// 40 x 8000 x 28 / 4 1: 116, 3: 75.9, 8: 80.4; 20 x 3000 x 32 1: 104, 2: 112; 8 x 700 tokens behind 3000 x 28 / 4 two blocks 1: 103,
+// 2: 135.
 inline SpanPlan span_plan(const SpanSizes& z, bool fits) {
     const int64_t rows = z.T * z.G, pairs = z.B * z.Hkv, all = z.start + z.T;
     SpanPlan best{};
@@ -59,14 +64,18 @@ inline SpanPlan span_plan(const SpanSizes& z, bool fits) {
         const int tile = p.wide ? 64 : SP_KEYS * SP_WAVES;
         const float steps = (float)(((mean + tile - 1) / tile + slices - 1) / slices);
         const bool d64 = z.d == 64;
+        // samples of their own lengths: some 0.6 of the longest one's keys in the mean, and a CU that begins with a long one goes
+        // on with a short one
+        const float share = z.ragged() ? 0.6f : 1.f, load = z.ragged() && on_cu > 1 ? 0.62f : 1.f;
         float us;
         if (!p.wide) {
             const float step = wgs <= 128 ? (d64 ? 0.85f : 1.55f) : (wgs <= 256 ? (d64 ? 1.1f : 2.1f) : (d64 ? 1.25f : 2.5f));
-            us = std::max(bytes / 5.8e6f, (float)on_cu * steps * step);
+            us = std::max(share * bytes / 5.8e6f, load * (float)on_cu * steps * step);
         } else {
-            const float step = d64 ? 0.65f : (blocks == 2 ? 1.9f : (wgs <= 128 ? 0.88f : 1.0f)), ends = blocks == 2 ? 8.5f : 7.f;
-            const float rounds = wgs > 1024 ? (float)wgs / 256.f : (float)on_cu;
-            us = std::max(bytes / 5.2e6f, rounds * steps * step) + (d64 ? (float)((wgs + 767) / 768) : rounds) * ends;
+            const float step = d64 ? 0.65f : (blocks == 2 ? (wgs <= 128 ? 1.6f : 1.8f) : (wgs <= 128 ? 0.88f : 1.0f));
+            const float ends = blocks == 2 ? 8.f : 7.f, rounds = wgs > 512 ? (float)wgs / 256.f + 0.3f : (float)on_cu;
+            us = std::max(share * bytes / 5.2e6f, std::max(1.f, load * rounds) * steps * step) +
+                 (d64 ? (float)((wgs + 767) / 768) : rounds) * ends;
         }
         if (slices > 1) us += 5.f + (float)(pairs * rows * slices) * (float)(8 * z.d) / 6e6f;
         if (first || us < least) {

@@ -63,6 +63,7 @@ struct SpanArgs {
     const int32_t *starts, *counts;
     int B, T, G, Hkv, start, window, sinks;  // (window and sinks: below start + T, so that sums with them fit 32 bits)
     float scale_log2e;
+    bool ragged;                             // samples in the order of their lengths
     int row_blocks, slices;                  // part_o, part_ml: [B,Hkv,T*G,slices] rows of d outputs, of (reference, sum)
     float *part_o, *part_ml;
     uint16_t* out;

@@ -161,6 +161,9 @@ WINDOWS = [
     (1, 16, 0, 2, 2, 128, 0, 0), (1, 17, 250, 14, 2, 128, 100, 300), (1, 33, 1, 4, 1, 64, 33, 32), (2, 63, 65, 3, 3, 128, 0, 7),
     (1, 64, 64, 4, 4, 128, 64, 64), (1, 65, 1200, 4, 1, 128, 500, 3), (1, 127, 0, 2, 1, 128, 0, 0), (2, 128, 0, 2, 2, 64, 32, 0),
     (1, 129, 33, 4, 2, 128, 65, 1), (1, 200, 0, 3, 1, 128, 1, 0), (1, 257, 100, 2, 2, 128, 64, 16), (1, 300, 700, 2, 1, 64, 0, 0),
+    # (two blocks of 128 query rows a workgroup)
+    (2, 700, 0, 28, 4, 128, 100, 5), (3, 700, 130, 16, 8, 128, 0, 0), (2, 600, 0, 32, 16, 128, 64, 16), (5, 500, 60, 16, 8, 128, 90, 3),
+    (2, 700, 33, 28, 4, 128, 60, 200), (2, 650, 0, 28, 4, 128, 1, 0),
     (1, 513, 0, 2, 1, 128, 130, 65), (1, 600, 50, 1, 1, 64, 200, 40), (1, 640, 0, 2, 2, 128, 0, 0), (2, 384, 0, 7, 1, 128, 100, 129),
 ]
 
@@ -172,7 +175,8 @@ def test_window(vc, B, T, start, Hq, Hkv, d, window, sinks):
 
 @pytest.mark.parametrize("B,T,start,Hq,Hkv,d,window,sinks", [
     (5, 1, 300, 8, 2, 128, 64, 4), (5, 1, 300, 2, 2, 64, 0, 0), (6, 9, 130, 28, 4, 128, 33, 2), (4, 70, 50, 4, 1, 64, 0, 0),
-    (4, 150, 0, 4, 2, 128, 40, 3), (4, 300, 20, 2, 2, 128, 0, 0), (4, 300, 20, 2, 1, 64, 100, 70), (3, 530, 0, 2, 1, 128, 70, 1)])
+    (4, 150, 0, 4, 2, 128, 40, 3), (4, 300, 20, 2, 2, 128, 0, 0), (4, 300, 20, 2, 1, 64, 100, 70), (3, 530, 0, 2, 1, 128, 70, 1), (5, 500, 60, 16, 8, 128, 90, 3), (4, 900, 100, 28, 4, 128, 0, 0),
+    (70, 1, 40, 2, 2, 64, 0, 0), (130, 3, 20, 4, 2, 128, 7, 1), (67, 20, 9, 4, 2, 64, 0, 0)])
 def test_samples_of_their_own_lengths(vc, B, T, start, Hq, Hkv, d, window, sinks):
     rng = np.random.default_rng(5)
     starts = rng.integers(0, start + 1, B).tolist()
@@ -204,7 +208,7 @@ def test_windows_and_sinks_past_the_cache(vc):
 
 
 TREES = [                                                # (of more than 64 query rows, too)
-    (1, 9, 200, 8, 1, 128), (2, 20, 63, 14, 2, 64), (1, 64, 1000, 4, 2, 128), (2, 33, 0, 4, 1, 128), (1, 40, 2100, 28, 4, 64),
+    (1, 9, 200, 8, 1, 128), (2, 20, 63, 14, 2, 64), (2, 20, 63, 2, 2, 64), (2, 5, 300, 16, 4, 64), (1, 64, 1000, 4, 2, 128), (2, 33, 0, 4, 1, 128), (1, 40, 2100, 28, 4, 64),
     # B, T, start, Hq, Hkv, d
     (1, 1, 0, 1, 1, 128), (1, 1, 33, 4, 4, 64), (2, 8, 384, 4, 4, 128), (1, 16, 31, 28, 4, 128), (1, 17, 32, 16, 4, 64),
     (2, 25, 500, 3, 3, 128), (1, 31, 2000, 2, 2, 128), (1, 32, 64, 4, 1, 128), (1, 33, 1000, 8, 1, 64), (1, 63, 5, 2, 1, 128),
