@@ -10,7 +10,7 @@
  *    aligned unless stated otherwise, rows contiguous, token-major.
  *  - The library allocates no device memory and carries no data from one call to
  *    the next (the only thing it remembers is that a kernel's shared-memory limit
- *    has been raised, a once-per-process flag that any thread may set again).
+ *    has been raised, flags that any thread may set again).
  *    Scratch memory comes from the caller through `ws` / `ws_bytes`; the size
  *    needed is returned by the matching *_workspace_bytes query.  The contents
  *    of `ws` need not be initialised and are undefined afterwards.
@@ -629,8 +629,10 @@ int vitcop_rope_axes(const vitcop_rope_axes_t* R, void* stream);
  * window 0: all of j <= p.  A token's step (T = 1), a further question (T tokens behind a long conversation) and a
  * right-padded prompt (start 0, n_samples) are the same call.  Rows of the cache that no token of the call sees may
  * hold anything.
- *   q [B,T,Hq,d] bf16;  out [B,T,Hq,d] bf16 dense;  lse_out [B,Hq,T] fp32 natural-log-sum-exp, may be NULL
- *   scale 0 selects 1/sqrt(d);  query head h reads KV head h / (Hq/Hkv)
+ *   q [B,T,Hq,d] bf16;  out [B,T,Hq,d] bf16 dense, no part of an input;  lse_out [B,Hq,T] fp32 natural-log-sum-exp, may be NULL
+ *   scale 0 selects 1/sqrt(d);  query head h reads KV head h / (Hq/Hkv).  Probabilities go into the sums over V with 24 bits
+ *   of up to 16 query rows T*Hq/Hkv of a KV head (as in vitcop_decode_attn), 16 of up to 32, and 8 of more (as in
+ *   vitcop_prefill_attn); all sums are fp32
  *   ws: device scratch of ws_bytes >= vitcop_window_attn_workspace_bytes, NULL where that is 0 (it is 0 too where the
  *   sizes are refused)
  * d in {64,128}; Hq % Hkv == 0; 0 <= start, start + T <= capacity; window, sinks >= 0; B, Hkv <= 65535;
@@ -649,7 +651,7 @@ int vitcop_window_attn(const uint16_t* q, int64_t q_row_stride, int64_t q_batch_
  *   q [B,T,Hq,d], k, v [B,T,Hkv,d] bf16;  tree [B,T] uint64, or one [T] for all samples (tree_batch_stride 0)
  *   C: k and v may be NULL where start is 0
  *   out, lse_out, scale, ws and limits as vitcop_window_attn's; 0 <= start <= capacity; row strides of k and v at least
- *   Hkv*d and below 2^25 (T > 1). */
+ *   Hkv*d and below 2^24 (T > 1). */
 #define VITCOP_MAX_DRAFTS 64
 size_t vitcop_tree_attn_workspace_bytes(int B, int T, int start, int Hq, int Hkv, int d);
 int vitcop_tree_attn(const uint16_t* q, int64_t q_row_stride, int64_t q_batch_stride, const vitcop_cache_t* C,

@@ -1147,13 +1147,16 @@ def vitcop_rope_axes(q, k, positions, sections, theta: float = 10000.0, v=None, 
     n_axes = len(sections)
     if not 1 <= n_axes <= VITCOP_MAX_AXES:
         raise ValueError(f"{n_axes} sections (1 to {VITCOP_MAX_AXES})")
-    if max(*sections, *shape, start) > _MOST or min(*sections, start) < _LEAST:
-        _past(max(*sections, *shape, start, key=abs), "a size, section or start")
+    if B > _MOST or T > _MOST or d > _MOST or not _LEAST <= start <= _MOST:
+        _past(max(B, T, d, start, key=abs), "a size or start")
+    if min(sections) < 0 or 2 * sum(sections) != d:
+        raise ValueError(f"sections {tuple(sections)} are not the {d // 2} pairs of {d} channels")
     _expect(positions, "positions", (n_axes, B, T), torch.int32, dev)
     Hq = Hkv = capacity = q_row = q_batch = k_row = k_batch = v_row = v_batch = 0
     q_at = q_to = k_at = k_to = v_at = v_to = None
     if q is not None:
-        Hq, q_at = q.shape[2], q.data_ptr()
+        q_shape = q.shape
+        Hq, q_at = q_shape[2] if len(q_shape) == 4 else 0, q.data_ptr()
         q_row, q_batch = _token_rows(q, "q", dev, (B, T, Hq, d))
         if out is None:
             out = torch.empty((B, T, Hq, d), dtype=q.dtype, device=q.device)
@@ -1172,8 +1175,8 @@ def vitcop_rope_axes(q, k, positions, sections, theta: float = 10000.0, v=None, 
         v_shape = v.shape
         Hkv, v_at = Hkv if k is not None else (v_shape[2] if len(v_shape) == 4 else 0), v.data_ptr()
         v_row, v_batch = _token_rows(v, "v", dev, (B, T, Hkv, d))
-    if Hkv > _MOST:
-        _past(Hkv, "k and v")
+    if Hq > _MOST or Hkv > _MOST:
+        _past(max(Hq, Hkv), "heads")
     if cache is not None:
         if k is None and v is None:
             raise ValueError("a cache without k and v")
@@ -1247,7 +1250,7 @@ def vitcop_window_attn(q, cache: Cache, start: int, window: int = 0, sinks: int 
     ``out`` = (out, lse) reuses buffers, ``ws`` a uint8 workspace."""
     shape, row, batch = _query_rows(q, cache)
     B, T, Hq, d = shape
-    if max(start, window, sinks) > _MOST or min(start, window, sinks) < _LEAST:
+    if not (_LEAST <= start <= _MOST and _LEAST <= window <= _MOST and _LEAST <= sinks <= _MOST):
         _past(max(start, window, sinks, key=abs), "start, window or sinks")
     dev = cache.device
     need = 0 if ws is not None else lib.vitcop_window_attn_workspace_bytes(B, T, start, Hq, cache.Hkv, d, window, sinks)
@@ -1340,7 +1343,7 @@ def vitcop_cache_append(k_caches, v_caches, k, v, start=None, start_samples=None
             raise ValueError("idx must be [B,rows]")
         rows = idx.shape[1]
         idx_at = _counts(idx, "idx", (B, rows), dev)
-    if max(*shape, capacity, rows) > _MOST:
+    if L > _MOST or B > _MOST or T > _MOST or Hkv > _MOST or d > _MOST or capacity > _MOST or rows > _MOST:
         _past(max(*shape, capacity, rows), "a size")
     if start_samples is not None:
         if start is not None:
@@ -1355,5 +1358,6 @@ def vitcop_cache_append(k_caches, v_caches, k, v, start=None, start_samples=None
         starts = (C.c_int * L)(*starts)
     (k_table, k_at, *k_strides), (v_table, v_at, *v_strides) = args
     desc = CacheAppendT(L, B, capacity, Hkv, d, T, rows, k_table, v_table, given if B and capacity else 0, k_at, v_at, *k_strides,
-                        *v_strides, starts, starts_at, idx_at, _counts(n_samples, "n_samples", (B,), dev))
+                        *v_strides, starts, starts_at, idx_at,
+                        _counts(n_samples, "n_samples", (B,), dev) if n_samples is not None else None)
     _check(lib.vitcop_cache_append(desc, _stream_of(dev)))

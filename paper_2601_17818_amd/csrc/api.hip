@@ -1572,7 +1572,7 @@ static void clamp_window(int rows, int& window, int& sinks) {
 size_t vitcop_window_attn_workspace_bytes(int B, int T, int start, int Hq, int Hkv, int d, int window, int sinks) {
     if (check_span("window_attn", B, T, start, Hq, Hkv, d) != VITCOP_OK || window < 0 || sinks < 0 || B == 0 || T == 0) return 0;
     clamp_window(start + T, window, sinks);
-    return span_workspace_bytes(B, T, start, Hq, Hkv, d, window, sinks, false);
+    return span_choice(B, T, start, Hq, Hkv, d, window, sinks, false, false).ws_bytes;
 }
 
 int vitcop_window_attn(const uint16_t* q, int64_t q_row_stride, int64_t q_batch_stride, const vitcop_cache_t* C,
@@ -1591,14 +1591,14 @@ int vitcop_window_attn(const uint16_t* q, int64_t q_row_stride, int64_t q_batch_
     clamp_window(start + T, window, sinks);
     SpanCall c{q, q_row_stride, q_batch_stride, nullptr, nullptr, 0, 0, 0, 0, nullptr, 0, start_samples, n_samples, T, start,
                window, sinks, scale, out, lse_out};
-    rc = check_span_call("window_attn", c, C->d, ws, ws_bytes,
-                         span_workspace_bytes(C->B, T, start, Hq, C->Hkv, C->d, window, sinks, false));
-    return rc ? rc : launch_span_attn(c, *C, Hq, ws, static_cast<hipStream_t>(stream));
+    const SpanChoice p = span_choice(C->B, T, start, Hq, C->Hkv, C->d, window, sinks, false, start_samples || n_samples);
+    rc = check_span_call("window_attn", c, C->d, ws, ws_bytes, p.ws_bytes);
+    return rc ? rc : launch_span_attn(c, *C, Hq, p, ws, static_cast<hipStream_t>(stream));
 }
 
 size_t vitcop_tree_attn_workspace_bytes(int B, int T, int start, int Hq, int Hkv, int d) {
     if (check_span("tree_attn", B, T, start, Hq, Hkv, d) != VITCOP_OK || T > VITCOP_MAX_DRAFTS || B == 0 || T == 0) return 0;
-    return span_workspace_bytes(B, T, start, Hq, Hkv, d, 0, 0, true);
+    return span_choice(B, T, start, Hq, Hkv, d, 0, 0, true, false).ws_bytes;
 }
 
 int vitcop_tree_attn(const uint16_t* q, int64_t q_row_stride, int64_t q_batch_stride, const vitcop_cache_t* C,
@@ -1617,8 +1617,9 @@ int vitcop_tree_attn(const uint16_t* q, int64_t q_row_stride, int64_t q_batch_st
     if (T <= 1) k_row_stride = v_row_stride = width;
     REQUIRE(k_row_stride >= width && v_row_stride >= width, VITCOP_EINVAL, "tree_attn: row strides of k and v (%lld, %lld)",
             (long long)k_row_stride, (long long)v_row_stride);
-    REQUIRE(k_row_stride < (1 << 25) && v_row_stride < (1 << 25), VITCOP_EUNSUPPORTED,
-            "tree_attn: row strides of k and v (%lld, %lld) of 2^25 and more", (long long)k_row_stride, (long long)v_row_stride);
+    // (63 rows lie within 31 bits of bytes)
+    REQUIRE(k_row_stride < (1 << 24) && v_row_stride < (1 << 24), VITCOP_EUNSUPPORTED,
+            "tree_attn: row strides of k and v (%lld, %lld) of 2^24 and more", (long long)k_row_stride, (long long)v_row_stride);
     REQUIRE(tree_batch_stride == 0 || tree_batch_stride >= T, VITCOP_EINVAL, "tree_attn: batch stride of the tree %lld",
             (long long)tree_batch_stride);
     REQUIRE(tree_batch_stride < ((int64_t)1 << 31), VITCOP_EUNSUPPORTED, "tree_attn: batch stride of the tree past 2^31");
@@ -1629,8 +1630,9 @@ int vitcop_tree_attn(const uint16_t* q, int64_t q_row_stride, int64_t q_batch_st
     REQUIRE((reinterpret_cast<uintptr_t>(tree) & 7u) == 0, VITCOP_EINVAL, "tree_attn: the tree must be 8-byte aligned");
     SpanCall c{q, q_row_stride, q_batch_stride, k, v, k_row_stride, k_batch_stride, v_row_stride, v_batch_stride, tree,
                tree_batch_stride, start_samples, n_samples, T, start, 0, 0, scale, out, lse_out};
-    rc = check_span_call("tree_attn", c, C->d, ws, ws_bytes, span_workspace_bytes(C->B, T, start, Hq, C->Hkv, C->d, 0, 0, true));
-    return rc ? rc : launch_span_attn(c, *C, Hq, ws, static_cast<hipStream_t>(stream));
+    const SpanChoice p = span_choice(C->B, T, start, Hq, C->Hkv, C->d, 0, 0, true, start_samples || n_samples);
+    rc = check_span_call("tree_attn", c, C->d, ws, ws_bytes, p.ws_bytes);
+    return rc ? rc : launch_span_attn(c, *C, Hq, p, ws, static_cast<hipStream_t>(stream));
 }
 
 int vitcop_cache_append(const vitcop_cache_append_t* A, void* stream) {

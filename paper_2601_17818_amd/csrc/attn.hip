@@ -1031,15 +1031,18 @@ constexpr int AW_U2_MIN_WGS = 256;  // if that still leaves more workgroups than
 template <int D, bool CAUSAL, int U, bool REST = false, typename WIN = AttnWhole>
 static int launch_attn_wide(const uint16_t* q, const uint16_t* k, const uint16_t* v, uint16_t* out, float* lse,
                             int B, int N, int Hq, int Hkv, float sl2, int64_t kv_batch, hipStream_t s, const WIN& win = WIN{}) {
-    static std::atomic<bool> attr_set{false};   // set once; a second thread repeating the call is harmless
+    static std::atomic<uint64_t> raised{0};     // the devices where the limit has been raised; a second thread doing so is harmless
     constexpr int lds = AW_STAGES<D> * AW_STAGE<D>;
-    if (!attr_set.load(std::memory_order_acquire)) {
-        const int rc = hip_status(hipFuncSetAttribute((const void*)attn_wide_kernel<D, CAUSAL, U, REST, WIN>,
-                                                      hipFuncAttributeMaxDynamicSharedMemorySize, lds),
-                                  "hipFuncSetAttribute(attn_wide)");
-        if (rc) return rc;
-        attr_set.store(true, std::memory_order_release);
+    int device = 0;
+    int rc = hip_status(hipGetDevice(&device), "hipGetDevice");
+    const uint64_t bit = device < 64 ? (uint64_t)1 << device : 0;
+    if (rc == VITCOP_OK && !(raised.load(std::memory_order_acquire) & bit)) {
+        rc = hip_status(hipFuncSetAttribute((const void*)attn_wide_kernel<D, CAUSAL, U, REST, WIN>,
+                                            hipFuncAttributeMaxDynamicSharedMemorySize, lds),
+                        "hipFuncSetAttribute(attn_wide)");
+        if (rc == VITCOP_OK) raised.fetch_or(bit, std::memory_order_release);
     }
+    if (rc) return rc;
     constexpr int BM = 128 * U;
     const int n_qb = (N + BM - 1) / BM;
     long n_heads = (long)Hq * B;

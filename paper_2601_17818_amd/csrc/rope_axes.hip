@@ -43,7 +43,7 @@ __global__ __launch_bounds__(RA_THREADS) void rope_axes_kernel(const RopeAxesArg
     const int64_t row = (int64_t)(R.start_samples ? R.start_samples[b] : R.start) + t;
     const bool live = t < (R.n_samples ? R.n_samples[b] : R.T);
     if (!live) return;
-    const bool k_in_place = R.k_out == R.k, fits = k_in_place || (row >= 0 && row < R.capacity);
+    const bool k_in_place = R.k && R.k_out == R.k, fits = k_in_place || (row >= 0 && row < R.capacity);
     const uint16_t* src[HEADS];
     uint16_t* dst[HEADS];
     uint4 lo[HEADS], hi[HEADS];

@@ -8,8 +8,10 @@
 // row), the softmax with the lane's row as its only query, O^T += V^T P^T.
 //  - K goes from memory straight into the product, V through the wavefront's own piece of LDS and back transposed
 //    (ds_read_b64_tr_b16).  The key of element 4 t + r of a lane's 8 is 16 t + 4 (lane / 16) + r, where the scores are.
-//  - A probability goes into the product as the sum of two bf16, 16 bits of it: one of 8 would double the error that the
-//    rounding of the output makes.  Sums, references and outputs are fp32.
+//  - A probability goes into the product as the sum of bf16: of three for up to 16 rows, 24 bits as in vitcop_decode_attn (us with
+//    two and with three: 8 drafts x 32 heads x 384 keys 9.9, 10.2, 64 windows of 4096 x 28 / 4 heads 85, 85), of two for 32, where
+//    the third would cost more (16 trees of 25 drafts 65, 69.5) and 16 bits are 2^-8 of what the output's rounding takes away.
+//    Sums, references and outputs are fp32.
 //  - The running reference of the softmax moves only when a score exceeds it by 2^8; until then no lane needs another's scores.
 //  - Rows past a span's end are past its descriptor and read as zeros; what is masked is so by selection, so that neither
 //    stale rows nor drafts that nobody sees reach a result, whatever they hold.
@@ -17,7 +19,6 @@
 #include "vitcop_internal.h"
 #include "device_utils.h"
 #include "span_device.h"
-#include "span_plan.h"
 
 #include <algorithm>
 #include <type_traits>
@@ -33,7 +34,7 @@ __device__ __forceinline__ float span_lse(float m, float l) {
 
 template <int D, int NB, bool TREE>
 __global__ __launch_bounds__(64 * SP_WAVES, NB == 2 ? 2 : 3) void span_attn_kernel(const SpanArgs A) {
-    constexpr int STEPS = D / 32, BLOCKS = D / 16, ROWS = 16 * NB;
+    constexpr int STEPS = D / 32, BLOCKS = D / 16, ROWS = 16 * NB, PARTS = NB == 1 ? 3 : 2;
     constexpr int VROW = 2 * D + 32;                                 // bytes of a V row in LDS: the pad keeps eight rows apart
     constexpr int LPR = D / 8, RPL = 64 / LPR, VL = SP_KEYS / RPL;   // V: lanes a row, rows a load, loads a tile
     static_assert(SP_KEYS * VROW >= 16 * D * 4, "the outputs take V's place at the end");
@@ -199,7 +200,7 @@ __global__ __launch_bounds__(64 * SP_WAVES, NB == 2 ? 2 : 3) void span_attn_kern
                     for (int r = 0; r < 4; ++r) o[n][i][r] *= alpha;
             }
         }
-        u32x4 high[NB], low[NB];                                     // of each pair of probabilities
+        u32x4 part[NB][PARTS];                                       // of each pair of probabilities, the rest of the rest last
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
             const float base = m[n] == -INFINITY ? 0.f : m[n];       // (nothing but -inf so far: 0, not NaN)
@@ -209,9 +210,14 @@ __global__ __launch_bounds__(64 * SP_WAVES, NB == 2 ? 2 : 3) void span_attn_kern
                 const float c = __builtin_amdgcn_exp2f(fmaf(s[n][e >> 1][2 * (e & 1) + 1], A.scale_log2e, -base));
                 l[n] += a;
                 l[n] += c;
-                const uint32_t w = pack_bf16(a, c);
-                high[n][e] = w;
-                low[n][e] = pack_bf16(a - bf16_lo(w), c - bf16_hi(w));
+                float ra = a, rc = c;
+#pragma unroll
+                for (int k = 0; k < PARTS; ++k) {
+                    const uint32_t w = pack_bf16(ra, rc);
+                    part[n][k][e] = w;
+                    ra -= bf16_lo(w);
+                    rc -= bf16_hi(w);
+                }
             }
         }
         __builtin_amdgcn_wave_barrier();                             // (one wavefront's LDS accesses stay in order)
@@ -223,10 +229,10 @@ __global__ __launch_bounds__(64 * SP_WAVES, NB == 2 ? 2 : 3) void span_attn_kern
                 (__attribute__((address_space(3))) s16x4*)(uintptr_t)(tr + i * 32 + 16 * VROW));
             const bf16x8 vf = __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-            for (int n = 0; n < NB; ++n) {
-                o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, high[n]), o[n][i], 0, 0, 0);
-                o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, low[n]), o[n][i], 0, 0, 0);
-            }
+            for (int k = 0; k < PARTS; ++k)
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+                    o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, part[n][k]), o[n][i], 0, 0, 0);
         }
         __builtin_amdgcn_wave_barrier();                             // the next tile's rows replace these
     }
@@ -358,26 +364,21 @@ static int launch_span_merge(const SpanArgs& A, hipStream_t s) {
     return launch_status("span_merge");
 }
 
-static SpanPlan plan_of(int B, int T, int start, int Hq, int Hkv, int d, int window, int sinks, bool tree, bool own,
-                        bool* ragged = nullptr) {
+SpanChoice span_choice(int B, int T, int start, int Hq, int Hkv, int d, int window, int sinks, bool tree, bool own) {
     // the wide kernel addresses a span with 32 bits of bytes
     const int64_t all = (int64_t)start + T, keys = window == 0 ? all : std::min<int64_t>(all, (int64_t)window + T);
-    const SpanSizes z{B, Hkv, T, Hq / Hkv, start, window, sinks, d, tree, own};
-    if (ragged) *ragged = z.ragged();
-    return span_plan(z, (std::max<int64_t>(keys, sinks) + 256) * Hkv * d * 2 < ((int64_t)1 << 32));
-}
-
-size_t span_workspace_bytes(int B, int T, int start, int Hq, int Hkv, int d, int window, int sinks, bool tree) {
-    size_t s = 1;                                            // (a call may have samples of their own lengths or not)
-    for (const bool own : {false, true})
-        s = std::max<size_t>(s, plan_of(B, T, start, Hq, Hkv, d, window, sinks, tree, own).slices);
-    return s == 1 ? 0 : up256((size_t)B * T * Hq * s * d * 4) + up256((size_t)B * T * Hq * s * 2 * 4);
+    const bool fits = (std::max<int64_t>(keys, sinks) + 256) * Hkv * d * 2 < ((int64_t)1 << 32);
+    SpanSizes z{B, Hkv, T, Hq / Hkv, start, window, sinks, d, tree, own};
+    SpanChoice c{span_plan(z, fits), z.ragged(), 0};
+    size_t most = c.plan.slices;                             // (the same sizes with the other kind of lengths)
+    z.own = !own;
+    if (z.ragged() != c.ragged) most = std::max<size_t>(most, span_plan(z, fits).slices);
+    if (most > 1) c.ws_bytes = up256((size_t)B * T * Hq * most * d * 4) + up256((size_t)B * T * Hq * most * 2 * 4);
+    return c;
 }
 
 template <int D>
-static int launch_span_d(SpanArgs A, int Hq, void* ws, hipStream_t s) {
-    const SpanPlan p = plan_of(A.B, A.T, A.start, Hq, A.Hkv, D, A.window, A.sinks, A.tree != nullptr, A.starts || A.counts,
-                               &A.ragged);
+static int launch_span_d(SpanArgs A, const SpanPlan& p, int Hq, void* ws, hipStream_t s) {
     A.row_blocks = p.row_blocks;
     A.slices = p.slices;
     A.part_o = static_cast<float*>(ws);
@@ -398,7 +399,7 @@ static int launch_span_d(SpanArgs A, int Hq, void* ws, hipStream_t s) {
     return rc || p.slices == 1 ? rc : launch_span_merge<D>(A, s);
 }
 
-int launch_span_attn(const SpanCall& c, const vitcop_cache_t& C, int Hq, void* ws, hipStream_t s) {
+int launch_span_attn(const SpanCall& c, const vitcop_cache_t& C, int Hq, const SpanChoice& p, void* ws, hipStream_t s) {
     SpanArgs A{};
     A.q = c.q;
     A.q_row = c.q_row;
@@ -426,7 +427,8 @@ int launch_span_attn(const SpanCall& c, const vitcop_cache_t& C, int Hq, void* w
     A.scale_log2e = c.scale * 1.4426950408889634f;
     A.out = c.out;
     A.lse = c.lse;
-    return C.d == 64 ? launch_span_d<64>(A, Hq, ws, s) : launch_span_d<128>(A, Hq, ws, s);
+    A.ragged = p.ragged;
+    return C.d == 64 ? launch_span_d<64>(A, p.plan, Hq, ws, s) : launch_span_d<128>(A, p.plan, Hq, ws, s);
 }
 
 }  // namespace vitcop

@@ -7,6 +7,7 @@
 #include <stdint.h>
 #include <stddef.h>
 
+#include "span_plan.h"
 #include "vitcop.h"
 
 namespace vitcop {
@@ -86,8 +87,13 @@ struct SpanCall {
     uint16_t* out;
     float* lse;
 };
-size_t span_workspace_bytes(int B, int T, int start, int Hq, int Hkv, int d, int window, int sinks, bool tree);
-int launch_span_attn(const SpanCall& c, const vitcop_cache_t& C, int Hq, void* ws, hipStream_t s);
+struct SpanChoice {
+    SpanPlan plan;
+    bool ragged;                             // samples in the order of their lengths
+    size_t ws_bytes;                         // for these sizes, with lengths of their own (`own`) or without
+};
+SpanChoice span_choice(int B, int T, int start, int Hq, int Hkv, int d, int window, int sinks, bool tree, bool own);
+int launch_span_attn(const SpanCall& c, const vitcop_cache_t& C, int Hq, const SpanChoice& p, void* ws, hipStream_t s);
 int launch_rope_axes(const vitcop_rope_axes_t& R, hipStream_t s);
 int launch_cache_append(const vitcop_cache_append_t& A, hipStream_t s);
 

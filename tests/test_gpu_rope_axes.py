@@ -129,6 +129,18 @@ def test_rows_outside_the_cache_are_skipped(vc):
     assert np.array_equal(host_bits(kc), want_k) and np.array_equal(host_bits(vcache), want_v)
 
 
+def test_values_alone_outside_the_cache_are_skipped(vc):
+    B, T, Hkv, d, capacity = 3, 2, 2, 64, 4
+    rng = np.random.default_rng(9)
+    v = bits(rng, (B, T, Hkv, d))
+    room = marked((B + 2, capacity, Hkv, d))                             # (the cache lies between two more)
+    cache = vc.Cache(marked((B, capacity, Hkv, d)), room[1:B + 1])
+    vc.vitcop_rope_axes(None, None, ints(np.zeros((1, B, T))), (32,), v=dev(v), cache=cache, start_samples=ints([-1, 3, 4]))
+    want = np.full((B + 2, capacity, Hkv, d), MARK, np.uint16)
+    want[1, 0], want[2, 3] = v[0, 1], v[1, 0]
+    assert np.array_equal(host_bits(room), want)
+
+
 def test_in_place_and_values_alone(vc):
     B, T, H, d = 2, 11, 3, 64
     rng = np.random.default_rng(5)

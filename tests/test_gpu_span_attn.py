@@ -2,8 +2,8 @@
 
 Bounds. A score's fp32 sum of d products and its scaling are off by at most e = (d + 4) 2^-24 of the sum of |q k| scale; a
 probability then by e twice over (its own and its sum's) and by 2^-21 of the exponential and its argument; the sums over n keys
-by n 2^-24. A probability goes into the product with V in 16 bits (half a step of the second eight: 2^-16), in calls of more than
-32 query rows to a KV head in eight (2^-8). The output is rounded to bf16: 2^-8 of it. lse: e, the sum's n 2^-24, 2^-21 and 2^-22 of its own size.
+by n 2^-24. A probability goes into the product with V in 24 bits (half a step of the third eight: 2^-24), in calls of more than
+16 query rows to a KV head in 16 (2^-16), of more than 32 in eight (2^-8). The output is rounded to bf16: 2^-8 of it. lse: e, the sum's n 2^-24, 2^-21 and 2^-22 of its own size.
 """
 import math
 
@@ -18,7 +18,6 @@ from oracle import vitcop_oracle as O
 
 pytestmark = pytest.mark.gpu
 
-FEW = 32                       # query rows to a KV head whose probabilities are 16 bits
 
 
 @pytest.fixture(scope="module")
@@ -36,7 +35,7 @@ def check(got, lse, want, rows, where):
     d = got.shape[-1]
     keys = want["keys"]
     e = (d + 4) * 2.0 ** -24 * want["reach"]
-    p = 2.0 ** -16 if rows <= FEW else 2.0 ** -8
+    p = 2.0 ** -24 if rows <= 16 else 2.0 ** -16 if rows <= 32 else 2.0 ** -8
     bound = 2.0 ** -8 * np.abs(want["out"]) + (p + 2 * e[..., None] + 2.0 ** -21 + keys * 2.0 ** -24) * want["mass"] * 1.01
     err = np.abs(got - want["out"])
     assert (err <= bound).all(), f"{where}: {np.max(err - bound)} over the bound {bound.flat[np.argmax(err - bound)]}"

@@ -73,7 +73,7 @@ def test_windows(change, code):
 @pytest.mark.parametrize("change,code", [
     (dict(T=65), EUNSUPPORTED), (dict(k=None), EINVAL), (dict(v=None), EINVAL), (dict(tree=None), EINVAL), (dict(tree=A + 4), EINVAL),
     (dict(k=A + 8), EINVAL), (dict(v=A + 8), EINVAL), (dict(k_row=248), EINVAL), (dict(v_row=128), EINVAL), (dict(v_row=260), EINVAL),
-    (dict(k_batch=-1024), EINVAL), (dict(k_row=1 << 25), EUNSUPPORTED), (dict(t_batch=3), EINVAL), (dict(t_batch=-4), EINVAL),
+    (dict(k_batch=-1024), EINVAL), (dict(k_row=1 << 24), EUNSUPPORTED), (dict(v_row=1 << 24), EUNSUPPORTED), (dict(t_batch=3), EINVAL), (dict(t_batch=-4), EINVAL),
     (dict(t_batch=1 << 31), EUNSUPPORTED)])
 def test_trees(change, code):
     assert tree(**change) == code
