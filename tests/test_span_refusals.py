@@ -10,14 +10,55 @@ lib = vc.lib
 A = 0x1000              # a fake, aligned, non-null device pointer (never dereferenced)
 EINVAL, EUNSUPPORTED, EWORKSPACE, OK = vc.VITCOP_EINVAL, vc.VITCOP_EUNSUPPORTED, vc.VITCOP_EWORKSPACE, vc.VITCOP_OK
 BIG = 2147483647
+Sections = C.c_int * vc.VITCOP_MAX_AXES
+
+
+class CacheT(C.Structure):
+    _fields_ = ([(n, C.c_int) for n in ("B", "capacity", "Hkv", "d")] + [("k", C.c_void_p), ("v", C.c_void_p)])
+
+
+class RopeAxesT(C.Structure):
+    _fields_ = ([(n, C.c_int) for n in ("B", "T", "Hq", "Hkv", "d", "n_axes", "interleaved")] +
+                [("sections", Sections), ("theta", C.c_float), ("capacity", C.c_int), ("start", C.c_int)] +
+                [(n, C.c_void_p) for n in ("positions", "q", "k", "v")] +
+                [(n, C.c_int64) for n in ("q_row_stride", "q_batch_stride", "k_row_stride", "k_batch_stride",
+                                           "v_row_stride", "v_batch_stride")] +
+                [(n, C.c_void_p) for n in ("q_out", "k_out", "v_out", "start_samples", "n_samples")])
+
+
+class CacheAppendT(C.Structure):
+    _fields_ = ([(n, C.c_int) for n in ("n_layers", "B", "capacity", "Hkv", "d", "T", "rows")] +
+                [("k_cache", C.POINTER(C.c_void_p)), ("v_cache", C.POINTER(C.c_void_p)), ("cache_layer_stride", C.c_int64),
+                 ("k", C.c_void_p), ("v", C.c_void_p)] +
+                [(n, C.c_int64) for n in ("k_layer_stride", "k_batch_stride", "k_row_stride",
+                                           "v_layer_stride", "v_batch_stride", "v_row_stride")] +
+                [("start", C.POINTER(C.c_int))] + [(n, C.c_void_p) for n in ("start_samples", "idx", "n_samples")])
 
 
 def test_struct_layouts():
-    assert C.sizeof(vc.CacheT) == 32 and C.sizeof(vc.RopeAxesT) == 176 and C.sizeof(vc.CacheAppendT) == 152
+    assert vc._CACHE.size == 32 and vc._ROPE_AXES.size == 176 and vc._CACHE_APPEND.size == 152
+    assert C.sizeof(CacheT) == 32 and C.sizeof(RopeAxesT) == 176 and C.sizeof(CacheAppendT) == 152
+
+
+def test_packed_descriptors():
+    """The binding's bytes are the structures'."""
+    for packed, kind in ((vc._CACHE, CacheT), (vc._ROPE_AXES, RopeAxesT), (vc._CACHE_APPEND, CacheAppendT)):
+        s = kind()
+        n, flat = 1, []
+        for name, field in kind._fields_:
+            if field is Sections:
+                s.sections = Sections(*range(n, n + 4))
+                flat += range(n, n + 4)
+                n += 4
+                continue
+            setattr(s, name, C.cast(n * 16, field) if issubclass(field, C._Pointer) else n * 16)
+            flat.append(n * 16)
+            n += 1
+        assert packed.pack(*flat) == bytes(s)
 
 
 def cache(B=2, capacity=64, Hkv=2, d=128, k=A, v=A):
-    return vc.CacheT(B, capacity, Hkv, d, k, v)
+    return CacheT(B, capacity, Hkv, d, k, v)
 
 
 CACHES = [(dict(B=-1), EINVAL), (dict(capacity=-1), EINVAL), (dict(Hkv=0), EINVAL), (dict(d=96), EUNSUPPORTED),
@@ -46,7 +87,7 @@ def test_descriptor(change, code):
 
 
 def test_null_descriptors():
-    null = C.POINTER(vc.CacheT)()
+    null = C.POINTER(CacheT)()
     assert window(null) == EINVAL and tree(null) == EINVAL
     assert lib.vitcop_rope_axes(None, None) == EINVAL and lib.vitcop_cache_append(None, None) == EINVAL
 
@@ -99,7 +140,7 @@ def rope(**change):
                   positions=A, q=A, k=A, v=A, q_row=512, q_batch=1536, k_row=512, k_batch=1536, v_row=512, v_batch=1536,
                   q_out=2 * A, k_out=3 * A, v_out=4 * A, start_samples=None, n_samples=None), **change)
     p["sections"] = (C.c_int * 4)(*p["sections"])
-    return lib.vitcop_rope_axes(vc.RopeAxesT(*p.values()), None)
+    return lib.vitcop_rope_axes(C.byref(RopeAxesT(*p.values())), None)
 
 
 @pytest.mark.parametrize("change,code", [
@@ -125,7 +166,7 @@ def append(**change):
     two, starts = (C.c_void_p * 2)(A, 2 * A), (C.c_int * 2)(0, 5)
     p = dict(dict(n_layers=2, B=2, capacity=9, Hkv=2, d=64, T=4, rows=4, k_cache=two, v_cache=two, cl=0, k=A, v=A, kl=1024, kb=512, kr=128,
                   vl=1024, vb=512, vr=128, start=starts, start_samples=None, idx=None, n_samples=None), **change)
-    return lib.vitcop_cache_append(vc.CacheAppendT(*p.values()), None)
+    return lib.vitcop_cache_append(C.byref(CacheAppendT(*p.values())), None)
 
 
 NULLS = C.POINTER(C.c_void_p)()
