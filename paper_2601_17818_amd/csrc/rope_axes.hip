@@ -13,8 +13,8 @@ namespace vitcop {
 // 32-bit product of a far position and a speed has lost (position 10^5, the fastest pair: 2^-8 of a radian), and costs two
 // integer products instead of arithmetic in 64-bit floating point.  The host gives the speed of every eighth pair, each thread
 // goes on from there by products with theta^(-2/d) (64 bits of each are kept: the eighth is off by less than 2^-60, the farthest
-// position's angle by 2^-29 of a revolution), which keeps the launch's arguments short: all speeds of 128 channels and the caches' descriptor
-// took 6.8 us of host time a call, this 4.1.
+// position's angle by 2^-29 of a revolution), which keeps the launch's arguments short: all speeds of 128 channels and the caches'
+// descriptor took 6.8 us of host time a call, this 4.1.
 struct RopeAxesArgs {
     vitcop_rope_axes_t R;
     int slots;                          // threads that share a pair group's heads
@@ -126,8 +126,9 @@ int launch_rope_axes(const vitcop_rope_axes_t& R, hipStream_t s) {
 }
 
 // Rows to the caches: 16 bytes a thread, with non-temporal stores (us with ordinary and with these, of 8 KB a row: 32 layers x 16
-// samples x up to 8 of 16 rows 26.3, 19.3, 4 x 16 x 64 19.5, 14.4).  The caches of up to CA_LAYERS layers by a table, or, where they are one allocation,
-// by the first one and their distance, which spares the call the table (32 layers, host time with the binding 14.0 -> 10.1 us).
+// samples x up to 8 of 16 rows 26.3, 19.3, 4 x 16 x 64 19.5, 14.4).  The caches of up to CA_LAYERS layers by a table, or, where
+// they are one allocation, by the first one and their distance, which spares the call the table (32 layers, host time with the
+// binding 14.0 -> 10.1 us).
 constexpr int CA_THREADS = 256, CA_LAYERS = 64;
 struct CacheTable {
     uint16_t* cache[2][CA_LAYERS];          // of k, of v
