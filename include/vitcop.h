@@ -636,7 +636,7 @@ int vitcop_rope_axes(const vitcop_rope_axes_t* R, void* stream);
  *   ws: device scratch of ws_bytes >= vitcop_window_attn_workspace_bytes, NULL where that is 0 (it is 0 too where the
  *   sizes are refused)
  * d in {64,128}; Hq % Hkv == 0; 0 <= start, start + T <= capacity; window, sinks >= 0; B, Hkv <= 65535;
- * B*T*Hq < 2^28. */
+ * B*T*Hq < 2^28; at most 32*65535 query rows T*Hq/Hkv where a sample's rows in reach are 4 GiB and more. */
 size_t vitcop_window_attn_workspace_bytes(int B, int T, int start, int Hq, int Hkv, int d, int window, int sinks);
 int vitcop_window_attn(const uint16_t* q, int64_t q_row_stride, int64_t q_batch_stride, const vitcop_cache_t* C,
                        uint16_t* out, float* lse_out, int T, int start, const int32_t* start_samples,
@@ -660,9 +660,9 @@ int vitcop_tree_attn(const uint16_t* q, int64_t q_row_stride, int64_t q_batch_st
                      uint16_t* out, float* lse_out, int T, int start, const int32_t* start_samples,
                      const int32_t* n_samples, int Hq, float scale, void* ws, size_t ws_bytes, void* stream);
 
-/* Rows to the caches of all layers in one launch (for 64 of them, where they are given one by one): row i < n_b of sample b, which is row idx[b,i] of k and v
- * (i, without idx), goes to row start + i of its cache in layer l: start[l], or start_samples[l*B + b] (caches of a pruned
- * prefill have lengths of their own in each layer).  n_b: `rows`, or n_samples[b] clamped to [0, rows].  Sources outside
+/* Rows to the caches of all layers in one launch (for 64 of them, where they are given one by one): row i < n_b of
+ * sample b, which is row idx[b,i] of k and v (i, without idx), goes to row start + i of its cache in layer l: start[l], or
+ * start_samples[l*B + b] (caches of a pruned prefill have lengths of their own in each layer).  n_b: `rows`, or n_samples[b] clamped to [0, rows].  Sources outside
  * [0,T) and targets outside [0,capacity) are skipped on the device; all other rows stay as they were.
  *   k_cache, v_cache: host arrays of n_layers device pointers, each [B,capacity,Hkv,d]; with a cache_layer_stride other than
  *   0, arrays of one, the first layer's, behind which the others lie that many elements apart

@@ -174,7 +174,8 @@ int launch_cache_append(const vitcop_cache_append_t& A, hipStream_t s) {
     const int sides = (A.k != nullptr) + (A.v != nullptr);
     const unsigned wgs = (unsigned)((units + CA_THREADS - 1) / CA_THREADS);
     if (A.cache_layer_stride != 0 && A.start_samples && A.n_layers * sides <= 65535) {
-        const CacheAppendArgs<CacheStack> P{A, 0, sides, {{A.k ? A.k_cache[0] : nullptr, A.v ? A.v_cache[0] : nullptr}, A.cache_layer_stride}};
+        const CacheStack caches{{A.k ? A.k_cache[0] : nullptr, A.v ? A.v_cache[0] : nullptr}, A.cache_layer_stride};
+        const CacheAppendArgs<CacheStack> P{A, 0, sides, caches};
         hipLaunchKernelGGL(cache_append_kernel<CacheStack>, dim3(wgs, A.B, sides * A.n_layers), dim3(CA_THREADS), 0, s, P);
         return launch_status("cache_append");
     }

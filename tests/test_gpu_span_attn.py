@@ -348,6 +348,50 @@ def test_another_stream_and_a_graph(vc):
                 assert torch.equal(o, wo) and torch.equal(e, we)
 
 
+def test_many_rows_on_two_streams_at_once_and_in_a_graph(vc):
+    """Questions of many rows: two streams at once, each with its own workspace, and replays that go by the lengths."""
+    B, T, n, Hq, Hkv, d = 3, 150, 700, 8, 2, 128
+    rng = np.random.default_rng(13)
+    k, v = (dev(bits(rng, (B, n + T, Hkv, d))) for _ in range(2))
+    q = dev(bits(rng, (B, T, Hq, d)))
+    starts, counts = (torch.zeros(B, dtype=torch.int32, device="cuda") for _ in range(2))
+    cache = vc.Cache(k, v)
+
+    def fresh():
+        return torch.zeros((B, T, Hq, d), dtype=torch.bfloat16, device="cuda"), torch.zeros((B, Hq, T), device="cuda")
+
+    def call(window, out):
+        return vc.vitcop_window_attn(q, cache, n, window, 4, starts, counts, out=out)
+
+    starts.copy_(torch.tensor([700, 20, 333], dtype=torch.int32))
+    counts.copy_(torch.tensor([150, 1, 70], dtype=torch.int32))
+    want = [call(w, fresh()) for w in (0, 90)]
+    outs = [[fresh() for _ in range(4)] for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for i in range(4):
+        for j, side in enumerate(streams):
+            with torch.cuda.stream(side):
+                call((0, 90)[j], outs[j][i])
+    torch.cuda.synchronize()
+    for j in range(2):
+        for o, e in outs[j]:
+            assert torch.equal(o, want[j][0]) and torch.equal(e, want[j][1])
+    out = fresh()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call(90, out)
+    for s, c in (([700, 0, 5], [150, 150, 0]), ([0, 699, 350], [149, 2, 128]), ([700, 700, 700], [1, 150, 33])):
+        starts.copy_(torch.tensor(s, dtype=torch.int32))
+        counts.copy_(torch.tensor(c, dtype=torch.int32))
+        for t in out:
+            t.zero_()
+        g.replay()
+        o, e = call(90, fresh())
+        torch.cuda.synchronize()
+        assert torch.equal(out[0], o) and torch.equal(out[1], e)
+
+
 def test_calls_repeat_bit_for_bit(vc):
     c = Case(vc, 11, 2, 20, 1500, 8, 2, 128)
     a = [t.clone() for t in c.window(0, 0)]

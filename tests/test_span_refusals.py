@@ -120,6 +120,14 @@ def test_trees(change, code):
     assert tree(**change) == code
 
 
+def test_more_query_rows_than_a_grid_has_blocks_for():
+    """65535 blocks of 32 rows, where a cache of 4 GiB and more leaves the kernel of many rows out."""
+    c = C.byref(cache(B=1, capacity=1 << 22, Hkv=32))
+    row = 32 * 128
+    assert window(c, T=32 * 65535 + 1, start=0, Hq=32, row=row) == EUNSUPPORTED
+    assert b"query rows" in lib.vitcop_last_error()
+
+
 def test_workspaces():
     c = C.byref(cache(B=1, capacity=5000, Hkv=1))
     for need, call in ((lib.vitcop_window_attn_workspace_bytes(1, 1, 4000, 1, 1, 128, 0, 0), window),
