@@ -448,7 +448,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
         const uint16_t* qp = q + ((int64_t)b * N + query) * q_rs + h * D + 8 * g;
         if constexpr (SPANS) {
             const int G = win.a.G, tok = query / G;
-            qp = q + b * win.a.q_batch + tok * win.a.q_row + (hk * G + query - tok * G) * D + 8 * g;
+            qp = q + b * win.a.q_batch + tok * win.a.q_row + (int64_t)(hk * G + query - tok * G) * D + 8 * g;
             at[u] = start + tok;
             if constexpr (TREE) {
                 const uint64_t w = win.a.tree[b * win.a.tree_batch + tok] & (~0ull >> (64 - n_tok));
@@ -1002,7 +1002,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
             float* lp = lse + ((int64_t)b * Hq + h) * N + query;
             if constexpr (SPANS) {
                 const int tok = query / win.a.G, head = hk * win.a.G + query - tok * win.a.G;
-                op = out + ((int64_t)b * win.a.T + tok) * q_rs + head * D;
+                op = out + ((int64_t)b * win.a.T + tok) * q_rs + (int64_t)head * D;
                 lp = lse + ((int64_t)b * Hq + head) * win.a.T + tok;
             }
 #pragma unroll

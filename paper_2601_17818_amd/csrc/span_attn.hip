@@ -110,7 +110,7 @@ __global__ __launch_bounds__(64 * SP_WAVES, NB == 2 ? 2 : 3) void span_attn_kern
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
         const int r = r0 + min(16 * n + l16, n_rows - 1), t = r / G, g = r - t * G;
-        const uint16_t* qp = A.q + b * A.q_batch + t * A.q_row + (hk * G + g) * D + 8 * g4;
+        const uint16_t* qp = A.q + b * A.q_batch + t * A.q_row + (int64_t)(hk * G + g) * D + 8 * g4;
 #pragma unroll
         for (int c = 0; c < STEPS; ++c) qf[n][c] = *reinterpret_cast<const bf16x8*>(qp + 32 * c);
         at[n] = start + t;

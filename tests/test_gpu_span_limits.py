@@ -1,0 +1,73 @@
+"""vitcop_window_attn and vitcop_tree_attn where offsets pass 31 and 32 bits.  Bounds as in test_gpu_span_attn.py."""
+import numpy as np
+import pytest
+import torch
+
+from gpu_util import dev
+from oracle import span_oracle as S
+from oracle import vitcop_oracle as O
+from test_gpu_span_attn import bits, vc  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+PERIOD = 1031                      # query heads repeat after so many: one that is read in another's place is seen
+
+
+def bounds(want, d, keys):
+    """Of outputs [n,Hq,d] and of lse [n,Hq], where more than 32 query rows read a KV head."""
+    e = (d + 4) * 2.0 ** -24 * want["reach"]
+    out = 2.0 ** -8 * np.abs(want["out"]) + (2.0 ** -8 + 2 * e[..., None] + 2.0 ** -21 + keys * 2.0 ** -24) * want["mass"] * 1.01
+    return out, 1.01 * e + 2.0 ** -21 + keys * 2.0 ** -24 + 2.0 ** -22 * np.abs(want["lse"].T)
+
+
+def assert_heads(out, lse, q, k, v, keys):
+    """out [Hkv,G,d] and lse [Hkv,G] of one token, head g of each being q[g % PERIOD], over k, v [keys,Hkv,d]."""
+    f64 = O.bf16_to_f64
+    Hkv, G, d = out.shape
+    for hk in sorted({0, 1, Hkv - 1} & set(range(Hkv))):
+        want = S.attend(f64(q)[None], f64(k[:, hk:hk + 1]), f64(v[:, hk:hk + 1]), np.ones((1, keys), bool))
+        ob, lb = (torch.from_numpy(x[0]).cuda() for x in bounds(want, d, keys))
+        wo, wl = torch.from_numpy(want["out"][0]).cuda(), torch.from_numpy(want["lse"][:, 0]).cuda()
+        for first in range(0, G, 256 * PERIOD):
+            n = min(256 * PERIOD, G - first)
+            at = torch.arange(n, device="cuda") % PERIOD
+            assert bool(((out[hk, first:first + n].double() - wo[at]).abs() <= ob[at]).all()), (hk, first)
+            assert bool(((lse[hk, first:first + n].double() - wl[at]).abs() <= lb[at]).all()), (hk, first)
+
+
+def heads(q, n):
+    tile = dev(q)
+    return tile.repeat((n + PERIOD - 1) // PERIOD, 1)[:n]
+
+
+def test_query_heads_past_31_bits(vc):  # noqa: F811
+    """A token of more than 2^24 query heads of 128 channels: a head's offset in its row passes 2^31."""
+    d, n, G = 128, 70, (1 << 24) + 200
+    rng = np.random.default_rng(1)
+    q, k, v = bits(rng, (PERIOD, d)), bits(rng, (n + 1, 1, d)), bits(rng, (n + 1, 1, d))
+    qd = heads(q, G).view(1, 1, G, d)
+    cache = vc.Cache(dev(k)[None], dev(v)[None])
+    out, lse = vc.vitcop_window_attn(qd, cache, n)
+    assert_heads(out.view(1, G, d), lse.view(1, G), q, k, v, n + 1)
+    out.fill_(7.5)
+    k2, v2 = (dev(x[n:]).view(1, 1, 1, d) for x in (k, v))
+    vc.vitcop_tree_attn(qd, k2, v2, torch.ones((1, 1), dtype=torch.int64, device="cuda"), cache, n, out=(out, lse))
+    assert_heads(out.view(1, G, d), lse.view(1, G), q, k, v, n + 1)
+
+
+def test_query_heads_past_31_bits_over_4_gib_of_cache(vc):  # noqa: F811
+    """The same where the cache's rows leave the kernel of many query rows out; few of the rows are there."""
+    d, n, Hkv, G, start = 128, 70, 16, (1 << 20) + 40, 1 << 20
+    rng = np.random.default_rng(2)
+    q, k, v = bits(rng, (PERIOD, d)), bits(rng, (n + 1, Hkv, d)), bits(rng, (n + 1, Hkv, d))
+    qd = heads(q, G)[None].expand(Hkv, G, d).reshape(1, 1, Hkv * G, d)
+    kc, vcache = (torch.empty((1, start + 1, Hkv, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    kc[0, :n + 1], vcache[0, :n + 1] = dev(k), dev(v)
+    cache, at = vc.Cache(kc, vcache), torch.tensor([n], dtype=torch.int32, device="cuda")
+    out, lse = vc.vitcop_window_attn(qd, cache, start, start_samples=at)
+    assert_heads(out.view(Hkv, G, d), lse.view(Hkv, G), q, k, v, n + 1)
+    out.fill_(7.5)
+    k2, v2 = (dev(x[n:]).view(1, 1, Hkv, d) for x in (k, v))
+    vc.vitcop_tree_attn(qd, k2, v2, torch.ones((1, 1), dtype=torch.int64, device="cuda"), cache, start, start_samples=at,
+                        out=(out, lse))
+    assert_heads(out.view(Hkv, G, d), lse.view(Hkv, G), q, k, v, n + 1)
