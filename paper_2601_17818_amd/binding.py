@@ -1145,7 +1145,7 @@ def vitcop_rope_axes(q, k, positions, sections, theta: float = 10000.0, v=None, 
         if out is None:
             out = torch.empty((B, T, Hq, d), dtype=q.dtype, device=q.device)
         q_to = out.data_ptr()
-        if q_to != q_at:
+        if q_to != q_at or not q_at:                     # (the address of every tensor without elements is 0)
             _expect(out, "out", (B, T, Hq, d), None, dev)
         elif out is not q and _token_rows(out, "out", dev, (B, T, Hq, d)) != (q_row, q_batch):
             raise ValueError("out begins where q does, with other strides")
@@ -1176,7 +1176,7 @@ def vitcop_rope_axes(q, k, positions, sections, theta: float = 10000.0, v=None, 
         if k_out is None:
             k_out = torch.empty((B, T, Hkv, d), dtype=k.dtype, device=k.device)
         k_to = k_out.data_ptr()
-        if k_to != k_at:
+        if k_to != k_at or not k_at:
             _expect(k_out, "k_out", (B, T, Hkv, d), None, dev)
         elif k_out is not k and _token_rows(k_out, "k_out", dev, (B, T, Hkv, d)) != (k_row, k_batch):
             raise ValueError("k_out begins where k does, with other strides")
