@@ -1644,7 +1644,7 @@ int vitcop_cache_append(const vitcop_cache_append_t* A, void* stream) {
     REQUIRE(A->B <= 65535 && (int64_t)A->Hkv * A->d <= INT32_MAX && at_most(A->rows, (int64_t)A->Hkv * A->d, INT32_MAX),
             VITCOP_EUNSUPPORTED, "cache_append: B above 65535, or rows*Hkv*d of 2^31 and more");
     REQUIRE(A->idx || A->rows <= A->T, VITCOP_EINVAL, "cache_append: %d rows of %d", A->rows, A->T);
-    if (A->n_layers == 0 || A->B == 0 || A->rows == 0) return VITCOP_OK;
+    if (A->n_layers == 0 || A->B == 0 || A->rows == 0 || A->T == 0) return VITCOP_OK;        // (T 0: there is no source)
     REQUIRE(A->k || A->v, VITCOP_EINVAL, "cache_append: k and v are both null");
     REQUIRE(aligned16(A->k) && aligned16(A->v), VITCOP_EINVAL, "cache_append: k and v must be 16-byte aligned");
     REQUIRE((!A->k || A->k_cache) && (!A->v || A->v_cache) && (A->start || A->start_samples), VITCOP_EINVAL,

@@ -71,3 +71,13 @@ def test_cache_append(B, T, stacked):
     caches = caches if stacked else list(caches)
     wide = rows(L, B, T + 2, 2 * HKV, D)[:, :, :T]
     vc.vitcop_cache_append(caches, caches, wide[:, :, :, :HKV], wide[:, :, :, HKV:], start_samples=ints(L, B))
+
+
+@pytest.mark.parametrize("stacked", [True, False])
+def test_cache_append_of_paths_through_no_token(stacked):
+    """Every source is outside of no rows: nothing is written."""
+    caches = rows(3, 2, 5, HKV, D)
+    caches = caches if stacked else list(caches)
+    wide = rows(3, 2, 0, 2 * HKV, D)
+    vc.vitcop_cache_append(caches, caches, wide[:, :, :, :HKV], wide[:, :, :, HKV:], start=1, idx=ints(2, 4))
+    vc.vitcop_cache_append(caches, None, wide[:, :, :, :HKV], None, start_samples=ints(3, 2), idx=ints(2, 4))
