@@ -3,10 +3,10 @@ import numpy as np
 import pytest
 import torch
 
-from gpu_util import dev
+from gpu_util import dev, host_f64
 from oracle import span_oracle as S
 from oracle import vitcop_oracle as O
-from test_gpu_span_attn import bits, vc  # noqa: F401
+from test_gpu_span_attn import bits, trees, vc  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -71,3 +71,56 @@ def test_query_heads_past_31_bits_over_4_gib_of_cache(vc):  # noqa: F811
     vc.vitcop_tree_attn(qd, k2, v2, torch.ones((1, 1), dtype=torch.int64, device="cuda"), cache, start, start_samples=at,
                         out=(out, lse))
     assert_heads(out.view(Hkv, G, d), lse.view(Hkv, G), q, k, v, n + 1)
+
+
+# Rows of 128 KiB, 512 KV heads of one query head each: 32400 of them end 14 MB below 2^32 bytes with the kernel's margin of 256 rows.
+HKV, D, ROWS, NEAR = 512, 128, 40000, 32400
+HEADS = [0, 1, 255, 511]
+
+
+@pytest.fixture(scope="module")
+def large(vc):  # noqa: F811
+    torch.manual_seed(3)
+    k, v = (torch.randn((1, ROWS, HKV, D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    q = torch.randn((1, 70, HKV, D), dtype=torch.bfloat16, device="cuda")
+    some = [host_f64(t[0][:, HEADS].contiguous()) for t in (q, k, v)]
+    return vc.Cache(k, v), q, some
+
+
+def assert_rows(out, lse, q, k, v, sees, where):
+    """out [T,Hq,d], lse [Hq,T] of all heads; q, k, v of those looked at."""
+    n, keys = sees.shape
+    want = S.attend(q[:n], k[:keys], v[:keys], sees)
+    ob, lb = bounds(want, D, keys)
+    assert (np.abs(host_f64(out)[:n, HEADS] - want["out"]) <= ob).all(), where
+    assert (np.abs(host_f64(lse)[HEADS, :n] - want["lse"]) <= lb.T).all(), where
+
+
+# T, start, window, sinks, tokens: rows past 2^31 bytes in the kernel of many query rows (NEAR and fewer rows), rows past 2^32 in the
+# other, three blocks of 32 query rows of it, the last one of six, or the later ones empty
+@pytest.mark.parametrize("T,start,window,sinks,tokens", [
+    (70, NEAR - 70, 0, 0, None), (70, NEAR - 70, 20000, 17000, None), (70, ROWS - 70, 32300, 40, None),
+    (70, ROWS - 70, 0, 0, None), (70, ROWS - 70, 33000, 3, None), (70, ROWS - 70, 0, 0, 32), (70, ROWS - 70, 33000, 3, 41)])
+def test_rows_past_31_and_32_bits(vc, large, T, start, window, sinks, tokens):  # noqa: F811
+    cache, q, (qh, kh, vh) = large
+    n = T if tokens is None else tokens
+    counts = None if tokens is None else torch.tensor([tokens], dtype=torch.int32, device="cuda")
+    out = torch.full((1, T, HKV, D), 7.5, dtype=torch.bfloat16, device="cuda"), torch.full((1, HKV, T), 7.5, device="cuda")
+    vc.vitcop_window_attn(q[:, :T], cache, start, window, sinks, n_samples=counts, out=out)
+    assert_rows(out[0][0], out[1][0], qh, kh, vh, S.window_sees(start, n, start + n, window, sinks), "window")
+    assert bool((out[0][:, n:] == 7.5).all()) and bool((out[1][:, :, n:] == 7.5).all())
+
+
+@pytest.mark.parametrize("T,start,tokens", [(64, NEAR - 64, None), (64, ROWS - 64, None), (45, ROWS - 45, 20), (45, ROWS - 64, None)])
+def test_trees_past_31_and_32_bits(vc, large, T, start, tokens):  # noqa: F811
+    """The drafts are rows of the cache behind the first `start`."""
+    cache, q, (qh, kh, vh) = large
+    n = T if tokens is None else tokens
+    counts = None if tokens is None else torch.tensor([tokens], dtype=torch.int32, device="cuda")
+    masks = trees(np.random.default_rng(T), 1, T)[0]
+    signed = torch.tensor([m - 2 ** 64 if m >= 2 ** 63 else m for m in masks], device="cuda")
+    out = torch.full((1, T, HKV, D), 7.5, dtype=torch.bfloat16, device="cuda"), torch.full((1, HKV, T), 7.5, device="cuda")
+    vc.vitcop_tree_attn(q[:, :T], cache.k[:, start:start + T], cache.v[:, start:start + T], signed, cache, start, n_samples=counts,
+                        out=out)
+    assert_rows(out[0][0], out[1][0], qh, kh, vh, S.tree_sees(start, n, masks), "tree")
+    assert bool((out[0][:, n:] == 7.5).all()) and bool((out[1][:, :, n:] == 7.5).all())
