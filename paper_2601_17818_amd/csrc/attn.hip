@@ -586,10 +586,11 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
             const u32x4 desc = (j & 1) ? (in_b ? v_desc_b : v_desc) : (in_b ? k_desc_b : k_desc);
             unsigned lane_at = lane_off;
             if constexpr (TREE) {
-                if (in_b) {                          // (there is one such tile; drafts that no token sees: past the range)
+                if (in_b) {                          // (there is one such tile; drafts that no token sees: past the range, which ends
+                                                     // below 2^31, by so little that 3 rows of 2^25 bytes do not pass 2^32)
                     const int r = GPW * wv + GROUPS * (lane / LPR) + i;
                     const unsigned off_b = (unsigned)(GPW * wv + GROUPS * (lane / LPR)) * of_b + ((unsigned)(lane % LPR) << 4);
-                    lane_at = !(seen >> r & 1) ? 0xFFFFF000u : off_b;
+                    lane_at = !(seen >> r & 1) ? 0x80000000u : off_b;
                 }
             }
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"

@@ -124,3 +124,31 @@ def test_trees_past_31_and_32_bits(vc, large, T, start, tokens):  # noqa: F811
                         out=out)
     assert_rows(out[0][0], out[1][0], qh, kh, vh, S.tree_sees(start, n, masks), "tree")
     assert bool((out[0][:, n:] == 7.5).all()) and bool((out[1][:, :, n:] == 7.5).all())
+
+
+@pytest.mark.parametrize("T,G,n,row", [(64, 1, 70, 6144), (33, 2, 0, 6144), (64, 1, 70, (1 << 24) - 8), (20, 1, 70, (1 << 24) - 8),
+                                       (5, 1, 0, (1 << 24) - 8)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_drafts_of_wide_rows_that_no_token_sees(vc, T, G, n, row, d):  # noqa: F811
+    """Keys and values of drafts in rows of `row` elements, up to the longest that there may be; every third draft is seen by none
+    and holds NaN and infinities, and so does what lies beside them."""
+    rng = np.random.default_rng(T)
+    f64 = O.bf16_to_f64
+    q, k, v = bits(rng, (T, G, d)), bits(rng, (n + T, 1, d)), bits(rng, (n + T, 1, d))
+    hidden = sum(1 << j for j in range(1, T, 3))
+    masks = [((2 << t) - 1) & ~hidden for t in range(T)]
+    k2, v2 = k[n:].copy(), v[n:].copy()
+    k2[1::3], v2[1::3] = 0xFF80, 0x7FC0
+    views = []
+    for x in (k2, v2):
+        wide = torch.empty((T - 1) * row + 2 * d, dtype=torch.bfloat16, device="cuda")
+        wide[:2 * d], wide[-2 * d:] = float("nan"), float("nan")
+        view = wide[d:].as_strided((1, T, 1, d), (T * row, row, d, 1))
+        view.copy_(dev(x)[None])
+        views.append(view)
+    cache = vc.Cache(dev(k[:n])[None], dev(v[:n])[None])
+    signed = torch.tensor([m - 2 ** 64 if m >= 2 ** 63 else m for m in masks], device="cuda")
+    out, lse = vc.vitcop_tree_attn(dev(q)[None], *views, signed, cache, n)
+    want = S.attend(f64(q), f64(k), f64(v), S.tree_sees(n, T, masks))
+    ob, lb = bounds(want, d, n + T)
+    assert (np.abs(host_f64(out)[0] - want["out"]) <= ob).all() and (np.abs(host_f64(lse)[0] - want["lse"]) <= lb.T).all()
