@@ -1000,11 +1000,11 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
         if (query >= 0) {
             const float inv = SPANS && l_tot == 0.f ? 0.f : 1.0f / l_tot;
             uint16_t* op = out + ((int64_t)b * N + query) * q_rs + h * D;
-            float* lp = lse + ((int64_t)b * Hq + h) * N + query;
+            int tok = 0, head = 0;                         // SPANS
             if constexpr (SPANS) {
-                const int tok = query / win.a.G, head = hk * win.a.G + query - tok * win.a.G;
+                tok = query / win.a.G;
+                head = hk * win.a.G + query - tok * win.a.G;
                 op = out + ((int64_t)b * win.a.T + tok) * q_rs + (int64_t)head * D;
-                lp = lse + ((int64_t)b * Hq + head) * win.a.T + tok;
             }
 #pragma unroll
             for (int db = 0; db < DB; ++db)
@@ -1015,8 +1015,11 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_wide_kernel(
                     pk.y = pack_bf16(o[u][db][4 * r4 + 2] * inv, o[u][db][4 * r4 + 3] * inv);
                     *reinterpret_cast<uint2*>(op + db * 32 + 8 * r4 + 4 * g) = pk;
                 }
-            if (lse && g == 0)
-                *lp = SPANS && l_tot == 0.f ? -INFINITY : (m_ref[u] + __builtin_amdgcn_logf(l_tot)) * 0.6931471805599453f;
+            if (lse && g == 0) {
+                int64_t row = ((int64_t)b * Hq + h) * N + query;
+                if constexpr (SPANS) row = ((int64_t)b * Hq + head) * win.a.T + tok;
+                lse[row] = SPANS && l_tot == 0.f ? -INFINITY : (m_ref[u] + __builtin_amdgcn_logf(l_tot)) * 0.6931471805599453f;
+            }
         }
     }
 }
