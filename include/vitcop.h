@@ -628,7 +628,8 @@ int vitcop_rope_axes(const vitcop_rope_axes_t* R, void* stream);
  * (start_b: start, or start_samples[b] clamped to [0, start]) and sees the rows j <= p with j > p - window or j < sinks;
  * window 0: all of j <= p.  A token's step (T = 1), a further question (T tokens behind a long conversation) and a
  * right-padded prompt (start 0, n_samples) are the same call.  Rows of the cache that no token of the call sees may
- * hold anything.
+ * hold anything.  A window counts rows of the cache: where a pruned prefill has left out tokens, its last `window` rows reach
+ * back further than `window` positions, and the results are not those of a model whose window is of positions.
  *   q [B,T,Hq,d] bf16;  out [B,T,Hq,d] bf16 dense, no part of an input;  lse_out [B,Hq,T] fp32 natural-log-sum-exp, may be NULL
  *   scale 0 selects 1/sqrt(d);  query head h reads KV head h / (Hq/Hkv).  Probabilities go into the sums over V with 24 bits
  *   of up to 16 query rows T*Hq/Hkv of a KV head (as in vitcop_decode_attn), 16 of up to 32, and 8 of more (as in
@@ -648,6 +649,9 @@ int vitcop_window_attn(const uint16_t* q, int64_t q_row_stride, int64_t q_batch_
  * bit j of tree[b*tree_batch_stride + t] is set (its ancestors in a tree, and itself).  A token that sees nothing gets zeros
  * and an lse of -inf.  The drafts' keys and values lie beside the cache, which is not written; vitcop_cache_append takes
  * the accepted ones over.  Rows of the cache from start_b on and drafts that no token sees may hold anything.
+ * The bits of the probabilities go by T*Hq/Hkv, as in vitcop_window_attn: with more than 32 query rows of a KV head a drafted
+ * token's output differs from that of its decoding step (24 bits) by up to 2^-8 of the sum of p |V| beside the two outputs' own
+ * roundings, with 17 to 32 by 2^-16, with fewer by the order of the sums.
  *   q [B,T,Hq,d], k, v [B,T,Hkv,d] bf16;  tree [B,T] uint64, or one [T] for all samples (tree_batch_stride 0)
  *   C: k and v may be NULL where start is 0
  *   out, lse_out, scale, ws and limits as vitcop_window_attn's; 0 <= start <= capacity; row strides of k and v at least
@@ -662,8 +666,9 @@ int vitcop_tree_attn(const uint16_t* q, int64_t q_row_stride, int64_t q_batch_st
 
 /* Rows to the caches of all layers in one launch (for 64 of them, where they are given one by one): row i < n_b of
  * sample b, which is row idx[b,i] of k and v (i, without idx), goes to row start + i of its cache in layer l: start[l], or
- * start_samples[l*B + b] (caches of a pruned prefill have lengths of their own in each layer).  n_b: `rows`, or n_samples[b] clamped to [0, rows].  Sources outside
- * [0,T) and targets outside [0,capacity) are skipped on the device; all other rows stay as they were.
+ * start_samples[l*B + b] (caches of a pruned prefill have lengths of their own in each layer).  n_b: `rows`, or n_samples[b]
+ * clamped to [0, rows].  Sources outside [0,T) (with T 0, all) and targets outside [0,capacity) are skipped; all other rows stay
+ * as they were.
  *   k_cache, v_cache: host arrays of n_layers device pointers, each [B,capacity,Hkv,d]; with a cache_layer_stride other than
  *   0, arrays of one, the first layer's, behind which the others lie that many elements apart
  *   start: host [n_layers], not looked at with start_samples.  start[l] + rows <= capacity is checked; without idx, rows <= T.

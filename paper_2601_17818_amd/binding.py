@@ -1341,6 +1341,7 @@ def vitcop_cache_append(k_caches, v_caches, k, v, start=None, start_samples=None
         starts = (C.c_int * L)(*starts)
     (k_table, k_at, *k_strides), (v_table, v_at, *v_strides) = args
     desc = _CACHE_APPEND.pack(L, B, capacity, Hkv, d, T, rows, k_table and C.addressof(k_table), v_table and C.addressof(v_table),
-                              given if B and capacity else 0, k_at, v_at, *k_strides, *v_strides, C.addressof(starts) if starts is not None else 0, starts_at, idx_at,
+                              given if B and capacity else 0, k_at, v_at, *k_strides, *v_strides,
+                              C.addressof(starts) if starts is not None else 0, starts_at, idx_at,
                               _counts(n_samples, "n_samples", (B,), dev) if n_samples is not None else 0)
     _check(lib.vitcop_cache_append(desc, _stream_of(dev)))

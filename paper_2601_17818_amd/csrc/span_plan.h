@@ -40,10 +40,11 @@ struct SpanSizes {
 // Many rows, in tiles of 64 keys: one block of 128 rows takes 0.88 us a tile where CUs are left over and 1.0 where not, and 7 to
 // begin and end; two blocks 1.6 to 1.8 and 8, so that one is better where a workgroup has few tiles or all fit at once, two where
 // there are rounds of workgroups.  (Drafts take one: with two the registers do not hold the masks, 2.0 us a tile even on an idle
-// chip.)  Measured, us: 317 tokens of 7 query heads x 4 KV heads behind 16384 rows one block 3: 91.0, 7: 93.5, two 3: 132, 5: 89.6,
-// 7: 81.9, 14: 98.4; 100 behind 8000 one 4: 38.8, 8: 29.0, 10: 30.4, two 7: 40.2, 21: 31.9; 2 x 8192 with a window of 2048 one 487,
-// two 421; 2 x 2000 with one of 500 54.6, 53.3; 640 tokens of 32 heads 15.9, 24.8; 8 x 64 drafts x 28 / 4 heads behind 4096
-// 1: 63.1, 2: 47.9, 3: 62.1; of 64: 4 x 64 x 16 / 4 behind 3000 1: 38.8, 4: 19.7, 8: 18.3, 16: 25.4.
+// chip.  Those of d = 64 are priced like windows, three workgroups to a CU, though their 170 registers leave room for two.)
+// Measured, us: 317 tokens of 7 query heads x 4 KV heads behind 16384 rows one block 3: 91.0, 7: 93.5, two 3: 132, 5: 89.6, 7: 81.9,
+// 14: 98.4; 100 behind 8000 one 4: 38.8, 8: 29.0, 10: 30.4, two 7: 40.2, 21: 31.9; 2 x 8192 with a window of 2048 one 487, two 421;
+// 2 x 2000 with one of 500 54.6, 53.3; 640 tokens of 32 heads 15.9, 24.8; 8 x 64 drafts x 28 / 4 heads behind 4096 1: 63.1, 2: 47.9,
+// 3: 62.1; of 64: 4 x 64 x 16 / 4 behind 3000 1: 38.8, 4: 19.7, 8: 18.3, 16: 25.4.
 // Samples of their own lengths: 64 x up to 16000 keys x 28 / 4 1: 263, 2: 211, 8: 224; 12 x 8000 x 16 1: 127, 2: 98.6, 4: 86.7;
 // 40 x 8000 x 28 / 4 1: 116, 3: 75.9, 8: 80.4; 20 x 3000 x 32 1: 104, 2: 112; 8 x 700 tokens behind 3000 x 28 / 4 two blocks 1: 103,
 // 2: 135.

@@ -71,7 +71,7 @@ struct SpanArgs {
     float* lse;
 };
 // In tiles of 64 keys, 128 or 256 query rows a workgroup (blocks 1 or 2); of more than one slice the partials are left in
-// part_o and part_ml.  Spans of less than 2^32 - 2^26 bytes.
+// part_o and part_ml.  Spans that end, with 256 more rows, below 2^32 bytes.
 int launch_attn_spans(const SpanArgs& A, int d, int blocks, hipStream_t s);
 // What vitcop_window_attn and vitcop_tree_attn (with `tree`, and the drafts' k and v) are given, checked.
 struct SpanCall {
