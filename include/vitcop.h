@@ -584,8 +584,9 @@ int vitcop_project_mx4(const uint16_t* x, int64_t x_row_stride, const uint8_t* w
  *   start_samples int32 [B]: rows that sample b's cache holds before the call (NULL: `start` of them)
  *   n_samples     int32 [B]: sample b has min(max(n_samples[b], 0), T) tokens, the first ones of its T (NULL: T).  What
  *                 belongs to its other tokens is neither read nor written: outputs there stay as they were.
- * Strides are in elements and multiples of 8; a token's heads lie side by side, so that q, k and v may be views of fused
- * QKV rows.  A row stride is not looked at where T is 1.
+ * Strides are in elements and multiples of 8, those of rows below 2^31 and those of samples below 2^46; a token's heads lie
+ * side by side, so that q, k and v may be views of fused QKV rows.  A row stride is not looked at where T is 1, a batch stride
+ * where B is 1.
  */
 typedef struct {
     int B, capacity, Hkv, d;
@@ -636,7 +637,7 @@ int vitcop_rope_axes(const vitcop_rope_axes_t* R, void* stream);
  *   vitcop_prefill_attn); all sums are fp32
  *   ws: device scratch of ws_bytes >= vitcop_window_attn_workspace_bytes, NULL where that is 0 (it is 0 too where the
  *   sizes are refused)
- * d in {64,128}; Hq % Hkv == 0; 0 <= start, start + T <= capacity; window, sinks >= 0; B, Hkv <= 65535;
+ * d in {64,128}; Hq % Hkv == 0; 0 <= start, start + T <= capacity <= 2^30; window, sinks >= 0; B, Hkv <= 65535; B*Hkv < 2^23;
  * B*T*Hq < 2^28; at most 32*65535 query rows T*Hq/Hkv where a sample's rows in reach are 4 GiB and more. */
 size_t vitcop_window_attn_workspace_bytes(int B, int T, int start, int Hq, int Hkv, int d, int window, int sinks);
 int vitcop_window_attn(const uint16_t* q, int64_t q_row_stride, int64_t q_batch_stride, const vitcop_cache_t* C,
@@ -654,8 +655,8 @@ int vitcop_window_attn(const uint16_t* q, int64_t q_row_stride, int64_t q_batch_
  * roundings, with 17 to 32 by 2^-16, with fewer by the order of the sums.
  *   q [B,T,Hq,d], k, v [B,T,Hkv,d] bf16;  tree [B,T] uint64, or one [T] for all samples (tree_batch_stride 0)
  *   C: k and v may be NULL where start is 0
- *   out, lse_out, scale, ws and limits as vitcop_window_attn's; 0 <= start <= capacity; row strides of k and v at least
- *   Hkv*d and below 2^24 (T > 1). */
+ *   out, lse_out, scale, ws and limits as vitcop_window_attn's; 0 <= start <= capacity, start + T <= 2^30; row strides of k and
+ *   v at least Hkv*d and below 2^24 (T > 1). */
 #define VITCOP_MAX_DRAFTS 64
 size_t vitcop_tree_attn_workspace_bytes(int B, int T, int start, int Hq, int Hkv, int d);
 int vitcop_tree_attn(const uint16_t* q, int64_t q_row_stride, int64_t q_batch_stride, const vitcop_cache_t* C,
@@ -674,7 +675,7 @@ int vitcop_tree_attn(const uint16_t* q, int64_t q_row_stride, int64_t q_batch_st
  *   start: host [n_layers], not looked at with start_samples.  start[l] + rows <= capacity is checked; without idx, rows <= T.
  *   k, v [n_layers,B,T,Hkv,d] with strides (the row stride is not looked at where T is 1); one of the two may be NULL,
  *   and its caches too.  They overlap no cache.
- * Hkv*d % 8 == 0; B <= 65535; rows*Hkv*d < 2^31. */
+ * Hkv*d % 8 == 0; B <= 65535; rows*Hkv*d < 2^31; layers lie at most 2^61 elements apart in all. */
 typedef struct {
     int n_layers, B, capacity, Hkv, d, T, rows;
     uint16_t* const* k_cache;
